@@ -339,6 +339,115 @@ int gorio_search_resident_noalloc(const gorio_index_desc *desc, const void *page
                                   uint32_t W, uint32_t *out_ids_dev, void *out_dists_dev,
                                   uint32_t *out_pages_distinct_dev, void *cuda_stream);
 
+/*
+ * ---- Paged key/value cache -------------------------------------------------------------------
+ *
+ * What follows the search on the same GPU (no counterpart in the paper): the passages that a search
+ * returns are read by a model whose attention keeps their keys and values in pages of device
+ * memory.  A request owns a row of a page table; its token at position p lives in page
+ * table[p / page_size], place p % page_size.  Pages may be shared between requests as long as nothing
+ * is stored to them.  Three calls work on such a cache: gorio_page_tables gives new tokens their pages
+ * and slots, gorio_cache_store puts their keys and values there, gorio_paged_attention lets them
+ * attend.  With 16 tokens of 128 16-bit numbers, one head's page is 4 KB.
+ *
+ * These calls enqueue kernels on `cuda_stream` of the CURRENT device and return without waiting; they
+ * allocate nothing and may be captured into a CUDA graph.  All pointers are DEVICE memory of that
+ * device and stay valid until the kernels have run.  Errors: INVALID_ARG (a precondition below),
+ * CUDA (a launch failed); gorio_last_error(NULL) says which.  Strides count elements.  What the calls
+ * cannot check without waiting (lengths, table entries) never leads to an access outside the
+ * arrays: lengths and starts are cut to what tables and tensors hold, a page number outside
+ * [0, n_pages) reads as zeros, a slot outside the cache is skipped.
+ */
+enum { GORIO_KV_BF16 = 0, GORIO_KV_FP16 = 1 };
+
+/*
+ * Page tables and slot maps of one step.  Request r has lengths[r] cached tokens, whose pages are in its
+ * table row, and brings new_lens[r] new ones; it needs ceil((lengths+new_lens)/page_size) -
+ * ceil(lengths/page_size) more pages.  Requests are served in order: request r is served when its
+ * numbers are not negative, its tokens fit its table row, the new tokens of requests 0..r are at most
+ * n_tokens, and the pages that the valid ones of requests 0..r need are at most the free ones.  So from the first
+ * request that does not find its pages on, none is served.  Pages come from the top of the stack:
+ * the first new page is free_pages[free_count-1].
+ *   tables        i32 [n_requests] rows of table_width entries, table_stride apart; new pages are
+ *                 written to it, nothing else is.
+ *   free_pages    i32 [free_capacity]; free_count i32 [1] (cut to [0, free_capacity]).
+ *   n_tokens      the sum of the new_lens that are positive, as the caller knows it; rows of the
+ *                 outputs past that sum are -1.
+ *   slots         i64 [n_tokens]: page * page_size + place, -1 where the request is not served.
+ *   positions, requests  i32 [n_tokens]: the token's position and its request.
+ *   starts        i32 [n_requests+1]: sums of the (positive) new_lens, at most n_tokens.
+ *   out_lengths   i32 [n_requests]: lengths + new_lens where served, else lengths.
+ *   out_served    i32 [n_requests]: 1 or 0.      out_free_count  i32 [1].
+ * lengths and free_count are read only: outputs must not overlap inputs.
+ * Preconditions: page_size >= 1, table_width >= 1, table_width * page_size < 2^31, n_requests <= 2^20,
+ * n_tokens < 2^31.
+ */
+typedef struct {
+  const int32_t *lengths, *new_lens;
+  int32_t *tables;
+  const int32_t *free_pages, *free_count;
+  int64_t *slots;
+  int32_t *positions, *requests, *starts, *out_lengths, *out_served, *out_free_count;
+  int64_t table_stride;
+  uint32_t n_requests, table_width, free_capacity, page_size, n_tokens, reserved;
+} gorio_page_tables_desc;
+int gorio_page_tables(const gorio_page_tables_desc *d, void *cuda_stream);
+
+/*
+ * Store of new keys and values: key_pages[slot / page_size][h][slot % page_size][:] = keys[t][h][:] for
+ * slot = slots[t], and the same for values.  Negative slots are skipped.  Two tokens of the same slot:
+ * either may win.  16-bit elements; the head's elements are contiguous everywhere.
+ * Preconditions: dim a multiple of 8, every stride a multiple of 8, pointers 16-byte aligned,
+ * n_pages * page_size < 2^31.
+ */
+typedef struct {
+  const void *keys, *values;
+  void *key_pages, *value_pages;
+  const int64_t *slots;
+  int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+  int64_t kp_page_stride, kp_head_stride, kp_token_stride, vp_page_stride, vp_head_stride, vp_token_stride;
+  uint32_t n_tokens, n_heads, dim, n_pages, page_size, reserved;
+} gorio_cache_store_desc;
+int gorio_cache_store(const gorio_cache_store_desc *d, void *cuda_stream);
+
+/*
+ * Attention of each request's new tokens over its cached keys and values.  Request r's queries are
+ * rows starts[r] .. starts[r+1]-1 of q; it has lengths[r] keys in the cache, its own included.  Query i
+ * of n stands at position p = lengths[r] - n + i.  It sees the keys j < lengths[r] with, if causal,
+ * j <= p and, if window > 0, j > p - window.  Query head h reads key head h / (n_heads / n_kv_heads):
+ *   x_j = scale * q.k_j;  if softcap > 0: x_j = softcap * tanh(x_j / softcap);
+ *   if slopes: x_j += slopes[h] * (j - p);   out = sum_j softmax(x)_j v_j;   lse = log sum_j exp(x_j).
+ * A query that sees no key gets out = 0 and lse = -inf.  Sums, maxima and the softmax are held in 32
+ * bits; the weights are rounded to the cache's type for the sum over values, and out once at the end.
+ * Keys and values that no query of the request sees are not read into any result, whatever they hold.
+ *   q, out        [n_tokens][n_heads][dim]; key_pages, value_pages [n_pages][n_kv_heads][page_size][dim],
+ *                 in any order of the outer axes (strides); lse f32 [n_tokens][n_heads] or NULL.
+ *   tables        i32 [n_requests] rows of table_width entries, table_stride apart.
+ *   max_new       at least the most new tokens of a request: a hint for the choice of the kernel.
+ *   workspace     gorio_attention_workspace_bytes() bytes, 256-byte aligned, whose first 64 KB were zero before
+ *                 its first use.  Each call leaves them zero; calls that may overlap need one each.
+ * Preconditions: dtype one of GORIO_KV_*, dim 64, 96 or 128, n_heads a multiple of n_kv_heads, every
+ * stride a multiple of 8 and pointer 16-byte aligned, scale > 0 and finite, softcap >= 0 and finite,
+ * page_size a multiple of 8, table_width * page_size < 2^31, n_requests <= 2^20.
+ */
+typedef struct {
+  const void *q, *key_pages, *value_pages;
+  void *out;
+  float *lse;
+  const int32_t *tables, *lengths, *starts;
+  const float *slopes;
+  void *workspace;
+  int64_t q_token_stride, q_head_stride, o_token_stride, o_head_stride;
+  int64_t kp_page_stride, kp_head_stride, kp_token_stride, vp_page_stride, vp_head_stride, vp_token_stride;
+  int64_t table_stride;
+  uint32_t n_requests, n_tokens, n_heads, n_kv_heads, dim, n_pages, page_size, table_width, dtype, causal, window, max_new;
+  float scale, softcap;
+} gorio_paged_attention_desc;
+int gorio_paged_attention(const gorio_paged_attention_desc *d, void *cuda_stream);
+
+/* Bytes of the workspace above on CUDA device `cuda_device`; 0 if there is no such device. */
+uint64_t gorio_attention_workspace_bytes(int cuda_device);
+
 /* Static strings; never NULL. */
 const char *gorio_status_str(int status);
 /* Human-readable detail of the last non-OK status on this index (valid until the next call);

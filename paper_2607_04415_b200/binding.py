@@ -15,6 +15,7 @@ EXPORTED_SYMBOLS = [
     "gorio_index_open", "gorio_cache_config", "gorio_set_tuning", "gorio_search", "gorio_search_host",
     "gorio_stats", "gorio_stats_reset", "gorio_index_close", "gorio_status_str", "gorio_last_error",
     "gorio_search_resident_noalloc", "gorio_link_probe",
+    "gorio_page_tables", "gorio_cache_store", "gorio_paged_attention", "gorio_attention_workspace_bytes",
 ]
 
 STATUS_NAMES = {0: "OK", 1: "INVALID_ARG", 2: "CUDA", 3: "NOMEM", 4: "STATE", 5: "TIMEOUT",
@@ -97,6 +98,10 @@ def load_library():
     for name in EXPORTED_SYMBOLS:
         if name not in ("gorio_status_str", "gorio_last_error"):
             getattr(lib, name).restype = ctypes.c_int
+    for name in ("gorio_page_tables", "gorio_cache_store", "gorio_paged_attention"):
+        getattr(lib, name).argtypes = [ctypes.c_char_p, vp]      # a packed descriptor, a stream
+    lib.gorio_attention_workspace_bytes.argtypes = [ctypes.c_int]
+    lib.gorio_attention_workspace_bytes.restype = ctypes.c_uint64
     _LIB = lib
     return lib
 

@@ -1,0 +1,271 @@
+// What the kernels of the paged key/value cache share: the arguments of an attention call, the
+// geometry of its units of work, and the plan that gives every block an equal share of them.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace gorio {
+namespace paged {
+
+typedef uint8_t u8;
+typedef uint16_t u16;
+typedef uint32_t u32;
+typedef uint64_t u64;
+typedef int64_t i64;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// Everything an attention kernel needs, passed by value.  Strides are in elements.
+struct Attn {
+  const void *q, *kp, *vp;
+  void *out;
+  float *lse;                  // [n_tokens][hq] or NULL
+  const int *tables, *lengths, *starts;
+  const float *slopes;         // [hq] or NULL
+  i64 q_t, q_h, o_t, o_h, k_p, k_h, k_t, v_p, v_h, v_t, tab_r;
+  u32 n_req, n_tok, hq, hkv, group, page, n_pages, width;
+  u32 causal, window;          // window 0: none
+  float scale;                 // of the dot product
+  float softcap;               // 0: none
+  // workspace: two partial results for every block, and a counter of arrivals for each
+  float *part_o, *part_ml;
+  u32 *arrived;
+};
+
+// One request as the kernels see it: keys it can have at most, its new tokens and where their rows
+// start.  Bad lengths or starts are cut to what the tables and the query tensor hold, so that no
+// access leaves them.
+struct Request {
+  int len, n, q0;
+};
+
+__device__ __forceinline__ Request request_at(const Attn &a, u32 r) {
+  Request x;
+  const i64 cap = (i64)a.width * a.page;
+  const int l = a.lengths[r], s0 = a.starts[r], s1 = a.starts[r + 1];
+  x.len = l < 0 ? 0 : (i64)l > cap ? (int)cap : l;
+  x.q0 = s0 < 0 ? 0 : s0 > (int)a.n_tok ? (int)a.n_tok : s0;
+  const int e = s1 > (int)a.n_tok ? (int)a.n_tok : s1;
+  x.n = e > x.q0 ? e - x.q0 : 0;
+  return x;
+}
+
+// A unit is up to ROWS rows -- (token, query head of the group) pairs, token outer -- of one request
+// and one key head.  Its visible keys are [lo, hi) over all its rows, in whole tiles of TK keys from
+// tile `first`; a unit without visible keys still has one (fully masked) tile, which writes its rows.
+struct Span {
+  int lo, hi, first, tiles;
+};
+
+template <int ROWS, int TK>
+__device__ __forceinline__ Span unit_span(const Attn &a, int len, int n, int m) {
+  const i64 rows = (i64)n * a.group;
+  const i64 r0 = (i64)m * ROWS, r1 = min(rows, r0 + ROWS);
+  const int ta = (int)(r0 / a.group), tb = (int)((r1 - 1) / a.group);
+  Span s;
+  s.hi = a.causal ? min(len, len - n + tb + 1) : len;
+  s.lo = a.window ? (int)max((i64)0, (i64)len - n + ta - a.window + 1) : 0;
+  if (s.hi <= s.lo) { s.lo = s.hi = 0; s.first = 0; s.tiles = 1; return s; }
+  s.first = s.lo / TK;
+  s.tiles = (s.hi + TK - 1) / TK - s.first;
+  return s;
+}
+
+template <int ROWS>
+__device__ __forceinline__ int unit_count(const Attn &a, int n) {
+  return (int)(((i64)n * a.group + ROWS - 1) / ROWS);
+}
+
+// The plan.  All tiles of a call, in the order (request, key head, unit, tile), are one line of `total`
+// tiles; block i of N takes tiles [total*i/N, total*(i+1)/N).  Every block finds its own place from the
+// lengths alone, so no host step and no extra launch stands between the lengths and the work.  A unit
+// that is cut by a block boundary is computed in parts, which the last of its blocks to finish joins
+// in the order of the key axis: results do not depend on which block that is.
+struct Cursor {
+  u32 r, h;
+  int m;           // unit of (r, h)
+  int at;          // next tile of the unit, counted from its first
+  Request req;
+  Span span;
+};
+
+struct PlanShared {
+  u64 warp_sum[32];
+  u64 found_before;
+  u32 found_r;
+  u32 pad;
+};
+
+__device__ __forceinline__ u64 part_begin(u64 total, u32 i, u32 n) { return total * i / n; }
+// the block that owns tile x: the largest i with total*i/n <= x
+__device__ __forceinline__ u32 part_owner(u64 total, u64 x, u32 n) { return (u32)(((x + 1) * n - 1) / total); }
+
+// Tiles of request r over all its units (of one key head).  Warp-collective; lane's own request is r
+// (in range where `have`); requests of many units are summed by the whole warp.
+template <int ROWS, int TK>
+__device__ __forceinline__ u32 request_tiles(const Attn &a, u32 r, bool have) {
+  const u32 lane = threadIdx.x & 31;
+  Request q{0, 0, 0};
+  if (have) q = request_at(a, r);
+  const int units = have ? unit_count<ROWS>(a, q.n) : 0;
+  u32 sum = 0;
+  if (units <= 2) {
+    for (int m = 0; m < units; ++m) sum += (u32)unit_span<ROWS, TK>(a, q.len, q.n, m).tiles;
+  }
+  u32 big = __ballot_sync(0xffffffffu, units > 2);
+  while (big) {
+    const int src = __ffs(big) - 1;
+    big &= big - 1;
+    const int len = __shfl_sync(0xffffffffu, q.len, src), n = __shfl_sync(0xffffffffu, q.n, src);
+    const int cnt = __shfl_sync(0xffffffffu, units, src);
+    u32 s = 0;
+    for (int m = (int)lane; m < cnt; m += 32) s += (u32)unit_span<ROWS, TK>(a, len, n, m).tiles;
+    s = __reduce_add_sync(0xffffffffu, s);
+    if ((int)lane == src) sum = s;
+  }
+  return sum;
+}
+
+// Inclusive sum over the block of one value a thread; `all` is the block's sum.  Two barriers.
+template <int NT>
+__device__ __forceinline__ u64 block_scan(u64 v, PlanShared &sh, u64 &all) {
+  const u32 lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  u64 x = v;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const u64 y = __shfl_up_sync(0xffffffffu, x, d);
+    if ((int)lane >= d) x += y;
+  }
+  if (lane == 31) sh.warp_sum[warp] = x;
+  __syncthreads();
+  u64 before = 0;
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < NT / 32; ++w) {
+    const u64 s = sh.warp_sum[w];
+    if (w < (int)warp) before += s;
+    all += s;
+  }
+  __syncthreads();
+  return x + before;
+}
+
+// Sets the cursor to the tile `offset` tiles after the first tile of request r.  Warp-collective, the same
+// for all warps.
+template <int ROWS, int TK>
+__device__ __forceinline__ Cursor cursor_in(const Attn &a, u32 r, u64 offset) {
+  const u32 lane = threadIdx.x & 31;
+  Cursor c;
+  c.r = r;
+  c.req = request_at(a, r);
+  const int units = unit_count<ROWS>(a, c.req.n);
+  u32 per_head = 0;
+  for (int m = (int)lane; m < units; m += 32) per_head += (u32)unit_span<ROWS, TK>(a, c.req.len, c.req.n, m).tiles;
+  per_head = __reduce_add_sync(0xffffffffu, per_head);
+  c.h = (u32)(offset / per_head);
+  u32 o = (u32)(offset % per_head);
+  c.m = 0;
+  c.at = 0;
+  for (int base = 0; base < units; base += 32) {
+    const int m = base + (int)lane;
+    const u32 t = m < units ? (u32)unit_span<ROWS, TK>(a, c.req.len, c.req.n, m).tiles : 0u;
+    u32 x = t;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const u32 y = __shfl_up_sync(0xffffffffu, x, d);
+      if ((int)lane >= d) x += y;
+    }
+    const u32 hit = __ballot_sync(0xffffffffu, o < x);
+    if (hit) {
+      const int src = __ffs(hit) - 1;
+      c.m = base + src;
+      c.at = (int)(o - (__shfl_sync(0xffffffffu, x, src) - __shfl_sync(0xffffffffu, t, src)));
+      break;
+    }
+    o -= __shfl_sync(0xffffffffu, x, 31);
+  }
+  c.span = unit_span<ROWS, TK>(a, c.req.len, c.req.n, c.m);
+  return c;
+}
+
+// The next unit after the cursor's; false at the end of the line.
+template <int ROWS, int TK>
+__device__ __forceinline__ bool next_unit(const Attn &a, Cursor &c) {
+  c.at = 0;
+  if (c.m + 1 < unit_count<ROWS>(a, c.req.n)) {
+    ++c.m;
+  } else if (c.h + 1 < a.hkv) {
+    ++c.h;
+    c.m = 0;
+  } else {
+    do {
+      if (++c.r >= a.n_req) return false;
+      c.req = request_at(a, c.r);
+    } while (c.req.n == 0);
+    c.h = 0;
+    c.m = 0;
+  }
+  c.span = unit_span<ROWS, TK>(a, c.req.len, c.req.n, c.m);
+  return true;
+}
+
+struct Plan {
+  u64 total, begin, end;   // of the line; [begin, end) is this block's
+  u32 parts;               // blocks that take part
+  Cursor first;
+};
+
+// Block-collective (NT threads).  At least `min_tiles` tiles a block (where there are as many).
+template <int ROWS, int TK, int NT>
+__device__ __forceinline__ Plan make_plan(const Attn &a, PlanShared &sh, u32 min_tiles) {
+  Plan p;
+  const u32 tid = threadIdx.x;
+  u64 all = 0, mine = 0, upto = 0;
+  for (u32 base = 0; base < a.n_req; base += NT) {
+    const u32 r = base + tid;
+    u64 sum;
+    mine = (u64)request_tiles<ROWS, TK>(a, r, r < a.n_req) * a.hkv;
+    upto = block_scan<NT>(mine, sh, sum) + all;
+    all += sum;
+  }
+  p.total = all;
+  u64 want = (all + min_tiles - 1) / min_tiles;
+  p.parts = (u32)min((u64)gridDim.x, max(want, (u64)1));
+  p.begin = p.end = 0;
+  if (blockIdx.x >= p.parts || all == 0) return p;
+  p.begin = part_begin(all, blockIdx.x, p.parts);
+  p.end = part_begin(all, blockIdx.x + 1, p.parts);
+  if (p.begin >= p.end) return p;
+  if (a.n_req <= NT) {
+    if (upto - mine <= p.begin && p.begin < upto) { sh.found_r = tid; sh.found_before = upto - mine; }
+  } else {                                              // the first pass kept only its last round
+    u64 before = 0;
+    for (u32 base = 0; base < a.n_req; base += NT) {
+      const u32 r = base + tid;
+      u64 sum;
+      mine = (u64)request_tiles<ROWS, TK>(a, r, r < a.n_req) * a.hkv;
+      upto = block_scan<NT>(mine, sh, sum) + before;
+      if (upto - mine <= p.begin && p.begin < upto) { sh.found_r = r; sh.found_before = upto - mine; }
+      before += sum;
+      if (before > p.begin) break;
+    }
+  }
+  __syncthreads();
+  p.first = cursor_in<ROWS, TK>(a, sh.found_r, p.begin - sh.found_before);
+  return p;
+}
+
+// Workspace for parts: a block leaves at most two of them, of 256 rows (or blocks on the same SM of fewer).
+constexpr u32 kPartRowsPerSm = 2 * 256;
+constexpr u32 kMaxDim = 128;
+inline u64 part_ml_bytes(u32 sms) { return (u64)sms * kPartRowsPerSm * 2 * sizeof(float); }
+inline u64 part_bytes(u32 sms) { return part_ml_bytes(sms) + (u64)sms * kPartRowsPerSm * kMaxDim * sizeof(float); }
+
+// launchers
+cudaError_t launch_rows(const Attn &a, int dtype, int dim, u32 sms, cudaStream_t s);
+
+}  // namespace paged
+}  // namespace gorio

@@ -1,0 +1,127 @@
+// Warp-level pieces of the attention kernels: asynchronous copies, matrix fragments, the weights'
+// arithmetic, and the end of a row.
+#pragma once
+#include "common.cuh"
+
+namespace gorio {
+namespace paged {
+
+__device__ __forceinline__ u32 smem_addr(const void *p) { return (u32)__cvta_generic_to_shared(p); }
+
+// 16 bytes, of which `bytes` (16 or 0) are read and the rest are zeros
+__device__ __forceinline__ void cp_async16(void *to, const void *from, u32 bytes) {
+  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(smem_addr(to)), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ void ldmatrix4(u32 (&r)[4], const void *p) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(smem_addr(p)) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4t(u32 (&r)[4], const void *p) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(smem_addr(p)) : "memory");
+}
+
+template <typename T>
+__device__ __forceinline__ void mma16816(float (&c)[4], const u32 (&a)[4], u32 b0, u32 b1);
+template <>
+__device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&c)[4], const u32 (&a)[4], u32 b0, u32 b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <>
+__device__ __forceinline__ void mma16816<__half>(float (&c)[4], const u32 (&a)[4], u32 b0, u32 b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+template <typename T>
+__device__ __forceinline__ u32 pack2(float lo, float hi);
+template <>
+__device__ __forceinline__ u32 pack2<__nv_bfloat16>(float lo, float hi) {
+  u32 r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+template <>
+__device__ __forceinline__ u32 pack2<__half>(float lo, float hi) {
+  u32 r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+template <typename T>
+__device__ __forceinline__ float2 unpack2(u32 v);
+template <>
+__device__ __forceinline__ float2 unpack2<__nv_bfloat16>(u32 v) { return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)); }
+template <>
+__device__ __forceinline__ float2 unpack2<__half>(u32 v) { return __half22float2(*reinterpret_cast<const __half2 *>(&v)); }
+
+// whether one of two (eight) 16-bit numbers is an infinity or not a number: its exponent bits are all ones
+template <typename T>
+struct ExponentBits { static constexpr u32 mask = 0x7f80u; };
+template <>
+struct ExponentBits<__half> { static constexpr u32 mask = 0x7c00u; };
+template <typename T>
+__device__ __forceinline__ bool not_finite2(u32 v) {
+  constexpr u32 lo = ExponentBits<T>::mask, hi = lo << 16;
+  return (v & lo) == lo || (v & hi) == hi;
+}
+template <typename T>
+__device__ __forceinline__ bool not_finite8(uint4 v) {
+  return not_finite2<T>(v.x) || not_finite2<T>(v.y) || not_finite2<T>(v.z) || not_finite2<T>(v.w);
+}
+
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// cap * tanh(x / cap) as cap * (1 - 2 / (1 + e^(2x/cap))): the error is some 1e-7 of the cap, where the
+// hardware's tanh is good to 5e-4 of it only, which would show in the weights.
+__device__ __forceinline__ float capped(float x, float cap) {
+  const float e = exp2_approx(x * (2.0f * kLog2e / cap));
+  return cap * (1.0f - __fdividef(2.0f, 1.0f + e));
+}
+
+// Writes four columns of a finished row: acc / sum, rounded once.  A row that sees no key has sum 0 and gives 0 and
+// -inf.  `row` counts (token, head of the group) pairs of the request, `top` is in units of log2.
+template <typename T>
+__device__ __forceinline__ void finish_row(const Attn &a, int q0, i64 row, u32 h, int col, float4 acc, float top, float sum) {
+  const int tok = (int)(row / a.group), head = (int)(row - (i64)tok * a.group) + (int)(h * a.group);
+  const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+  uint2 v = make_uint2(pack2<T>(acc.x * f, acc.y * f), pack2<T>(acc.z * f, acc.w * f));
+  *(uint2 *)((u16 *)a.out + (i64)(q0 + tok) * a.o_t + (i64)head * a.o_h + col) = v;
+  if (col == 0 && a.lse) a.lse[(i64)(q0 + tok) * a.hq + head] = sum == 0.0f ? -INFINITY : top * kLn2 + logf(sum);
+}
+
+// Joins the parts of a unit that blocks i0..i1 left, in the order of the key axis.  Block-collective.
+template <typename T, int D, int ROWS, int NT>
+__device__ __forceinline__ void join_parts(const Attn &a, const Cursor &c, i64 row0, int rows, u32 i0, u32 i1) {
+  for (int x = (int)threadIdx.x; x < rows * (D / 4); x += NT) {
+    const int row = x / (D / 4), col = (x - row * (D / 4)) * 4;
+    float top = -INFINITY, sum = 0.0f;
+    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (u32 i = i0; i <= i1; ++i) {
+      const i64 at = (i64)(2 * i + (i == i0 ? 1 : 0)) * ROWS + row;
+      const float2 ml = __ldcg((const float2 *)(a.part_ml + at * 2));
+      const float4 v = __ldcg((const float4 *)(a.part_o + at * D + col));
+      const float now = fmaxf(top, ml.x), base = now == -INFINITY ? 0.0f : now;
+      const float f0 = exp2_approx(top - base), f1 = exp2_approx(ml.x - base);
+      top = now;
+      sum = sum * f0 + ml.y * f1;
+      acc.x = acc.x * f0 + v.x * f1;
+      acc.y = acc.y * f0 + v.y * f1;
+      acc.z = acc.z * f0 + v.z * f1;
+      acc.w = acc.w * f0 + v.w * f1;
+    }
+    finish_row<T>(a, c.req.q0, row0 + row, c.h, col, acc, top, sum);
+  }
+}
+
+}  // namespace paged
+}  // namespace gorio

@@ -1,0 +1,126 @@
+// C entry points of the paged key/value cache: checks of arguments, then one launch.
+#include <cmath>
+#include <cstdio>
+#include <mutex>
+
+#include "../../include/gorio.h"
+#include "paged/common.cuh"
+#include "paged/entries.h"
+
+namespace gorio { void set_global_error(const char *msg); }
+
+namespace {
+
+using namespace gorio::paged;
+
+int bad(const char *msg) {
+  gorio::set_global_error(msg);
+  return GORIO_ERR_INVALID_ARG;
+}
+
+int launched(cudaError_t e, const char *what) {
+  if (e == cudaSuccess) return GORIO_OK;
+  char buf[160];
+  std::snprintf(buf, sizeof buf, "%s: %s", what, cudaGetErrorString(e));
+  gorio::set_global_error(buf);
+  return GORIO_ERR_CUDA;
+}
+
+bool aligned(const void *p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
+constexpr int kMaxDevices = 64;
+constexpr uint64_t kCounterBytes = 64u << 10;   // one arrival counter a block
+
+// SMs of a device, read once
+int sm_count(int dev) {
+  static int known[kMaxDevices] = {};
+  static std::mutex mu;
+  if (dev < 0 || dev >= kMaxDevices) return 0;
+  std::lock_guard<std::mutex> lk(mu);
+  if (!known[dev]) {
+    int n = 0;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    known[dev] = n;
+  }
+  return known[dev];
+}
+
+}  // namespace
+
+extern "C" int gorio_page_tables(const gorio_page_tables_desc *d, void *cuda_stream) {
+  if (!d || !d->free_count || !d->starts || !d->out_free_count) return bad("page tables: null argument");
+  if (d->n_requests && (!d->lengths || !d->new_lens || !d->tables || !d->out_lengths || !d->out_served))
+    return bad("page tables: null argument");
+  if (d->n_tokens && (!d->slots || !d->positions || !d->requests)) return bad("page tables: null argument");
+  if (d->free_capacity && !d->free_pages) return bad("page tables: null argument");
+  if (d->page_size < 1 || d->table_width < 1 || (uint64_t)d->page_size * d->table_width >= (1ull << 31))
+    return bad("page tables: need page_size >= 1, table_width >= 1 and page_size * table_width < 2^31");
+  if (d->n_requests > (1u << 20) || d->n_tokens >= (1u << 31)) return bad("page tables: at most 2^20 requests and 2^31 - 1 tokens");
+  if (d->table_stride < (int64_t)d->table_width && d->n_requests > 1) return bad("page tables: rows of the table overlap");
+  return launched(launch_page_tables(*d, (cudaStream_t)cuda_stream), "page tables");
+}
+
+extern "C" int gorio_cache_store(const gorio_cache_store_desc *d, void *cuda_stream) {
+  if (!d) return bad("cache store: null argument");
+  if (d->n_tokens == 0 || d->n_heads == 0 || d->n_pages == 0) return GORIO_OK;
+  if (!d->keys || !d->values || !d->key_pages || !d->value_pages || !d->slots) return bad("cache store: null argument");
+  if (d->dim == 0 || d->dim % 8 != 0 || d->page_size < 1 || (uint64_t)d->n_pages * d->page_size >= (1ull << 31))
+    return bad("cache store: need dim a multiple of 8, page_size >= 1 and n_pages * page_size < 2^31");
+  const int64_t strides = d->k_token_stride | d->k_head_stride | d->v_token_stride | d->v_head_stride | d->kp_page_stride | d->kp_head_stride |
+                          d->kp_token_stride | d->vp_page_stride | d->vp_head_stride | d->vp_token_stride;
+  if (strides & 7) return bad("cache store: every stride must be a multiple of 8 elements");
+  if (!aligned(d->keys, 16) || !aligned(d->values, 16) || !aligned(d->key_pages, 16) || !aligned(d->value_pages, 16))
+    return bad("cache store: keys, values and pages must be 16-byte aligned");
+  if (d->n_heads > 65536 || d->dim > 65536 || (uint64_t)d->n_tokens * d->n_heads * d->dim >= (1ull << 40))
+    return bad("cache store: too large");
+  return launched(launch_cache_store(*d, (cudaStream_t)cuda_stream), "cache store");
+}
+
+extern "C" uint64_t gorio_attention_workspace_bytes(int cuda_device) {
+  const int sms = sm_count(cuda_device);
+  return sms ? kCounterBytes + part_bytes((u32)sms) : 0;
+}
+
+extern "C" int gorio_paged_attention(const gorio_paged_attention_desc *d, void *cuda_stream) {
+  if (!d) return bad("paged attention: null argument");
+  if (d->n_requests == 0 || d->n_tokens == 0) return GORIO_OK;
+  if (!d->q || !d->out || !d->tables || !d->lengths || !d->starts || !d->workspace) return bad("paged attention: null argument");
+  if (d->n_pages && (!d->key_pages || !d->value_pages)) return bad("paged attention: null argument");
+  if (d->dtype > GORIO_KV_FP16) return bad("paged attention: unknown dtype");
+  if (d->dim != 64 && d->dim != 96 && d->dim != 128) return bad("paged attention: dim must be 64, 96 or 128");
+  if (d->n_kv_heads < 1 || d->n_heads < 1 || d->n_heads % d->n_kv_heads != 0 || d->n_heads > 65536)
+    return bad("paged attention: n_heads must be a multiple of n_kv_heads");
+  if (d->page_size < 8 || d->page_size % 8 != 0 || d->table_width < 1 || (uint64_t)d->page_size * d->table_width >= (1ull << 31) ||
+      (uint64_t)d->n_pages * d->page_size >= (1ull << 31))
+    return bad("paged attention: need page_size a multiple of 8 and fewer than 2^31 places in a table row and in the cache");
+  if (d->n_requests > (1u << 20) || d->n_tokens >= (1u << 31)) return bad("paged attention: at most 2^20 requests and 2^31 - 1 tokens");
+  if (!(d->scale > 0.0f) || !std::isfinite(d->scale) || !(d->softcap >= 0.0f) || !std::isfinite(d->softcap))
+    return bad("paged attention: need a finite scale > 0 and a finite softcap >= 0");
+  const int64_t strides = d->q_token_stride | d->q_head_stride | d->o_token_stride | d->o_head_stride | d->kp_page_stride | d->kp_head_stride |
+                          d->kp_token_stride | d->vp_page_stride | d->vp_head_stride | d->vp_token_stride;
+  if (strides & 7) return bad("paged attention: every stride must be a multiple of 8 elements");
+  if (!aligned(d->q, 16) || !aligned(d->out, 16) || !aligned(d->key_pages, 16) || !aligned(d->value_pages, 16))
+    return bad("paged attention: q, out and pages must be 16-byte aligned");
+  if (!aligned(d->workspace, 256)) return bad("paged attention: the workspace must be 256-byte aligned");
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return launched(e, "paged attention");
+  const int sms = sm_count(dev);
+  if (sms < 1) return launched(cudaErrorInvalidDevice, "paged attention");
+
+  Attn a{};
+  a.q = d->q; a.kp = d->key_pages; a.vp = d->value_pages; a.out = d->out; a.lse = d->lse;
+  a.tables = d->tables; a.lengths = d->lengths; a.starts = d->starts; a.slopes = d->slopes;
+  a.q_t = d->q_token_stride; a.q_h = d->q_head_stride; a.o_t = d->o_token_stride; a.o_h = d->o_head_stride;
+  a.k_p = d->kp_page_stride; a.k_h = d->kp_head_stride; a.k_t = d->kp_token_stride;
+  a.v_p = d->vp_page_stride; a.v_h = d->vp_head_stride; a.v_t = d->vp_token_stride;
+  a.tab_r = d->table_stride;
+  a.n_req = d->n_requests; a.n_tok = d->n_tokens; a.hq = d->n_heads; a.hkv = d->n_kv_heads; a.group = d->n_heads / d->n_kv_heads;
+  a.page = d->page_size; a.n_pages = d->n_pages; a.width = d->table_width;
+  a.causal = d->causal != 0; a.window = d->window;
+  a.scale = d->scale; a.softcap = d->softcap;
+  a.arrived = (u32 *)d->workspace;
+  a.part_ml = (float *)((char *)d->workspace + kCounterBytes);
+  a.part_o = (float *)((char *)a.part_ml + part_ml_bytes((u32)sms));
+  return launched(launch_rows(a, (int)d->dtype, (int)d->dim, (u32)sms, (cudaStream_t)cuda_stream), "paged attention");
+}
