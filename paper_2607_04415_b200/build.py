@@ -8,11 +8,11 @@ import sys
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libgorio.so")
-SOURCES = ["gorio_api.cu", "search_kernels.cu", "noalloc_entry.cu", "paged_api.cu", "paged_tables.cu", "paged_rows.cu"]
+SOURCES = ["gorio_api.cu", "search_kernels.cu", "noalloc_entry.cu", "paged_api.cu", "paged_tables.cu", "paged_rows.cu", "paged_chunk.cu"]
 HEADERS = ["gorio_internal.h", os.path.join("..", "..", "include", "gorio.h")] + [
     os.path.join("device", f) for f in ("mem.cuh", "queue.cuh", "page_cache.cuh", "scoring.cuh", "arrival.cuh", "batch.cuh",
                                         "list.cuh", "pq.cuh", "scheduler.cuh", "resident.cuh")] + [
-    os.path.join("paged", f) for f in ("common.cuh", "mma.cuh", "entries.h")]
+    os.path.join("paged", f) for f in ("common.cuh", "mma.cuh", "tensor.cuh", "entries.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-pthread"]
 

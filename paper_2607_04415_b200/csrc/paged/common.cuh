@@ -264,7 +264,12 @@ constexpr u32 kMaxDim = 128;
 inline u64 part_ml_bytes(u32 sms) { return (u64)sms * kPartRowsPerSm * 2 * sizeof(float); }
 inline u64 part_bytes(u32 sms) { return part_ml_bytes(sms) + (u64)sms * kPartRowsPerSm * kMaxDim * sizeof(float); }
 
+constexpr u64 kCounterBytes = 64u << 10;   // arrival counters, one a block; zero between calls
+constexpr u32 kErrorWord = (u32)(kCounterBytes / 4) - 1;   // set by a block whose waits ran out
+
 // launchers
+// False where no tensor map of the pages can be made (strides or addresses that it does not hold): nothing ran.
+bool launch_chunk(const Attn &a, int dtype, int dim, u32 sms, cudaStream_t s, cudaError_t *e);
 cudaError_t launch_rows(const Attn &a, int dtype, int dim, u32 sms, cudaStream_t s);
 
 }  // namespace paged

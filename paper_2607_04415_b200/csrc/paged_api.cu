@@ -29,7 +29,6 @@ int launched(cudaError_t e, const char *what) {
 bool aligned(const void *p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
 constexpr int kMaxDevices = 64;
-constexpr uint64_t kCounterBytes = 64u << 10;   // one arrival counter a block
 
 // SMs of a device, read once
 int sm_count(int dev) {
@@ -96,6 +95,7 @@ extern "C" int gorio_paged_attention(const gorio_paged_attention_desc *d, void *
   if (d->n_requests > (1u << 20) || d->n_tokens >= (1u << 31)) return bad("paged attention: at most 2^20 requests and 2^31 - 1 tokens");
   if (!(d->scale > 0.0f) || !std::isfinite(d->scale) || !(d->softcap >= 0.0f) || !std::isfinite(d->softcap))
     return bad("paged attention: need a finite scale > 0 and a finite softcap >= 0");
+  if ((uint64_t)d->n_tokens * d->n_heads >= (1ull << 31)) return bad("paged attention: n_tokens * n_heads must be below 2^31");
   const int64_t strides = d->q_token_stride | d->q_head_stride | d->o_token_stride | d->o_head_stride | d->kp_page_stride | d->kp_head_stride |
                           d->kp_token_stride | d->vp_page_stride | d->vp_head_stride | d->vp_token_stride;
   if (strides & 7) return bad("paged attention: every stride must be a multiple of 8 elements");
@@ -103,8 +103,8 @@ extern "C" int gorio_paged_attention(const gorio_paged_attention_desc *d, void *
     return bad("paged attention: q, out and pages must be 16-byte aligned");
   if (!aligned(d->workspace, 256)) return bad("paged attention: the workspace must be 256-byte aligned");
   int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return launched(e, "paged attention");
+  const cudaError_t found = cudaGetDevice(&dev);
+  if (found != cudaSuccess) return launched(found, "paged attention");
   const int sms = sm_count(dev);
   if (sms < 1) return launched(cudaErrorInvalidDevice, "paged attention");
 
@@ -122,5 +122,10 @@ extern "C" int gorio_paged_attention(const gorio_paged_attention_desc *d, void *
   a.arrived = (u32 *)d->workspace;
   a.part_ml = (float *)((char *)d->workspace + kCounterBytes);
   a.part_o = (float *)((char *)a.part_ml + part_ml_bytes((u32)sms));
+  // Up to 16 rows share a key head in a request: the rows kernel, which is bound by the cache's bytes.  More: the chunk kernel.
+  if ((uint64_t)d->max_new * a.group > 16) {
+    cudaError_t e = cudaSuccess;
+    if (launch_chunk(a, (int)d->dtype, (int)d->dim, (u32)sms, (cudaStream_t)cuda_stream, &e)) return launched(e, "paged attention");
+  }
   return launched(launch_rows(a, (int)d->dtype, (int)d->dim, (u32)sms, (cudaStream_t)cuda_stream), "paged attention");
 }
