@@ -83,9 +83,11 @@ __device__ __forceinline__ float exp2_approx(float x) {
 
 // cap * tanh(x / cap) as cap * (1 - 2 / (1 + e^(2x/cap))): the error is some 1e-7 of the cap, where the
 // hardware's tanh is good to 5e-4 of it only, which would show in the weights.
-__device__ __forceinline__ float capped(float x, float cap) {
-  const float e = exp2_approx(x * (2.0f * kLog2e / cap));
-  return cap * (1.0f - __fdividef(2.0f, 1.0f + e));
+// Result in units of log2; `in` is scale * 2 log2(e) / cap, `out` is cap * log2(e).
+__device__ __forceinline__ float capped_log2(float dot, float in, float out) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + exp2_approx(dot * in)));
+  return fmaf(-2.0f * out, r, out);
 }
 
 // Writes four columns of a finished row: acc / sum, rounded once.  A row that sees no key has sum 0 and gives 0 and
@@ -99,27 +101,55 @@ __device__ __forceinline__ void finish_row(const Attn &a, int q0, i64 row, u32 h
   if (col == 0 && a.lse) a.lse[(i64)(q0 + tok) * a.hq + head] = sum == 0.0f ? -INFINITY : top * kLn2 + logf(sum);
 }
 
-// Joins the parts of a unit that blocks i0..i1 left, in the order of the key axis.  Block-collective.
-template <typename T, int D, int ROWS, int NT>
+// Joins the parts of a unit that blocks i0..i1 left, in the order of the key axis.  Block-collective.  What it costs
+// is waiting for loads, so a thread keeps ITEMS * AHEAD of them in flight (ITEMS pieces of four columns, AHEAD
+// parts): with one at a time, the join of 256 rows took longer than the attention of a short unit.
+template <typename T, int D, int ROWS, int NT, int ITEMS, int AHEAD>
 __device__ __forceinline__ void join_parts(const Attn &a, const Cursor &c, i64 row0, int rows, u32 i0, u32 i1) {
-  for (int x = (int)threadIdx.x; x < rows * (D / 4); x += NT) {
-    const int row = x / (D / 4), col = (x - row * (D / 4)) * 4;
-    float top = -INFINITY, sum = 0.0f;
-    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (u32 i = i0; i <= i1; ++i) {
-      const i64 at = (i64)(2 * i + (i == i0 ? 1 : 0)) * ROWS + row;
-      const float2 ml = __ldcg((const float2 *)(a.part_ml + at * 2));
-      const float4 v = __ldcg((const float4 *)(a.part_o + at * D + col));
-      const float now = fmaxf(top, ml.x), base = now == -INFINITY ? 0.0f : now;
-      const float f0 = exp2_approx(top - base), f1 = exp2_approx(ml.x - base);
-      top = now;
-      sum = sum * f0 + ml.y * f1;
-      acc.x = acc.x * f0 + v.x * f1;
-      acc.y = acc.y * f0 + v.y * f1;
-      acc.z = acc.z * f0 + v.z * f1;
-      acc.w = acc.w * f0 + v.w * f1;
+  const int items = rows * (D / 4);
+  for (int x0 = (int)threadIdx.x; x0 < items; x0 += NT * ITEMS) {
+    float top[ITEMS], sum[ITEMS];
+    float4 acc[ITEMS];
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) { top[k] = -INFINITY; sum[k] = 0.0f; acc[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
+    for (u32 i = i0; i <= i1; i += AHEAD) {
+      float2 ml[ITEMS][AHEAD];
+      float4 v[ITEMS][AHEAD];
+#pragma unroll
+      for (int k = 0; k < ITEMS; ++k)
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+          ml[k][j] = make_float2(-INFINITY, 0.0f);
+          v[k][j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          const int x = x0 + k * NT, row = x / (D / 4);
+          if (x < items && i + j <= i1) {
+            const i64 at = (i64)(2 * (i + j) + (i + j == i0 ? 1 : 0)) * ROWS + row;
+            ml[k][j] = __ldcg((const float2 *)(a.part_ml + at * 2));
+            v[k][j] = __ldcg((const float4 *)(a.part_o + at * D + (x - row * (D / 4)) * 4));
+          }
+        }
+#pragma unroll
+      for (int k = 0; k < ITEMS; ++k) {
+        float now = top[k];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) now = fmaxf(now, ml[k][j].x);
+        const float base = now == -INFINITY ? 0.0f : now, f = exp2_approx(top[k] - base);
+        top[k] = now;
+        sum[k] *= f;
+        acc[k].x *= f; acc[k].y *= f; acc[k].z *= f; acc[k].w *= f;
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+          const float g = exp2_approx(ml[k][j].x - base);
+          sum[k] += g * ml[k][j].y;
+          acc[k].x += g * v[k][j].x; acc[k].y += g * v[k][j].y; acc[k].z += g * v[k][j].z; acc[k].w += g * v[k][j].w;
+        }
+      }
     }
-    finish_row<T>(a, c.req.q0, row0 + row, c.h, col, acc, top, sum);
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+      const int x = x0 + k * NT, row = x / (D / 4);
+      if (x < items) finish_row<T>(a, c.req.q0, row0 + row, c.h, (x - row * (D / 4)) * 4, acc[k], top[k], sum[k]);
+    }
   }
 }
 

@@ -38,6 +38,15 @@ __device__ __forceinline__ bool bar_wait(u64 *bar, u32 parity, volatile u32 *fai
   return true;
 }
 
+// The same for a whole warp, with one answer that the compiler knows to be one.
+__device__ __forceinline__ bool warp_wait(u64 *bar, u32 parity, volatile u32 *failed) { return __all_sync(0xffffffffu, bar_wait(bar, parity, failed)); }
+__device__ __forceinline__ u32 uniform(u32 v) { return __shfl_sync(0xffffffffu, v, 0); }
+__device__ __forceinline__ bool one_lane() {
+  u32 yes;
+  asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(yes));
+  return yes != 0;
+}
+
 // One box of a (head size, token, head, page) tensor into shared memory.
 __device__ __forceinline__ void copy_box(void *to, const CUtensorMap *map, int x, int token, int head, int page, u64 *bar) {
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(smem_addr(to)),
@@ -63,9 +72,9 @@ __device__ __forceinline__ void mma_commit(u64 *bar) {
 // Shared-memory operand of 128-byte rows with the 128-byte swizzle.  Rows along K (keys' or queries' head
 // elements): groups of 8 rows follow each other, 1024 bytes.  Columns along K (values, whose rows are keys): 64 of
 // the head's elements a row, the next 64 `lead` bytes on, the next 8 keys 1024 bytes on.
-__device__ __forceinline__ u64 operand(const void *p, u32 lead) {
-  return (u64)((smem_addr(p) & 0x3FFFF) >> 4) | ((u64)(lead >> 4) << 16) | ((u64)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
-}
+// The low word holds the address and `lead`, both in units of 16 bytes, the high word is the same for all.
+__device__ __forceinline__ u32 operand(const void *p, u32 lead) { return ((smem_addr(p) & 0x3FFFF) >> 4) | ((lead >> 4) << 16); }
+constexpr u32 kOperandHigh = (1024 >> 4) | (1u << 14) | (2u << 29);
 
 template <typename T>
 struct TypeCode { static constexpr u32 value = 1; };       // bfloat16
@@ -78,12 +87,14 @@ __host__ __device__ constexpr u32 mma_shape(u32 n, bool b_columns) {
   return (1u << 4) | (TypeCode<T>::value << 7) | (TypeCode<T>::value << 10) | ((b_columns ? 1u : 0u) << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24);
 }
 
-__device__ __forceinline__ void mma_ss(u32 d, u64 a, u64 b, u32 shape, bool add) {
-  asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d), "l"(a), "l"(b), "r"(shape), "r"((u32)add)
+__device__ __forceinline__ void mma_ss(u32 d, u32 a, u32 b, u32 shape, bool add) {
+  asm volatile("{ .reg .pred p; .reg .b64 x, y; setp.ne.u32 p, %4, 0; mov.b64 x, {%1, %5}; mov.b64 y, {%2, %5}; "
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p; }" ::"r"(d), "r"(a), "r"(b), "r"(shape), "r"((u32)add), "n"(kOperandHigh)
                : "memory");
 }
-__device__ __forceinline__ void mma_ts(u32 d, u32 a, u64 b, u32 shape, bool add) {
-  asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d), "r"(a), "l"(b), "r"(shape), "r"((u32)add)
+__device__ __forceinline__ void mma_ts(u32 d, u32 a, u32 b, u32 shape, bool add) {
+  asm volatile("{ .reg .pred p; .reg .b64 y; setp.ne.u32 p, %4, 0; mov.b64 y, {%2, %5}; "
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p; }" ::"r"(d), "r"(a), "r"(b), "r"(shape), "r"((u32)add), "n"(kOperandHigh)
                : "memory");
 }
 
@@ -113,6 +124,56 @@ __device__ __forceinline__ void tmem_st32(u32 at, const u32 *v) {
       : "memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ u32 load_acquire(const u32 *p) {
+  u32 v;
+  asm volatile("ld.acquire.gpu.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+
+// two 32-bit numbers to an instruction
+typedef u64 f32x2;
+__device__ __forceinline__ f32x2 pack_f32(float lo, float hi) {
+  f32x2 v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
+  return v;
+}
+__device__ __forceinline__ void unpack_f32(f32x2 v, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma_f32x2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 v;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
+  return v;
+}
+__device__ __forceinline__ f32x2 add_f32x2(f32x2 a, f32x2 b) {
+  f32x2 v;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+  return v;
+}
+
+
+// 2^x of two numbers in the multiply-add units.  x = n + f, n whole (found by adding 1.5 * 2^23, which leaves n in the
+// low bits), f in [-1/2, 1/2]; 2^f by the polynomial of degree 5 with the least largest relative error there (Remez's
+// exchange; 2e-7 with its coefficients in 32 bits), 2^n by the exponent's bits.  Below 2^-127 the result is 0.
+__device__ __forceinline__ void exp2_poly2(f32x2 x, float &y0, float &y1) {
+  float x0, x1;
+  unpack_f32(x, x0, x1);
+  asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(x0));     // -127; what is not a number stays so
+  asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(x1));
+  x = pack_f32(x0, x1);
+  const f32x2 t = add_f32x2(x, pack_f32(12582912.0f, 12582912.0f));
+  const f32x2 n = add_f32x2(t, pack_f32(-12582912.0f, -12582912.0f));
+  const f32x2 f = fma_f32x2(n, pack_f32(-1.0f, -1.0f), x);
+  f32x2 p = fma_f32x2(pack_f32(0.0013276472454890609f, 0.0013276472454890609f), f, pack_f32(0.009675540961325169f, 0.009675540961325169f));
+  p = fma_f32x2(p, f, pack_f32(0.05550713092088699f, 0.05550713092088699f));
+  p = fma_f32x2(p, f, pack_f32(0.24022120237350464f, 0.24022120237350464f));
+  p = fma_f32x2(p, f, pack_f32(0.6931469440460205f, 0.6931469440460205f));
+  p = fma_f32x2(p, f, pack_f32(1.0000001192092896f, 1.0000001192092896f));
+  float t0, t1;
+  unpack_f32(t, t0, t1);
+  unpack_f32(p, y0, y1);
+  y0 *= __uint_as_float((__float_as_uint(t0) << 23) + 0x3F800000u);
+  y1 *= __uint_as_float((__float_as_uint(t1) << 23) + 0x3F800000u);
+}
 
 template <int N>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }

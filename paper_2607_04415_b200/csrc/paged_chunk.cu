@@ -11,6 +11,7 @@
 //   9         copies key and value tiles, page by page (tensor copies, zeros for pages outside the cache), into a
 //             ring of stages with the 128-byte swizzle.
 //   10        looks for values that are not finite in tiles that some rows see and others do not.
+//   11        walks the block's share of the work and tells the others its parts, one ahead; gathers the queries.
 // Tensor memory, 512 columns: scores of tile 0 and 1 (128 each), outputs of tile 0 and 1 (head size each).
 //
 // Running maximum: a row's reference only moves when its maximum passes it by more than 2^8, since moving it
@@ -19,7 +20,7 @@
 //
 // Blocks take equal shares of all key tiles of the call (make_plan), cut units are joined by their last block.
 // Values that are not finite (and masked for some rows) would reach rows that do not see them, as 0 * inf in the
-// product: a unit that meets one is computed again row by row from the cache, slowly, in plain_columns.
+// product: a unit that meets one is computed again row by row from the cache, slowly, in plain_row.
 #include "paged/common.cuh"
 #include "paged/tensor.cuh"
 
@@ -32,9 +33,11 @@ constexpr int kRows = 256;
 constexpr int kTileRows = 128;
 constexpr int kTileKeys = 128;
 constexpr int kThreads = 384;
-constexpr int kSoftmaxRegs = 224, kOtherRegs = 56;   // a thread, of 168 * 3 = 224 * 2 + 56 at launch
-constexpr u32 kScores = 0, kOutputs = 256;       // columns of tensor memory
-constexpr int kScans = 8;                         // more parts than the ring of stages lets warp 10 run ahead
+constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;   // a thread, of 168 * 3 = 208 * 2 + 88 at launch
+constexpr u32 kScores = 0, kOutputs = 256;           // columns of tensor memory
+constexpr int kParts = 4;                            // parts that have been told and not yet finished
+constexpr int kScans = 8;                            // more parts than the ring of stages lets warp 10 run ahead
+constexpr int kPolyPairs = 4;                        // of 16 pairs of weights, those whose exponential is a polynomial
 
 template <int D>
 struct Shape {
@@ -43,32 +46,27 @@ struct Shape {
   static constexpr int stages = chunks == 1 ? 8 : 5;
 };
 
+// A part of a unit: `tiles` key tiles from `tile` on; 0 tiles: the end.
+struct __align__(16) PartInfo {
+  int r, h, len, n;
+  int q0, row0, rows, tile;
+  int tiles, lo, hi, whole;
+  u32 i0, i1;          // of a cut unit: the blocks that hold parts of it
+  u32 pad[2];
+};
+
 template <int D>
 struct ChunkShared {
   unsigned char q[2][Shape<D>::tile_bytes];
   unsigned char kv[Shape<D>::stages][Shape<D>::tile_bytes];
+  PartInfo part[kParts];
   u64 kv_full[Shape<D>::stages], kv_empty[Shape<D>::stages];
-  u64 q_full[2], s_full[2], p_full[2], o_full[2], scanned[kScans];
+  u64 part_full[kParts], part_empty[kParts];
+  u64 q_full[2], q_empty[2], s_full[2], p_full[2][2], o_full[2], scanned[kScans], meet;
   u32 odd[kScans];
   u32 tmem, failed, last;
   PlanShared plan;
 };
-
-// One part of a unit: its tiles [from, to) of this block's share.
-struct Part {
-  int from, to;
-  i64 row0;
-  int rows;
-};
-
-__device__ __forceinline__ Part part_of(const Attn &a, const Cursor &c, u64 left) {
-  Part p;
-  p.from = c.at;
-  p.to = (int)min((u64)c.span.tiles, (u64)c.at + left);
-  p.row0 = (i64)c.m * kRows;
-  p.rows = (int)min((i64)kRows, (i64)c.req.n * a.group - p.row0);
-  return p;
-}
 
 // What one row sees.
 struct Row {
@@ -77,35 +75,25 @@ struct Row {
   i64 tok;           // row of q and out
 };
 
-__device__ __forceinline__ Row row_of(const Attn &a, const Cursor &c, i64 row) {
+__device__ __forceinline__ Row row_of(const Attn &a, const PartInfo &p, u32 flat) {
   Row r;
-  const int tok = (int)((u32)row / a.group);
-  r.head = (int)((u32)row - (u32)tok * a.group + c.h * a.group);
-  r.tok = c.req.q0 + tok;
-  r.pos = c.req.len - c.req.n + tok;
-  r.hi = a.causal ? min(c.req.len, r.pos + 1) : c.req.len;
+  const u32 tok = flat / a.group;
+  r.head = (int)(flat - tok * a.group) + p.h * (int)a.group;
+  r.tok = p.q0 + (int)tok;
+  r.pos = p.len - p.n + (int)tok;
+  r.hi = a.causal ? min(p.len, r.pos + 1) : p.len;
   r.lo = a.window ? (int)max((i64)0, (i64)r.pos - a.window + 1) : 0;
   return r;
 }
 
-// Whether every row of the unit sees every key of [lo, hi) that lies in the tile.
-__device__ __forceinline__ bool seen_by_all(const Attn &a, const Cursor &c, const Part &p, int key0) {
-  const int t0 = (int)((u32)p.row0 / a.group), t1 = (int)((u32)(p.row0 + p.rows - 1) / a.group);
-  const int first = c.req.len - c.req.n + t0, last = c.req.len - c.req.n + t1;
-  if (a.causal && min(key0 + kTileKeys, c.span.hi) > first + 1) return false;
-  if (a.window && (i64)max(key0, c.span.lo) < (i64)last - a.window + 1) return false;
-  return true;
-}
-
-// Score of one row and key in units of log2, and 32 columns of the weighted sum, straight from the cache: for units with
-// values that are not finite.  Keys [k0, k1) of the row's own [lo, hi); `top` is the reference of the weights, taken
-// from the row's maximum where `fresh`.
+// One row straight from the cache, for units with values that are not finite: over the keys [k0, k1) that the row sees, with
+// col < 0 the maximum score (in units of log2) and the sum of the weights, else 32 columns of the weighted sum.
 template <typename T, int D>
-__device__ __noinline__ void plain_columns(const Attn &a, u32 req, u32 h, const Row &r, int k0, int k1, int col, float *acc, float &top, float &sum) {
+__device__ __noinline__ void plain_row(const Attn &a, u32 req, u32 h, const Row &r, int k0, int k1, int col, float *acc, float &top, float &sum) {
   const u16 *q = (const u16 *)a.q + r.tok * a.q_t + (i64)r.head * a.q_h;
   const float slope = a.slopes ? a.slopes[r.head] * kLog2e : 0.0f;
-  for (int pass = col == 0 ? 0 : 1; pass < 2; ++pass) {
-    if (pass == 0) top = -INFINITY; else sum = col == 0 ? 0.0f : sum;
+  if (col < 0) { top = -INFINITY; sum = 0.0f; }
+  for (int pass = col < 0 ? 0 : 1; pass < 2; ++pass) {
     for (int key = max(k0, r.lo); key < min(k1, r.hi); ++key) {
       const u32 at = (u32)key / a.page;
       const int pg = a.tables[(i64)req * a.tab_r + at];
@@ -118,12 +106,11 @@ __device__ __noinline__ void plain_columns(const Attn &a, u32 req, u32 h, const 
         x += u.x * v.x;
         x += u.y * v.y;
       }
-      x *= a.scale;
-      if (a.softcap > 0.0f) x = capped(x, a.softcap);
-      x = x * kLog2e + slope * (float)(key - r.pos);
+      x = a.softcap > 0.0f ? capped_log2(x, a.scale * (2.0f * kLog2e / a.softcap), a.softcap * kLog2e) : x * a.scale * kLog2e;
+      x += slope * (float)(key - r.pos);
       if (pass == 0) { top = fmaxf(top, x); continue; }
       const float w = exp2_approx(x - (top == -INFINITY ? 0.0f : top));
-      if (col == 0) sum += w;
+      if (col < 0) { sum += w; continue; }
       if (!there) continue;
       const u16 *v = (const u16 *)a.vp + (i64)pg * a.v_p + (i64)h * a.v_h + in * a.v_t + col;
 #pragma unroll
@@ -136,8 +123,29 @@ __device__ __noinline__ void plain_columns(const Attn &a, u32 req, u32 h, const 
   }
 }
 
+// Columns [0, 64) or [64, 128) of a row's scores to weights: 2^(x * mul - base), summed unrounded into `sum`, rounded to the
+// cache's type in w.  kPolyPairs of 16 exponentials are computed in the multiply-add units instead of the special function
+// units, which are what the softmax waits for.
+template <typename T>
+__device__ __forceinline__ void weights64(const float *s, f32x2 mul, f32x2 minus_base, f32x2 (&sum)[2], u32 *w) {
+#pragma unroll
+  for (int k = 0; k < 32; ++k) {
+    const f32x2 x = fma_f32x2(pack_f32(s[2 * k], s[2 * k + 1]), mul, minus_base);
+    float x0, x1;
+    if (((k & 15) * kPolyPairs) / 16 != (((k & 15) + 1) * kPolyPairs) / 16) {
+      exp2_poly2(x, x0, x1);
+    } else {
+      unpack_f32(x, x0, x1);
+      x0 = exp2_approx(x0);
+      x1 = exp2_approx(x1);
+    }
+    sum[k & 1] = add_f32x2(sum[k & 1], pack_f32(x0, x1));
+    w[k] = pack2<T>(x0, x1);
+  }
+}
+
 template <typename T, int D, bool SCORED>
-__global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const Attn a, const __grid_constant__ CUtensorMap keys,
+__global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __grid_constant__ Attn a, const __grid_constant__ CUtensorMap keys,
                                                                       const __grid_constant__ CUtensorMap values, const u32 box_rows) {
   extern __shared__ unsigned char raw[];
   ChunkShared<D> &sh = *(ChunkShared<D> *)(raw + ((1024 - (smem_addr(raw) & 1023)) & 1023));
@@ -145,8 +153,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const Attn
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (tid == 0) {
     for (int i = 0; i < S::stages; ++i) { bar_init(&sh.kv_full[i], 1); bar_init(&sh.kv_empty[i], 2); }
-    for (int t = 0; t < 2; ++t) { bar_init(&sh.q_full[t], kTileRows); bar_init(&sh.s_full[t], 1); bar_init(&sh.p_full[t], kTileRows); bar_init(&sh.o_full[t], 1); }
+    for (int i = 0; i < kParts; ++i) { bar_init(&sh.part_full[i], 1); bar_init(&sh.part_empty[i], 11); }
+    for (int t = 0; t < 2; ++t) {
+      bar_init(&sh.q_full[t], 1); bar_init(&sh.q_empty[t], 1); bar_init(&sh.s_full[t], 1); bar_init(&sh.o_full[t], 1);
+      bar_init(&sh.p_full[t][0], 4); bar_init(&sh.p_full[t][1], 4);
+    }
     for (int i = 0; i < kScans; ++i) { bar_init(&sh.scanned[i], 1); sh.odd[i] = 0; }
+    bar_init(&sh.meet, 8);
     sh.failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async();
@@ -158,45 +171,42 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const Attn
   mma_fence_after();
   const u32 tmem = sh.tmem;
   volatile u32 *failed = &sh.failed;
-  Cursor c = plan.first;
-  u64 left = plan.end - plan.begin;
+  // the part that is told `no`-th; false at the end
+  auto take_part = [&](u32 no, PartInfo &p) {
+    if (!bar_wait(&sh.part_full[no % kParts], (no / kParts) & 1, failed)) return false;
+    p = sh.part[no % kParts];
+    return p.tiles != 0;
+  };
+  auto part_done = [&](u32 no) {
+    __syncwarp();
+    if (lane == 0) bar_arrive(&sh.part_empty[no % kParts]);
+  };
 
   if (warp < 8) {
     // ------------------------------------------------------------------ softmax of row tile t
     more_registers<kSoftmaxRegs>();
     const int t = warp >> 2, row = tid & (kTileRows - 1);
+    constexpr int kCols = D % 64 == 0 ? 64 : 32;             // columns of the output that are worked on at a time
     const u32 lanes = (u32)(warp & 3) << 21;                 // this warp's 32 lanes of tensor memory
     const u32 scores = tmem + kScores + t * 128 + lanes, outputs = tmem + kOutputs + t * D + lanes;
-    u32 s_phase = 0, o_phase = 0, part_no = 0;
-    auto put_q = [&](const Cursor &at, const Part &p) {      // the tile's queries, swizzled; zeros past the last row
-      constexpr int P = D / 8;
-#pragma unroll 4
-      for (int x = row; x < kTileRows * P; x += kTileRows) {
-        const int r = x / P, piece = x - r * P;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (t * kTileRows + r < p.rows) {
-          const u32 flat = (u32)(p.row0 + t * kTileRows + r), tok = flat / a.group, head = flat - tok * a.group + at.h * a.group;
-          v = *(const uint4 *)((const u16 *)a.q + (i64)(at.req.q0 + (int)tok) * a.q_t + (i64)head * a.q_h + piece * 8);
-        }
-        *(uint4 *)(sh.q[t] + (piece >> 3) * (kTileRows * 128) + r * 128 + (((piece & 7) ^ (r & 7)) << 4)) = v;
-      }
-      fence_async();
-      bar_arrive(&sh.q_full[t]);
+    u32 s_phase = 0, o_phase = 0, meet_phase = 0;
+    auto meet = [&]() {                                      // all eight warps, with the limit of every other wait
+      __syncwarp();
+      if (lane == 0) bar_arrive(&sh.meet);
+      const bool ok = bar_wait(&sh.meet, meet_phase, failed);
+      meet_phase ^= 1;
+      return ok;
     };
-    const float to_log2 = a.scale * kLog2e;
-    Part p{};
-    if (left) {
-      p = part_of(a, c, left);
-      if (t == 0 || p.rows > kTileRows) put_q(c, p);
-    }
-    while (left) {
+    PartInfo p;
+    for (u32 no = 0; take_part(no, p); ++no) {
       const bool mine = t == 0 || p.rows > kTileRows;        // does the unit have this row tile at all
       const bool valid = t * kTileRows + row < p.rows;
-      const Row r = row_of(a, c, valid ? p.row0 + t * kTileRows + row : p.row0);
-      const float slope = SCORED && a.slopes ? a.slopes[r.head] * kLog2e : 0.0f;
+      const Row r = row_of(a, p, (u32)p.row0 + (valid ? t * kTileRows + row : 0));
       float m = -INFINITY, l = 0.0f;
       if (mine) {
-        for (int at = p.from; at < p.to; ++at) {
+        const float slope = SCORED && a.slopes ? a.slopes[r.head] * kLog2e : 0.0f;
+        const float mul = SCORED ? 1.0f : a.scale * kLog2e;
+        for (int at = 0; at < p.tiles; ++at) {
           if (!bar_wait(&sh.s_full[t], s_phase, failed)) break;
           s_phase ^= 1;
           mma_fence_after();
@@ -206,25 +216,33 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const Attn
           tmem_wait_ld();
 #pragma unroll
           for (int i = 0; i < 4; ++i) keep(s + 32 * i);
-          const int key0 = (c.span.first + at) * kTileKeys;
-          float mul = to_log2;
+          const int key0 = (p.tile + at) * kTileKeys;
           if (SCORED) {
-            mul = 1.0f;
+            if (a.softcap > 0.0f) {
+              const float in = a.scale * (2.0f * kLog2e / a.softcap), out = a.softcap * kLog2e;
 #pragma unroll
-            for (int i = 0; i < 128; ++i) {
-              float x = s[i] * a.scale;
-              if (a.softcap > 0.0f) x = capped(x, a.softcap);
-              s[i] = x * kLog2e + slope * (float)(key0 + i - r.pos);
+              for (int i = 0; i < 128; ++i) s[i] = capped_log2(s[i], in, out);
+            } else {
+              const float in = a.scale * kLog2e;
+#pragma unroll
+              for (int i = 0; i < 128; ++i) s[i] *= in;
             }
+            const float far = (float)(key0 - r.pos);
+#pragma unroll
+            for (int i = 0; i < 128; ++i) s[i] = fmaf(slope, far + (float)i, s[i]);
           }
           if (__any_sync(0xffffffffu, key0 < r.lo || key0 + kTileKeys > r.hi)) {
+            const int lo = r.lo - key0, hi = r.hi - key0;
 #pragma unroll
             for (int i = 0; i < 128; ++i)
-              if (key0 + i < r.lo || key0 + i >= r.hi) s[i] = -INFINITY;
+              if (i < lo || i >= hi) s[i] = -INFINITY;
           }
-          float top = s[0];
+          float tops[4] = {s[0], s[1], s[2], s[3]};          // four chains of three-way maxima
 #pragma unroll
-          for (int i = 1; i < 128; ++i) top = fmaxf(top, s[i]);
+          for (int i = 4; i < 124; i += 8)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) tops[k] = fmaxf(fmaxf(tops[k], s[i + k]), s[i + 4 + k]);
+          float top = fmaxf(fmaxf(fmaxf(tops[0], s[124]), fmaxf(tops[1], s[125])), fmaxf(fmaxf(tops[2], s[126]), fmaxf(tops[3], s[127])));
           top *= mul;
           const bool moves = top > m + 8.0f || (m == -INFINITY && top > -INFINITY);
           if (__any_sync(0xffffffffu, moves)) {
@@ -232,7 +250,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const Attn
             const float f = m == -INFINITY ? 0.0f : exp2_approx(m - to);
             m = to;
             l *= f;
-            if (at > p.from) {                               // the scores' arrival says that the product before is done
+            if (at > 0) {                                    // the scores' arrival says that the product before is done
 #pragma unroll
               for (int i = 0; i < D / 32; ++i) {
                 float o[32];
@@ -246,179 +264,241 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const Attn
               }
             }
           }
-          const float base = m == -INFINITY ? 0.0f : m;
-          float l0 = 0.0f, l1 = 0.0f, l2 = 0.0f, l3 = 0.0f;
+          const float minus_base = m == -INFINITY ? 0.0f : -m;
+          const f32x2 mul2 = pack_f32(mul, mul), base2 = pack_f32(minus_base, minus_base);
+          f32x2 sum[2] = {pack_f32(l, 0.0f), pack_f32(0.0f, 0.0f)};
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
+          for (int i = 0; i < 2; ++i) {                      // the product starts on the first half of the weights
             u32 w[32];
-#pragma unroll
-            for (int k = 0; k < 32; k += 2) {
-              const float w0 = exp2_approx(fmaf(s[64 * i + 2 * k], mul, -base)), w1 = exp2_approx(fmaf(s[64 * i + 2 * k + 1], mul, -base));
-              const float w2 = exp2_approx(fmaf(s[64 * i + 2 * k + 2], mul, -base)), w3 = exp2_approx(fmaf(s[64 * i + 2 * k + 3], mul, -base));
-              l0 += w0; l1 += w1; l2 += w2; l3 += w3;
-              w[k] = pack2<T>(w0, w1);
-              w[k + 1] = pack2<T>(w2, w3);
-            }
+            weights64<T>(s + 64 * i, mul2, base2, sum, w);
             tmem_st32(scores + 32 * i, w);
+            tmem_wait_st();
+            mma_fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(&sh.p_full[t][i]);
           }
-          l += (l0 + l1) + (l2 + l3);
-          tmem_wait_st();
-          mma_fence_before();
-          bar_arrive(&sh.p_full[t]);
+          float l0, l1;
+          unpack_f32(add_f32x2(sum[0], sum[1]), l0, l1);
+          l = l0 + l1;
         }
       }
-      left -= (u64)(p.to - p.from);
-      // the next unit's queries go in before this unit's output is read: its first product runs meanwhile
-      Cursor next = c;
-      Part np{};
-      if (left) {
-        next_unit<kRows, kTileKeys>(a, next);
-        np = part_of(a, next, left);
-        if ((t == 0 || np.rows > kTileRows) && !*failed) put_q(next, np);
-      }
-      const bool whole = p.from == 0 && p.to == c.span.tiles;
-      const u64 unit0 = plan.end - left - (u64)p.to;
-      const u32 i0 = whole ? 0 : part_owner(plan.total, unit0, plan.parts);
-      bool fine = true;
+      bool fine = true, odd = false;
+      const int k0 = p.tile * kTileKeys, k1 = (p.tile + p.tiles) * kTileKeys;
       if (mine) {
-        fine = bar_wait(&sh.scanned[part_no % kScans], (part_no / kScans) & 1, failed) && bar_wait(&sh.o_full[t], o_phase, failed);
+        fine = bar_wait(&sh.scanned[no % kScans], (no / kScans) & 1, failed) && bar_wait(&sh.o_full[t], o_phase, failed);
         o_phase ^= 1;
         mma_fence_after();
-        if (fine) {
-          const bool odd = sh.odd[part_no % kScans] != 0;
-          const int k0 = (c.span.first + p.from) * kTileKeys, k1 = (c.span.first + p.to) * kTileKeys;
-          const i64 slot_row = (i64)(2 * blockIdx.x + (blockIdx.x == i0 ? 1 : 0)) * kRows + t * kTileRows + row;
+        odd = fine && sh.odd[no % kScans] != 0;
+        if (odd) {
+          float top, sum;
+          plain_row<T, D>(a, p.r, p.h, r, k0, k1, -1, nullptr, top, sum);
+          m = top;
+          l = sum;
+        }
+      }
+      auto output = [&](float *o, int col) {                 // kCols columns of the row's output, not yet divided by l
+#pragma unroll
+        for (int i = 0; i < kCols / 32; ++i) {
+          if (!odd) {
+            tmem_ld32(o + 32 * i, outputs + col + 32 * i);
+          } else {
+            float x[32], top = m, sum = l;                   // not o itself, which stays in registers
+#pragma unroll
+            for (int k = 0; k < 32; ++k) x[k] = 0.0f;
+            plain_row<T, D>(a, p.r, p.h, r, k0, k1, col + 32 * i, x, top, sum);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) o[32 * i + k] = x[k];
+          }
+        }
+        tmem_wait_ld();
+#pragma unroll
+        for (int i = 0; i < kCols / 32; ++i) keep(o + 32 * i);
+      };
+      auto write = [&](const float *o, int col, float f) {
+        uint4 *to = (uint4 *)((u16 *)a.out + r.tok * a.o_t + (i64)r.head * a.o_h + col);
+#pragma unroll
+        for (int k = 0; k < kCols / 8; ++k)
+          to[k] = make_uint4(pack2<T>(o[8 * k] * f, o[8 * k + 1] * f), pack2<T>(o[8 * k + 2] * f, o[8 * k + 3] * f), pack2<T>(o[8 * k + 4] * f, o[8 * k + 5] * f),
+                             pack2<T>(o[8 * k + 6] * f, o[8 * k + 7] * f));
+      };
+      const int unit_row = t * kTileRows + row;
+      if (p.whole) {
+        if (mine && fine) {
+          const float f = l == 0.0f ? 0.0f : 1.0f / l;
+          if (valid && a.lse) a.lse[r.tok * a.hq + r.head] = l == 0.0f ? -INFINITY : m * kLn2 + logf(l);
 #pragma unroll 1
-          for (int i = 0; i < D / 32; ++i) {
-            float o[32];
-            if (!odd) {
-              tmem_ld32(o, outputs + 32 * i);
-              tmem_wait_ld();
-              keep(o);
-            } else {
-              float x[32], top = m, sum = l;                 // not o itself, which stays in registers
+          for (int col = 0; col < D; col += kCols) {
+            float o[kCols];
+            output(o, col);
+            if (valid) write(o, col, f);
+          }
+        }
+      } else {
+        // A cut unit.  The last block to get here joins the parts, its own out of tensor memory; the others leave theirs in
+        // the workspace: [part][column / 4][row][4], so that neighbouring threads' rows lie side by side.
+        const u32 own = blockIdx.x, others = p.i1 - p.i0;
+        if (tid == 0) sh.last = load_acquire(a.arrived + p.i0) == others;
+        fine = meet() && fine;
+        bool join = sh.last != 0;
+        if (!join) {
+          const i64 slot = 2 * own + (own == p.i0 ? 1 : 0);
+          if (mine && fine) {
+            *(float2 *)(a.part_ml + (slot * kRows + unit_row) * 2) = make_float2(m, l);
+#pragma unroll 1
+            for (int col = 0; col < D; col += kCols) {
+              float o[kCols];
+              output(o, col);
 #pragma unroll
-              for (int k = 0; k < 32; ++k) x[k] = 0.0f;
-              plain_columns<T, D>(a, c.r, c.h, r, k0, k1, 32 * i, x, top, sum);
-              m = top;
-              l = sum;
-#pragma unroll
-              for (int k = 0; k < 32; ++k) o[k] = x[k];
+              for (int k = 0; k < kCols / 4; ++k)
+                __stcg((float4 *)a.part_o + (slot * (D / 4) + col / 4 + k) * kRows + unit_row, make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]));
             }
-            if (!valid) continue;
-            if (whole) {
-              const float f = l == 0.0f ? 0.0f : 1.0f / l;
-              uint4 *to = (uint4 *)((u16 *)a.out + r.tok * a.o_t + (i64)r.head * a.o_h + 32 * i);
+          }
+          __threadfence();
+          fine = meet() && fine;
+          if (tid == 0) { sh.last = atomicAdd(a.arrived + p.i0, 1u) == others; __threadfence(); }
+          fine = meet() && fine;
+          join = sh.last != 0;
+        }
+        if (join) {
+          if (tid == 0) a.arrived[p.i0] = 0;                 // ready for the next call
+          if (mine && fine) {
+            auto place = [&](u32 i) { return (i64)(2 * i + (i == p.i0 ? 1 : 0)); };
+            float top = -INFINITY, sum = 0.0f;
+#pragma unroll 4
+            for (u32 i = p.i0; i <= p.i1; ++i) {
+              const float x = __ldcg(a.part_ml + (place(i) * kRows + unit_row) * 2);
+              top = fmaxf(top, i == own ? m : x);
+            }
+            const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll 4
+            for (u32 i = p.i0; i <= p.i1; ++i) {
+              const float2 x = __ldcg((const float2 *)(a.part_ml + (place(i) * kRows + unit_row) * 2));
+              sum += i == own ? exp2_approx(m - base) * l : exp2_approx(x.x - base) * x.y;
+            }
+            const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+            if (valid && a.lse) a.lse[r.tok * a.hq + r.head] = sum == 0.0f ? -INFINITY : top * kLn2 + logf(sum);
+#pragma unroll 1
+            for (int col = 0; col < D; col += kCols) {
+              float acc[kCols];
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
-                to[k] = make_uint4(pack2<T>(o[8 * k] * f, o[8 * k + 1] * f), pack2<T>(o[8 * k + 2] * f, o[8 * k + 3] * f), pack2<T>(o[8 * k + 4] * f, o[8 * k + 5] * f),
-                                   pack2<T>(o[8 * k + 6] * f, o[8 * k + 7] * f));
-              if (i == 0 && a.lse) a.lse[r.tok * a.hq + r.head] = l == 0.0f ? -INFINITY : m * kLn2 + logf(l);
-            } else {
-              float4 *to = (float4 *)(a.part_o + slot_row * D + 32 * i);
+              for (int k = 0; k < kCols; ++k) acc[k] = 0.0f;
+#pragma unroll 1
+              for (u32 i = p.i0; i <= p.i1; ++i) {
+                float o[kCols], g;
+                if (i == own) {
+                  g = exp2_approx(m - base);
+                  output(o, col);
+                } else {
+                  const float4 *from = (const float4 *)a.part_o + (place(i) * (D / 4) + col / 4) * kRows + unit_row;
 #pragma unroll
-              for (int k = 0; k < 8; ++k) to[k] = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
-              if (i == 0) *(float2 *)(a.part_ml + slot_row * 2) = make_float2(m, l);
+                  for (int k = 0; k < kCols / 4; ++k) {
+                    const float4 x = __ldcg(from + k * kRows);
+                    o[4 * k] = x.x; o[4 * k + 1] = x.y; o[4 * k + 2] = x.z; o[4 * k + 3] = x.w;
+                  }
+                  g = exp2_approx(__ldcg(a.part_ml + (place(i) * kRows + unit_row) * 2) - base);
+                }
+#pragma unroll
+                for (int k = 0; k < kCols; ++k) acc[k] += g * o[k];
+              }
+              if (valid) write(acc, col, f);
             }
           }
         }
+        meet();                                              // sh.last is free again
       }
-      ++part_no;
       mma_fence_before();
-      if (!whole) {
-        const u32 i1 = part_owner(plan.total, unit0 + (u64)c.span.tiles - 1, plan.parts);
-        __threadfence();
-        some_barrier(1, 256);
-        if (tid == 0) {
-          const u32 before = atomicAdd(a.arrived + i0, 1u);
-          sh.last = before == i1 - i0;
-          if (sh.last) a.arrived[i0] = 0;
-          __threadfence();
-        }
-        some_barrier(1, 256);
-        if (sh.last) join_parts<T, D, kRows, 256>(a, c, p.row0, p.rows, i0, i1);
-        some_barrier(1, 256);
-      }
-      c = next;                                              // after a failed wait the rest is walked through, not computed
-      p = np;
+      part_done(no);
     }
   } else {
     fewer_registers<kOtherRegs>();
     if (warp == 8) {
       // ---------------------------------------------------------------- the products
+      // All that the one issuing lane needs is the same in all lanes and known to be: the operands then stay in uniform
+      // registers, where the instruction wants them (moved there for each instruction, issuing took 80 of its 64 cycles).
       constexpr u32 kScoreShape = mma_shape<T>(kTileKeys, false), kOutShape = mma_shape<T>(D, true);
-      int stage = 0;
-      u32 kv_phase = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
+      constexpr u32 kChunk = (kTileKeys * 128) >> 4, kTile = S::tile_bytes >> 4;
+      const u32 tm = uniform(tmem), q_at = uniform(operand(sh.q[0], 16)), k_at = uniform(operand(sh.kv[0], 16)), v_at = uniform(operand(sh.kv[0], kTileKeys * 128));
+      u32 stage = 0, kv_phase = 0, q_phase = 0, p_phase = 0;          // bit t of the last two
       bool fine = true;
-      auto scores_of = [&](int t, int k_stage) {
-        if (lane == 0) {
+      auto scores_of = [&](u32 t, u32 k_stage, bool last) {
+        if (one_lane()) {
 #pragma unroll
-          for (int k = 0; k < D / 16; ++k) {
-            const int at = (k >> 2) * (kTileKeys * 128) + (k & 3) * 32;
-            mma_ss(tmem + kScores + t * 128, operand(sh.q[t] + at, 16), operand(sh.kv[k_stage] + at, 16), kScoreShape, k > 0);
-          }
+          for (u32 i = 0; i < D / 16; ++i)
+            mma_ss(tm + kScores + t * 128, q_at + t * kTile + (i >> 2) * kChunk + (i & 3) * 2, k_at + k_stage * kTile + (i >> 2) * kChunk + (i & 3) * 2, kScoreShape, i > 0);
           mma_commit(&sh.s_full[t]);
+          if (last) mma_commit(&sh.q_empty[t]);
         }
+        __syncwarp();
       };
-      auto step = [&]() { if (++stage == S::stages) { stage = 0; kv_phase ^= 1; } };
-      while (left && fine) {
-        const Part p = part_of(a, c, left);
-        const int tiles = p.rows > kTileRows ? 2 : 1;
-        for (int t = 0; t < tiles; ++t) {
-          fine = fine && bar_wait(&sh.q_full[t], q_phase[t], failed);
-          q_phase[t] ^= 1;
+      auto outputs_of = [&](u32 t, u32 v_stage, u32 half, bool add) {
+        if (one_lane()) {
+#pragma unroll
+          for (u32 k = 0; k < kTileKeys / 32; ++k)
+            mma_ts(tm + kOutputs + t * D, tm + kScores + t * 128 + (half * 4 + k) * 8, v_at + v_stage * kTile + (half * 4 + k) * (2048 >> 4), kOutShape, add || k > 0);
         }
-        fine = fine && bar_wait(&sh.kv_full[stage], kv_phase, failed);
+        __syncwarp();
+      };
+      auto free_stage = [&](u32 i) {
+        if (one_lane()) mma_commit(&sh.kv_empty[i]);
+        __syncwarp();
+      };
+      auto step = [&]() { if (++stage == (u32)S::stages) { stage = 0; kv_phase ^= 1; } };
+      for (u32 no = 0; fine; ++no) {
+        PartInfo p;
+        if (!__all_sync(0xffffffffu, take_part(no, p))) break;
+        const u32 n_tiles = uniform((u32)p.tiles), row_tiles = uniform(p.rows > kTileRows ? 2u : 1u);
+        for (u32 t = 0; t < row_tiles; ++t) {
+          fine = fine && warp_wait(&sh.q_full[t], (q_phase >> t) & 1, failed);
+          q_phase ^= 1u << t;
+        }
+        fine = fine && warp_wait(&sh.kv_full[stage], kv_phase, failed);
         if (!fine) break;
         mma_fence_after();
-        for (int t = 0; t < tiles; ++t) scores_of(t, stage);
-        if (lane == 0) mma_commit(&sh.kv_empty[stage]);
+        for (u32 t = 0; t < row_tiles; ++t) scores_of(t, stage, n_tiles == 1);
+        free_stage(stage);
         step();
-        for (int at = p.from; at < p.to && fine; ++at) {
-          const int v_stage = stage;
-          const bool more = at + 1 < p.to;
-          fine = bar_wait(&sh.kv_full[v_stage], kv_phase, failed);
-          if (!fine) break;
+        for (u32 at = 0; at < n_tiles && fine; ++at) {
+          const u32 v_stage = stage;
+          const bool more = at + 1 < n_tiles;
+          fine = warp_wait(&sh.kv_full[v_stage], kv_phase, failed);
           step();
-          // rows of the tile that lie outside [lo, hi) in pages that were read: zero, whatever the pages hold there
-          const int key0 = (c.span.first + at) * kTileKeys;
-          if (key0 < c.span.lo || key0 + kTileKeys > c.span.hi) {
-            const int z0 = max(0, min(kTileKeys, c.span.lo - key0)), z1 = max(0, min(kTileKeys, c.span.hi - key0));
-            for (int x = lane; x < S::chunks * kTileKeys * 8; x += 32) {
-              const int k = (x >> 3) & (kTileKeys - 1);
-              if (k < z0 || k >= z1) *(uint4 *)(sh.kv[v_stage] + x * 16) = make_uint4(0, 0, 0, 0);
+          if (more) fine = fine && warp_wait(&sh.kv_full[stage], kv_phase, failed);
+          if (!fine) break;
+          // rows of the tile that lie outside [lo, hi): zero, whatever the pages hold there
+          const int key0 = (p.tile + (int)at) * kTileKeys;
+          if (key0 < p.lo || key0 + kTileKeys > p.hi) {
+            const int z0 = max(0, min(kTileKeys, p.lo - key0)), z1 = max(z0, min(kTileKeys, p.hi - key0)), rows = z0 + kTileKeys - z1;
+            for (int x = lane; x < rows * 8; x += 32) {
+              const int k = (x >> 3) < z0 ? x >> 3 : (x >> 3) - z0 + z1;
+#pragma unroll
+              for (int i = 0; i < S::chunks; ++i) *(uint4 *)(sh.kv[v_stage] + i * (kTileKeys * 128) + k * 128 + (x & 7) * 16) = make_uint4(0, 0, 0, 0);
             }
             fence_async();
             __syncwarp();
           }
-          for (int t = 0; t < tiles && fine; ++t) {
-            fine = bar_wait(&sh.p_full[t], p_phase[t], failed);
-            p_phase[t] ^= 1;
-            if (!fine) break;
-            mma_fence_after();
-            if (lane == 0) {
-#pragma unroll
-              for (int k = 0; k < kTileKeys / 16; ++k)
-                mma_ts(tmem + kOutputs + t * D, tmem + kScores + t * 128 + k * 8, operand(sh.kv[v_stage] + k * 2048, kTileKeys * 128), kOutShape, at > p.from || k > 0);
-              if (!more) mma_commit(&sh.o_full[t]);
+          for (u32 t = 0; t < row_tiles; ++t) {
+            for (u32 half = 0; half < 2; ++half) {
+              fine = fine && warp_wait(&sh.p_full[t][half], (p_phase >> t) & 1, failed);
+              if (!fine) break;
+              mma_fence_after();
+              outputs_of(t, v_stage, half, at > 0 || half > 0);
             }
+            p_phase ^= 1u << t;
+            if (!fine) break;
             if (more) {
-              if (t == 0) {
-                fine = bar_wait(&sh.kv_full[stage], kv_phase, failed);
-                if (!fine) break;
-                mma_fence_after();
-              }
-              scores_of(t, stage);
+              scores_of(t, stage, at + 2 == n_tiles);
+            } else {
+              if (one_lane()) mma_commit(&sh.o_full[t]);
+              __syncwarp();
             }
           }
-          if (lane == 0) mma_commit(&sh.kv_empty[v_stage]);
+          free_stage(v_stage);
           if (more) {
-            if (lane == 0) mma_commit(&sh.kv_empty[stage]);
+            free_stage(stage);
             step();
           }
         }
-        left -= (u64)(p.to - p.from);
-        if (left) next_unit<kRows, kTileKeys>(a, c);
+        part_done(no);
       }
     } else if (warp == 9) {
       // ---------------------------------------------------------------- the copies
@@ -427,14 +507,14 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const Attn
       int stage = 0;
       u32 phase = 1;                                                  // the first round finds the stages free
       bool fine = true;
-      while (left && fine) {
-        const Part p = part_of(a, c, left);
-        for (int at = p.from; at < p.to && fine; ++at) {
-          const int key = (c.span.first + at) * kTileKeys + g * (int)box_rows;
+      PartInfo p;
+      for (u32 no = 0; fine && take_part(no, p); ++no) {
+        for (int at = 0; at < p.tiles && fine; ++at) {
+          const int key = (p.tile + at) * kTileKeys + g * (int)box_rows;
           int page = (int)a.n_pages, in = 0;                          // past the last page: zeros
-          if (lane < boxes && key < c.span.hi && key + (int)box_rows > c.span.lo) {
+          if (lane < boxes && key < p.hi && key + (int)box_rows > p.lo) {
             const u32 pi = (u32)key / a.page;
-            const int pg = __ldg(a.tables + (i64)c.r * a.tab_r + pi);
+            const int pg = __ldg(a.tables + (i64)p.r * a.tab_r + pi);
             if ((u32)pg < a.n_pages) { page = pg; in = (int)((u32)key - pi * a.page); }
           }
 #pragma unroll
@@ -444,39 +524,37 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const Attn
             if (lane == 0) bar_expect(&sh.kv_full[stage], (u32)S::tile_bytes);
             __syncwarp();
             if (lane < boxes)
-              copy_box(sh.kv[stage] + chunk * (kTileKeys * 128) + g * (int)box_rows * 128, kv ? &values : &keys, chunk * 64, in, (int)c.h, page, &sh.kv_full[stage]);
+              copy_box(sh.kv[stage] + chunk * (kTileKeys * 128) + g * (int)box_rows * 128, kv ? &values : &keys, chunk * 64, in, p.h, page, &sh.kv_full[stage]);
             if (++stage == S::stages) { stage = 0; phase ^= 1; }
           }
         }
-        left -= (u64)(p.to - p.from);
-        if (left) next_unit<kRows, kTileKeys>(a, c);
+        part_done(no);
       }
-      if (!fine) {                                                    // leave no copy in flight behind: each stage's last one
+      if (*failed) {                                                  // leave no copy in flight behind: wait for each stage's last one
         const u64 t0 = now_ns();
-        for (int i = 0; i < S::stages; ++i) {
-          const u32 ph = (u32)(i < stage ? phase ^ 1 : phase);        // phase of the stage's last fill, as kv_full counts it
-          while (!bar_try(&sh.kv_full[i], ph ^ 0) && now_ns() - t0 < kWaitLimitNs) {}
-        }
+        for (int i = 0; i < S::stages; ++i)
+          while (!bar_try(&sh.kv_full[i], i < stage ? phase ^ 1 : phase) && now_ns() - t0 < kWaitLimitNs) {}
       }
     } else if (warp == 10) {
       // ---------------------------------------------------------------- values that are not finite
       int stage = 0;
-      u32 phase = 0, part_no = 0;
+      u32 phase = 0;
       bool fine = true;
-      while (left && fine) {
-        const Part p = part_of(a, c, left);
+      PartInfo p;
+      for (u32 no = 0; fine && take_part(no, p); ++no) {
+        // keys that all rows see: [last row's first, first row's last]
+        const Row first = row_of(a, p, (u32)p.row0), last = row_of(a, p, (u32)(p.row0 + p.rows - 1));
         u32 odd = 0;
-        for (int at = p.from; at < p.to && fine; ++at) {
-          const int key0 = (c.span.first + at) * kTileKeys;
-          const bool look = !seen_by_all(a, c, p, key0);
+        for (int at = 0; at < p.tiles && fine; ++at) {
+          const int key0 = (p.tile + at) * kTileKeys, z0 = max(key0, p.lo), z1 = min(key0 + kTileKeys, p.hi);
+          const bool look = z0 < last.lo || z1 > first.hi;
 #pragma unroll
           for (int kv = 0; kv < 2; ++kv) {
             fine = fine && bar_wait(&sh.kv_full[stage], phase, failed);
             if (!fine) break;
             if (kv && look) {
-              const int z0 = max(0, c.span.lo - key0), z1 = min(kTileKeys, c.span.hi - key0);
               for (int x = lane; x < S::chunks * kTileKeys * 8; x += 32) {
-                const int k = (x >> 3) & (kTileKeys - 1);
+                const int k = key0 + ((x >> 3) & (kTileKeys - 1));
                 if (k >= z0 && k < z1 && not_finite8<T>(*(const uint4 *)(sh.kv[stage] + x * 16))) odd = 1;
               }
             }
@@ -487,12 +565,74 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const Attn
         }
         odd = __any_sync(0xffffffffu, odd);
         if (lane == 0) {
-          sh.odd[part_no % kScans] = odd;
-          bar_arrive(&sh.scanned[part_no % kScans]);
+          sh.odd[no % kScans] = odd;
+          bar_arrive(&sh.scanned[no % kScans]);
         }
-        ++part_no;
-        left -= (u64)(p.to - p.from);
-        if (left) next_unit<kRows, kTileKeys>(a, c);
+        part_done(no);
+      }
+    } else {
+      // ---------------------------------------------------------------- the parts and their queries
+      Cursor c = plan.first;
+      u64 left = plan.end - plan.begin;
+      u32 told = 0;
+      auto tell = [&]() {                                             // the part at c, or the end
+        const u32 slot = told % kParts;
+        const bool ok = bar_wait(&sh.part_empty[slot], ((told / kParts) & 1) ^ 1, failed);
+        ++told;
+        if (!ok) return false;
+        PartInfo p{};
+        if (left) {
+          p.r = (int)c.r; p.h = (int)c.h; p.len = c.req.len; p.n = c.req.n; p.q0 = c.req.q0;
+          p.row0 = c.m * kRows;
+          p.rows = (int)min((i64)kRows, (i64)c.req.n * a.group - p.row0);
+          const int to = (int)min((u64)c.span.tiles, (u64)c.at + left);
+          p.tile = c.span.first + c.at;
+          p.tiles = to - c.at;
+          p.lo = c.span.lo; p.hi = c.span.hi;
+          p.whole = c.at == 0 && to == c.span.tiles;
+          if (!p.whole) {
+            const u64 unit0 = plan.end - left - (u64)c.at;
+            p.i0 = part_owner(plan.total, unit0, plan.parts);
+            p.i1 = part_owner(plan.total, unit0 + (u64)c.span.tiles - 1, plan.parts);
+          }
+          left -= (u64)p.tiles;
+        }
+        if (lane == 0) {
+          sh.part[slot] = p;
+          bar_arrive(&sh.part_full[slot]);
+        }
+        __syncwarp();
+        return true;
+      };
+      u32 phase = 3;                                                  // bit t: the first round finds both tiles free
+      bool more = left != 0, fine = tell();
+      for (u32 no = 0; fine && more; ++no) {
+        const PartInfo p = sh.part[no % kParts];                      // stays until all warps are done with it
+        more = left != 0;
+        if (more) next_unit<kRows, kTileKeys>(a, c);
+        fine = tell();
+        const int tiles = p.rows > kTileRows ? 2 : 1;
+        for (int t = 0; t < tiles && fine; ++t) {
+          fine = bar_wait(&sh.q_empty[t], (phase >> t) & 1, failed);
+          phase ^= 1u << t;
+          if (!fine) break;
+          for (int r = lane >> 2; r < kTileRows; r += 8) {            // four lanes a row; zeros past the last row
+            const bool valid = t * kTileRows + r < p.rows;
+            const u32 flat = valid ? (u32)(p.row0 + t * kTileRows + r) : 0u, tok = flat / a.group, head = flat - tok * a.group + p.h * a.group;
+            const u16 *src = (const u16 *)a.q + (i64)(p.q0 + (int)tok) * a.q_t + (i64)head * a.q_h;
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) {
+              const int piece = (lane & 3) + 4 * j;
+              cp_async16(sh.q[t] + (piece >> 3) * (kTileRows * 128) + r * 128 + (((piece & 7) ^ (r & 7)) << 4), src + piece * 8, valid ? 16u : 0u);
+            }
+          }
+          cp_async_commit();
+        }
+        cp_async_wait<0>();
+        fence_async();
+        __syncwarp();
+        if (lane == 0 && fine)
+          for (int t = 0; t < tiles; ++t) bar_arrive(&sh.q_full[t]);
       }
     }
   }

@@ -162,9 +162,8 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) attention_rows_kernel(
         for (int x = 0; x < 4; ++x) {
           const int i = x >> 1, key = key0 + n * 8 + t4 * 2 + (x & 1);
           if (SCORED) {
-            float v = s[n][x] * a.scale;
-            if (a.softcap > 0.0f) v = capped(v, a.softcap);
-            s[n][x] = v * kLog2e + slope[i] * (float)(key - pos[i]);
+            const float v = a.softcap > 0.0f ? capped_log2(s[n][x], a.scale * (2.0f * kLog2e / a.softcap), a.softcap * kLog2e) : s[n][x] * to_log2;
+            s[n][x] = v + slope[i] * (float)(key - pos[i]);
           } else {
             s[n][x] *= to_log2;
           }
@@ -290,7 +289,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) attention_rows_kernel(
         __threadfence();
       }
       __syncthreads();
-      if (sh.last) join_parts<T, D, kRows, kThreads>(a, c, row0, rows, i0, i1);
+      if (sh.last) join_parts<T, D, kRows, kThreads, 1, 8>(a, c, row0, rows, i0, i1);
     }
     __syncthreads();
     issue(stage);
