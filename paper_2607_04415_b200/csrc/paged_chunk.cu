@@ -37,7 +37,7 @@ constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;   // a thread, of 168 * 3 = 2
 constexpr u32 kScores = 0, kOutputs = 256;           // columns of tensor memory
 constexpr int kParts = 4;                            // parts that have been told and not yet finished
 constexpr int kScans = 8;                            // more parts than the ring of stages lets warp 10 run ahead
-constexpr int kPolyPairs = 4;                        // of 16 pairs of weights, those whose exponential is a polynomial
+constexpr int kPolyPairs = 0;                        // of 16 pairs of weights, those whose exponential is a polynomial
 
 template <int D>
 struct Shape {
@@ -420,26 +420,31 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
       const u32 tm = uniform(tmem), q_at = uniform(operand(sh.q[0], 16)), k_at = uniform(operand(sh.kv[0], 16)), v_at = uniform(operand(sh.kv[0], kTileKeys * 128));
       u32 stage = 0, kv_phase = 0, q_phase = 0, p_phase = 0;          // bit t of the last two
       bool fine = true;
-      auto scores_of = [&](u32 t, u32 k_stage, bool last) {
+      // Scores of row tile t with the key tile in k_stage; `last`: the queries are not needed after it.  `frees`: no product needs
+      // the stages v_stage and k_stage after it.  One region of the issuing lane for all, since what stands between two
+      // products has to be shorter than what the matrix unit has queued, some 200 cycles.
+      auto scores_of = [&](u32 t, u32 k_stage, bool last, bool frees, u32 v_stage) {
         if (one_lane()) {
 #pragma unroll
           for (u32 i = 0; i < D / 16; ++i)
             mma_ss(tm + kScores + t * 128, q_at + t * kTile + (i >> 2) * kChunk + (i & 3) * 2, k_at + k_stage * kTile + (i >> 2) * kChunk + (i & 3) * 2, kScoreShape, i > 0);
           mma_commit(&sh.s_full[t]);
+          if (frees) {
+            if (v_stage != k_stage) mma_commit(&sh.kv_empty[v_stage]);
+            mma_commit(&sh.kv_empty[k_stage]);
+          }
           if (last) mma_commit(&sh.q_empty[t]);
         }
         __syncwarp();
       };
-      auto outputs_of = [&](u32 t, u32 v_stage, u32 half, bool add) {
+      auto outputs_of = [&](u32 t, u32 v_stage, u32 half, bool add, bool last, bool frees) {
         if (one_lane()) {
 #pragma unroll
           for (u32 k = 0; k < kTileKeys / 32; ++k)
             mma_ts(tm + kOutputs + t * D, tm + kScores + t * 128 + (half * 4 + k) * 8, v_at + v_stage * kTile + (half * 4 + k) * (2048 >> 4), kOutShape, add || k > 0);
+          if (last) mma_commit(&sh.o_full[t]);
+          if (frees) mma_commit(&sh.kv_empty[v_stage]);
         }
-        __syncwarp();
-      };
-      auto free_stage = [&](u32 i) {
-        if (one_lane()) mma_commit(&sh.kv_empty[i]);
         __syncwarp();
       };
       auto step = [&]() { if (++stage == (u32)S::stages) { stage = 0; kv_phase ^= 1; } };
@@ -454,16 +459,16 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
         fine = fine && warp_wait(&sh.kv_full[stage], kv_phase, failed);
         if (!fine) break;
         mma_fence_after();
-        for (u32 t = 0; t < row_tiles; ++t) scores_of(t, stage, n_tiles == 1);
-        free_stage(stage);
+        for (u32 t = 0; t < row_tiles; ++t) scores_of(t, stage, n_tiles == 1, t + 1 == row_tiles, stage);
         step();
+        fine = warp_wait(&sh.kv_full[stage], kv_phase, failed);
         for (u32 at = 0; at < n_tiles && fine; ++at) {
+          // here stage holds the tile's values, and they have arrived
           const u32 v_stage = stage;
           const bool more = at + 1 < n_tiles;
-          fine = warp_wait(&sh.kv_full[v_stage], kv_phase, failed);
           step();
-          if (more) fine = fine && warp_wait(&sh.kv_full[stage], kv_phase, failed);
-          if (!fine) break;
+          const u32 k_stage = stage;
+          if (more && at == 0) fine = warp_wait(&sh.kv_full[k_stage], kv_phase, failed);
           // rows of the tile that lie outside [lo, hi): zero, whatever the pages hold there
           const int key0 = (p.tile + (int)at) * kTileKeys;
           if (key0 < p.lo || key0 + kTileKeys > p.hi) {
@@ -476,26 +481,28 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
             fence_async();
             __syncwarp();
           }
-          for (u32 t = 0; t < row_tiles; ++t) {
+          if (more) step();                                           // to the next tile's values
+#pragma unroll
+          for (u32 t = 0; t < 2; ++t) {
+            if (t >= row_tiles) break;
+            const bool final_t = t + 1 == row_tiles;
             for (u32 half = 0; half < 2; ++half) {
               fine = fine && warp_wait(&sh.p_full[t][half], (p_phase >> t) & 1, failed);
               if (!fine) break;
               mma_fence_after();
-              outputs_of(t, v_stage, half, at > 0 || half > 0);
+              outputs_of(t, v_stage, half, at > 0 || half > 0, half == 1 && !more, half == 1 && !more && final_t);
             }
             p_phase ^= 1u << t;
             if (!fine) break;
             if (more) {
-              scores_of(t, stage, at + 2 == n_tiles);
-            } else {
-              if (one_lane()) mma_commit(&sh.o_full[t]);
-              __syncwarp();
+              scores_of(t, k_stage, at + 2 == n_tiles, final_t, v_stage);
+              // what the next tile needs, looked at while these products run: its values, then the keys after it
+              if (t == 0) fine = warp_wait(&sh.kv_full[stage], kv_phase, failed);
+              if (fine && final_t && at + 2 < n_tiles) {
+                const u32 after = stage + 1 == (u32)S::stages ? 0 : stage + 1;
+                fine = warp_wait(&sh.kv_full[after], after ? kv_phase : kv_phase ^ 1, failed);
+              }
             }
-          }
-          free_stage(v_stage);
-          if (more) {
-            free_stage(stage);
-            step();
           }
         }
         part_done(no);
