@@ -79,15 +79,16 @@ __device__ __forceinline__ int unit_count(const Attn &a, int n) {
   return (int)(((i64)n * a.group + ROWS - 1) / ROWS);
 }
 
-// The plan.  All tiles of a call, in the order (request, key head, unit, tile), are one line of `total`
-// tiles; block i of N takes tiles [total*i/N, total*(i+1)/N).  Every block finds its own place from the
-// lengths alone, so no host step and no extra launch stands between the lengths and the work.  A unit
-// that is cut by a block boundary is computed in parts, which the last of its blocks to finish joins
-// in the order of the key axis: results do not depend on which block that is.
+// The plan.  All tiles of a call, in the order (request, key head, unit, tile), are one line; a unit's tiles are followed
+// by OVER places without work, for what a unit costs besides its tiles (a block with many short units got as many
+// tiles as one with a single long unit, and took twice as long).  Block i of N takes places [total*i/N,
+// total*(i+1)/N).  Every block finds its own from the lengths alone, so no host step and no extra launch stands
+// between the lengths and the work.  A unit that is cut by a block boundary is computed in parts, which the last of
+// its blocks to finish joins in the order of the key axis: results do not depend on which block that is.
 struct Cursor {
   u32 r, h;
   int m;           // unit of (r, h)
-  int at;          // next tile of the unit, counted from its first
+  int at;          // next place of the unit, counted from its first tile
   Request req;
   Span span;
 };
@@ -100,20 +101,20 @@ struct PlanShared {
 };
 
 __device__ __forceinline__ u64 part_begin(u64 total, u32 i, u32 n) { return total * i / n; }
-// the block that owns tile x: the largest i with total*i/n <= x
+// the block that owns place x: the largest i with total*i/n <= x
 __device__ __forceinline__ u32 part_owner(u64 total, u64 x, u32 n) { return (u32)(((x + 1) * n - 1) / total); }
 
-// Tiles of request r over all its units (of one key head).  Warp-collective; lane's own request is r
+// Places of request r over all its units (of one key head).  Warp-collective; lane's own request is r
 // (in range where `have`); requests of many units are summed by the whole warp.
-template <int ROWS, int TK>
-__device__ __forceinline__ u32 request_tiles(const Attn &a, u32 r, bool have) {
+template <int ROWS, int TK, int OVER>
+__device__ __forceinline__ u32 request_places(const Attn &a, u32 r, bool have) {
   const u32 lane = threadIdx.x & 31;
   Request q{0, 0, 0};
   if (have) q = request_at(a, r);
   const int units = have ? unit_count<ROWS>(a, q.n) : 0;
   u32 sum = 0;
   if (units <= 2) {
-    for (int m = 0; m < units; ++m) sum += (u32)unit_span<ROWS, TK>(a, q.len, q.n, m).tiles;
+    for (int m = 0; m < units; ++m) sum += (u32)unit_span<ROWS, TK>(a, q.len, q.n, m).tiles + OVER;
   }
   u32 big = __ballot_sync(0xffffffffu, units > 2);
   while (big) {
@@ -122,7 +123,7 @@ __device__ __forceinline__ u32 request_tiles(const Attn &a, u32 r, bool have) {
     const int len = __shfl_sync(0xffffffffu, q.len, src), n = __shfl_sync(0xffffffffu, q.n, src);
     const int cnt = __shfl_sync(0xffffffffu, units, src);
     u32 s = 0;
-    for (int m = (int)lane; m < cnt; m += 32) s += (u32)unit_span<ROWS, TK>(a, len, n, m).tiles;
+    for (int m = (int)lane; m < cnt; m += 32) s += (u32)unit_span<ROWS, TK>(a, len, n, m).tiles + OVER;
     s = __reduce_add_sync(0xffffffffu, s);
     if ((int)lane == src) sum = s;
   }
@@ -153,9 +154,9 @@ __device__ __forceinline__ u64 block_scan(u64 v, PlanShared &sh, u64 &all) {
   return x + before;
 }
 
-// Sets the cursor to the tile `offset` tiles after the first tile of request r.  Warp-collective, the same
+// Sets the cursor to the place `offset` places after the first of request r.  Warp-collective, the same
 // for all warps.
-template <int ROWS, int TK>
+template <int ROWS, int TK, int OVER>
 __device__ __forceinline__ Cursor cursor_in(const Attn &a, u32 r, u64 offset) {
   const u32 lane = threadIdx.x & 31;
   Cursor c;
@@ -163,7 +164,7 @@ __device__ __forceinline__ Cursor cursor_in(const Attn &a, u32 r, u64 offset) {
   c.req = request_at(a, r);
   const int units = unit_count<ROWS>(a, c.req.n);
   u32 per_head = 0;
-  for (int m = (int)lane; m < units; m += 32) per_head += (u32)unit_span<ROWS, TK>(a, c.req.len, c.req.n, m).tiles;
+  for (int m = (int)lane; m < units; m += 32) per_head += (u32)unit_span<ROWS, TK>(a, c.req.len, c.req.n, m).tiles + OVER;
   per_head = __reduce_add_sync(0xffffffffu, per_head);
   c.h = (u32)(offset / per_head);
   u32 o = (u32)(offset % per_head);
@@ -171,7 +172,7 @@ __device__ __forceinline__ Cursor cursor_in(const Attn &a, u32 r, u64 offset) {
   c.at = 0;
   for (int base = 0; base < units; base += 32) {
     const int m = base + (int)lane;
-    const u32 t = m < units ? (u32)unit_span<ROWS, TK>(a, c.req.len, c.req.n, m).tiles : 0u;
+    const u32 t = m < units ? (u32)unit_span<ROWS, TK>(a, c.req.len, c.req.n, m).tiles + OVER : 0u;
     u32 x = t;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -212,27 +213,39 @@ __device__ __forceinline__ bool next_unit(const Attn &a, Cursor &c) {
   return true;
 }
 
+// Moves the cursor from a place without work, or past the unit's last tile, to the next tile; `left`: places of the block's
+// share from the cursor on, 0 at its end.
+template <int ROWS, int TK, int OVER>
+__device__ __forceinline__ void settle(const Attn &a, Cursor &c, u64 &left) {
+  while (left && c.at >= c.span.tiles) {
+    const u64 skip = (u64)(c.span.tiles + OVER - c.at);
+    if (skip >= left) { left = 0; return; }
+    left -= skip;
+    if (!next_unit<ROWS, TK>(a, c)) left = 0;
+  }
+}
+
 struct Plan {
-  u64 total, begin, end;   // of the line; [begin, end) is this block's
+  u64 total, begin, end;   // places; [begin, end) is this block's
   u32 parts;               // blocks that take part
   Cursor first;
 };
 
-// Block-collective (NT threads).  At least `min_tiles` tiles a block (where there are as many).
-template <int ROWS, int TK, int NT>
-__device__ __forceinline__ Plan make_plan(const Attn &a, PlanShared &sh, u32 min_tiles) {
+// Block-collective (NT threads).  At least `least` places a block (where there are as many).
+template <int ROWS, int TK, int OVER, int NT>
+__device__ __forceinline__ Plan make_plan(const Attn &a, PlanShared &sh, u32 least) {
   Plan p;
   const u32 tid = threadIdx.x;
   u64 all = 0, mine = 0, upto = 0;
   for (u32 base = 0; base < a.n_req; base += NT) {
     const u32 r = base + tid;
     u64 sum;
-    mine = (u64)request_tiles<ROWS, TK>(a, r, r < a.n_req) * a.hkv;
+    mine = (u64)request_places<ROWS, TK, OVER>(a, r, r < a.n_req) * a.hkv;
     upto = block_scan<NT>(mine, sh, sum) + all;
     all += sum;
   }
   p.total = all;
-  u64 want = (all + min_tiles - 1) / min_tiles;
+  u64 want = (all + least - 1) / least;
   p.parts = (u32)min((u64)gridDim.x, max(want, (u64)1));
   p.begin = p.end = 0;
   if (blockIdx.x >= p.parts || all == 0) return p;
@@ -246,7 +259,7 @@ __device__ __forceinline__ Plan make_plan(const Attn &a, PlanShared &sh, u32 min
     for (u32 base = 0; base < a.n_req; base += NT) {
       const u32 r = base + tid;
       u64 sum;
-      mine = (u64)request_tiles<ROWS, TK>(a, r, r < a.n_req) * a.hkv;
+      mine = (u64)request_places<ROWS, TK, OVER>(a, r, r < a.n_req) * a.hkv;
       upto = block_scan<NT>(mine, sh, sum) + before;
       if (upto - mine <= p.begin && p.begin < upto) { sh.found_r = r; sh.found_before = upto - mine; }
       before += sum;
@@ -254,7 +267,7 @@ __device__ __forceinline__ Plan make_plan(const Attn &a, PlanShared &sh, u32 min
     }
   }
   __syncthreads();
-  p.first = cursor_in<ROWS, TK>(a, sh.found_r, p.begin - sh.found_before);
+  p.first = cursor_in<ROWS, TK, OVER>(a, sh.found_r, p.begin - sh.found_before);
   return p;
 }
 

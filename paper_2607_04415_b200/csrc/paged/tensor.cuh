@@ -150,31 +150,6 @@ __device__ __forceinline__ f32x2 add_f32x2(f32x2 a, f32x2 b) {
   return v;
 }
 
-
-// 2^x of two numbers in the multiply-add units.  x = n + f, n whole (found by adding 1.5 * 2^23, which leaves n in the
-// low bits), f in [-1/2, 1/2]; 2^f by the polynomial of degree 5 with the least largest relative error there (Remez's
-// exchange; 2e-7 with its coefficients in 32 bits), 2^n by the exponent's bits.  Below 2^-127 the result is 0.
-__device__ __forceinline__ void exp2_poly2(f32x2 x, float &y0, float &y1) {
-  float x0, x1;
-  unpack_f32(x, x0, x1);
-  asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(x0));     // -127; what is not a number stays so
-  asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(x1));
-  x = pack_f32(x0, x1);
-  const f32x2 t = add_f32x2(x, pack_f32(12582912.0f, 12582912.0f));
-  const f32x2 n = add_f32x2(t, pack_f32(-12582912.0f, -12582912.0f));
-  const f32x2 f = fma_f32x2(n, pack_f32(-1.0f, -1.0f), x);
-  f32x2 p = fma_f32x2(pack_f32(0.0013276472454890609f, 0.0013276472454890609f), f, pack_f32(0.009675540961325169f, 0.009675540961325169f));
-  p = fma_f32x2(p, f, pack_f32(0.05550713092088699f, 0.05550713092088699f));
-  p = fma_f32x2(p, f, pack_f32(0.24022120237350464f, 0.24022120237350464f));
-  p = fma_f32x2(p, f, pack_f32(0.6931469440460205f, 0.6931469440460205f));
-  p = fma_f32x2(p, f, pack_f32(1.0000001192092896f, 1.0000001192092896f));
-  float t0, t1;
-  unpack_f32(t, t0, t1);
-  unpack_f32(p, y0, y1);
-  y0 *= __uint_as_float((__float_as_uint(t0) << 23) + 0x3F800000u);
-  y1 *= __uint_as_float((__float_as_uint(t1) << 23) + 0x3F800000u);
-}
-
 template <int N>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>

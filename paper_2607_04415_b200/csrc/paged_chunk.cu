@@ -10,8 +10,10 @@
 //   8         issues both products (one thread); zeros value rows that no query sees before they are used.
 //   9         copies key and value tiles, page by page (tensor copies, zeros for pages outside the cache), into a
 //             ring of stages with the 128-byte swizzle.
-//   10        looks for values that are not finite in tiles that some rows see and others do not.
-//   11        walks the block's share of the work and tells the others its parts, one ahead; gathers the queries.
+//   10        gathers the queries; looks for values that are not finite in tiles that some rows see and others do not.
+//   11        walks the block's share of the work and tells the others its parts, ahead of them.
+// A unit of at most 128 rows has its even key tiles worked on as row tile 0 and its odd ones as row tile 1, with a running
+// maximum, sum and output each, which are joined at its end: otherwise one tile's softmax and products would wait for each other.
 // Tensor memory, 512 columns: scores of tile 0 and 1 (128 each), outputs of tile 0 and 1 (head size each).
 //
 // Running maximum: a row's reference only moves when its maximum passes it by more than 2^8, since moving it
@@ -37,7 +39,7 @@ constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;   // a thread, of 168 * 3 = 2
 constexpr u32 kScores = 0, kOutputs = 256;           // columns of tensor memory
 constexpr int kParts = 4;                            // parts that have been told and not yet finished
 constexpr int kScans = 8;                            // more parts than the ring of stages lets warp 10 run ahead
-constexpr int kPolyPairs = 0;                        // of 16 pairs of weights, those whose exponential is a polynomial
+constexpr int kOver = 2;                             // a unit's start and end cost about what two tiles do
 
 template <int D>
 struct Shape {
@@ -64,6 +66,7 @@ struct ChunkShared {
   u64 part_full[kParts], part_empty[kParts];
   u64 q_full[2], q_empty[2], s_full[2], p_full[2][2], o_full[2], scanned[kScans], meet;
   u32 odd[kScans];
+  float2 half_ml[kTileRows];
   u32 tmem, failed, last;
   PlanShared plan;
 };
@@ -123,22 +126,17 @@ __device__ __noinline__ void plain_row(const Attn &a, u32 req, u32 h, const Row 
   }
 }
 
-// Columns [0, 64) or [64, 128) of a row's scores to weights: 2^(x * mul - base), summed unrounded into `sum`, rounded to the
-// cache's type in w.  kPolyPairs of 16 exponentials are computed in the multiply-add units instead of the special function
-// units, which are what the softmax waits for.
+// 64 of a row's scores to weights: 2^(x * mul - base), summed unrounded into `sum`, rounded to the cache's type in w.  All
+// exponentials go to the special function units: computing some of them in the multiply-add units (a polynomial, two numbers an
+// instruction) was slower at every share tried, 1/8 to 1/2, as a warp then waits for its own multiply-adds instead.
 template <typename T>
 __device__ __forceinline__ void weights64(const float *s, f32x2 mul, f32x2 minus_base, f32x2 (&sum)[2], u32 *w) {
 #pragma unroll
   for (int k = 0; k < 32; ++k) {
-    const f32x2 x = fma_f32x2(pack_f32(s[2 * k], s[2 * k + 1]), mul, minus_base);
     float x0, x1;
-    if (((k & 15) * kPolyPairs) / 16 != (((k & 15) + 1) * kPolyPairs) / 16) {
-      exp2_poly2(x, x0, x1);
-    } else {
-      unpack_f32(x, x0, x1);
-      x0 = exp2_approx(x0);
-      x1 = exp2_approx(x1);
-    }
+    unpack_f32(fma_f32x2(pack_f32(s[2 * k], s[2 * k + 1]), mul, minus_base), x0, x1);
+    x0 = exp2_approx(x0);
+    x1 = exp2_approx(x1);
     sum[k & 1] = add_f32x2(sum[k & 1], pack_f32(x0, x1));
     w[k] = pack2<T>(x0, x1);
   }
@@ -165,7 +163,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
     fence_async();
   }
   if (warp == 8) tmem_alloc(&sh.tmem, 512);
-  const Plan plan = make_plan<kRows, kTileKeys, kThreads>(a, sh.plan, 1);
+  const Plan plan = make_plan<kRows, kTileKeys, kOver, kThreads>(a, sh.plan, 1);
   mma_fence_before();
   __syncthreads();
   mma_fence_after();
@@ -189,7 +187,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
     constexpr int kCols = D % 64 == 0 ? 64 : 32;             // columns of the output that are worked on at a time
     const u32 lanes = (u32)(warp & 3) << 21;                 // this warp's 32 lanes of tensor memory
     const u32 scores = tmem + kScores + t * 128 + lanes, outputs = tmem + kOutputs + t * D + lanes;
-    u32 s_phase = 0, o_phase = 0, meet_phase = 0;
+    u32 s_phase = 0, o_phase = 0, meet_phase = 0;            // o_phase: a bit for each row tile's output
     auto meet = [&]() {                                      // all eight warps, with the limit of every other wait
       __syncwarp();
       if (lane == 0) bar_arrive(&sh.meet);
@@ -199,14 +197,16 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
     };
     PartInfo p;
     for (u32 no = 0; take_part(no, p); ++no) {
-      const bool mine = t == 0 || p.rows > kTileRows;        // does the unit have this row tile at all
-      const bool valid = t * kTileRows + row < p.rows;
-      const Row r = row_of(a, p, (u32)p.row0 + (valid ? t * kTileRows + row : 0));
+      const bool split = p.rows <= kTileRows;                // one row tile: key tiles by turns
+      const bool mine = t == 0 || !split;                    // whose rows this warpgroup writes
+      const int unit_row = (split ? 0 : t * kTileRows) + row, first = split ? t : 0;
+      const bool valid = unit_row < p.rows;
+      const Row r = row_of(a, p, (u32)p.row0 + (valid ? unit_row : 0));
       float m = -INFINITY, l = 0.0f;
-      if (mine) {
+      {
         const float slope = SCORED && a.slopes ? a.slopes[r.head] * kLog2e : 0.0f;
         const float mul = SCORED ? 1.0f : a.scale * kLog2e;
-        for (int at = 0; at < p.tiles; ++at) {
+        for (int at = first; at < p.tiles; at += split ? 2 : 1) {
           if (!bar_wait(&sh.s_full[t], s_phase, failed)) break;
           s_phase ^= 1;
           mma_fence_after();
@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
             const float f = m == -INFINITY ? 0.0f : exp2_approx(m - to);
             m = to;
             l *= f;
-            if (at > 0) {                                    // the scores' arrival says that the product before is done
+            if (at > first) {                                // the scores' arrival says that the product before is done
 #pragma unroll
               for (int i = 0; i < D / 32; ++i) {
                 float o[32];
@@ -284,10 +284,28 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
       }
       bool fine = true, odd = false;
       const int k0 = p.tile * kTileKeys, k1 = (p.tile + p.tiles) * kTileKeys;
+      const bool two = split && p.tiles > 1;                 // both warpgroups have a part of the same rows
+      if (two && t == 1) sh.half_ml[row] = make_float2(m, l);
+      if (mine) fine = bar_wait(&sh.scanned[no % kScans], (no / kScans) & 1, failed);
+      for (int u = 0; u < 2; ++u) {                          // each keeps count of both outputs' phases
+        if (u == 1 && split && !two) continue;
+        if (u == t || two) fine = bar_wait(&sh.o_full[u], (o_phase >> u) & 1, failed) && fine;
+        o_phase ^= 1u << u;
+      }
+      mma_fence_after();
+      float f0 = 1.0f, f1 = 0.0f;
+      if (two) {
+        fine = meet() && fine;
+        if (t == 0) {
+          const float2 other = sh.half_ml[row];
+          const float top = fmaxf(m, other.x), base = top == -INFINITY ? 0.0f : top;
+          f0 = exp2_approx(m - base);
+          f1 = exp2_approx(other.x - base);
+          l = l * f0 + other.y * f1;
+          m = top;
+        }
+      }
       if (mine) {
-        fine = bar_wait(&sh.scanned[no % kScans], (no / kScans) & 1, failed) && bar_wait(&sh.o_full[t], o_phase, failed);
-        o_phase ^= 1;
-        mma_fence_after();
         odd = fine && sh.odd[no % kScans] != 0;
         if (odd) {
           float top, sum;
@@ -313,6 +331,17 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
         tmem_wait_ld();
 #pragma unroll
         for (int i = 0; i < kCols / 32; ++i) keep(o + 32 * i);
+        if (two && !odd) {
+#pragma unroll
+          for (int i = 0; i < kCols / 32; ++i) {
+            float x[32];
+            tmem_ld32(x, outputs + D + col + 32 * i);
+            tmem_wait_ld();
+            keep(x);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) o[32 * i + k] = f0 * o[32 * i + k] + f1 * x[k];
+          }
+        }
       };
       auto write = [&](const float *o, int col, float f) {
         uint4 *to = (uint4 *)((u16 *)a.out + r.tok * a.o_t + (i64)r.head * a.o_h + col);
@@ -321,7 +350,6 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
           to[k] = make_uint4(pack2<T>(o[8 * k] * f, o[8 * k + 1] * f), pack2<T>(o[8 * k + 2] * f, o[8 * k + 3] * f), pack2<T>(o[8 * k + 4] * f, o[8 * k + 5] * f),
                              pack2<T>(o[8 * k + 6] * f, o[8 * k + 7] * f));
       };
-      const int unit_row = t * kTileRows + row;
       if (p.whole) {
         if (mine && fine) {
           const float f = l == 0.0f ? 0.0f : 1.0f / l;
@@ -404,9 +432,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
             }
           }
         }
-        meet();                                              // sh.last is free again
       }
       mma_fence_before();
+      if (two || !p.whole) meet();                           // sh.last and the other's output are free again
       part_done(no);
     }
   } else {
@@ -420,20 +448,20 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
       const u32 tm = uniform(tmem), q_at = uniform(operand(sh.q[0], 16)), k_at = uniform(operand(sh.kv[0], 16)), v_at = uniform(operand(sh.kv[0], kTileKeys * 128));
       u32 stage = 0, kv_phase = 0, q_phase = 0, p_phase = 0;          // bit t of the last two
       bool fine = true;
-      // Scores of row tile t with the key tile in k_stage; `last`: the queries are not needed after it.  `frees`: no product needs
+      // Scores of queries q_tile with the key tile in k_stage, to row tile t's place; `last`: the queries are not needed after it.  `frees`: no product needs
       // the stages v_stage and k_stage after it.  One region of the issuing lane for all, since what stands between two
       // products has to be shorter than what the matrix unit has queued, some 200 cycles.
-      auto scores_of = [&](u32 t, u32 k_stage, bool last, bool frees, u32 v_stage) {
+      auto scores_of = [&](u32 t, u32 q_tile, u32 k_stage, bool last, bool frees, u32 v_stage) {
         if (one_lane()) {
 #pragma unroll
           for (u32 i = 0; i < D / 16; ++i)
-            mma_ss(tm + kScores + t * 128, q_at + t * kTile + (i >> 2) * kChunk + (i & 3) * 2, k_at + k_stage * kTile + (i >> 2) * kChunk + (i & 3) * 2, kScoreShape, i > 0);
+            mma_ss(tm + kScores + t * 128, q_at + q_tile * kTile + (i >> 2) * kChunk + (i & 3) * 2, k_at + k_stage * kTile + (i >> 2) * kChunk + (i & 3) * 2, kScoreShape, i > 0);
           mma_commit(&sh.s_full[t]);
           if (frees) {
             if (v_stage != k_stage) mma_commit(&sh.kv_empty[v_stage]);
             mma_commit(&sh.kv_empty[k_stage]);
           }
-          if (last) mma_commit(&sh.q_empty[t]);
+          if (last) mma_commit(&sh.q_empty[q_tile]);
         }
         __syncwarp();
       };
@@ -451,15 +479,63 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
       for (u32 no = 0; fine; ++no) {
         PartInfo p;
         if (!__all_sync(0xffffffffu, take_part(no, p))) break;
-        const u32 n_tiles = uniform((u32)p.tiles), row_tiles = uniform(p.rows > kTileRows ? 2u : 1u);
-        for (u32 t = 0; t < row_tiles; ++t) {
-          fine = fine && warp_wait(&sh.q_full[t], (q_phase >> t) & 1, failed);
-          q_phase ^= 1u << t;
+        const u32 n_tiles = uniform((u32)p.tiles);
+        // rows of a tile that lie outside [lo, hi): zero, whatever the pages hold there
+        auto zero_rows = [&](u32 at, u32 v_stage) {
+          const int key0 = (p.tile + (int)at) * kTileKeys;
+          if (key0 >= p.lo && key0 + kTileKeys <= p.hi) return;
+          const int z0 = max(0, min(kTileKeys, p.lo - key0)), z1 = max(z0, min(kTileKeys, p.hi - key0)), rows = z0 + kTileKeys - z1;
+          for (int x = lane; x < rows * 8; x += 32) {
+            const int k = (x >> 3) < z0 ? x >> 3 : (x >> 3) - z0 + z1;
+#pragma unroll
+            for (int i = 0; i < S::chunks; ++i) *(uint4 *)(sh.kv[v_stage] + i * (kTileKeys * 128) + k * 128 + (x & 7) * 16) = make_uint4(0, 0, 0, 0);
+          }
+          fence_async();
+          __syncwarp();
+        };
+        fine = warp_wait(&sh.q_full[0], q_phase & 1, failed);
+        q_phase ^= 1;
+        if (uniform(p.rows <= kTileRows)) {
+          // one row tile: key tile i goes to place i & 1; the ring holds key, value, key, value ...
+          auto ahead = [&](u32 by, u32 &ph) {                         // the stage `by` fills after this one
+            const u32 i = stage + by;
+            ph = i >= (u32)S::stages ? kv_phase ^ 1 : kv_phase;
+            return i >= (u32)S::stages ? i - S::stages : i;
+          };
+          for (u32 i = 0; i < 2 && i < n_tiles && fine; ++i) {
+            u32 ph;
+            const u32 k_stage = ahead(2 * i, ph);
+            fine = warp_wait(&sh.kv_full[k_stage], ph, failed);
+            if (!fine) break;
+            mma_fence_after();
+            scores_of(i, 0, k_stage, i + 1 == n_tiles, true, k_stage);
+          }
+          for (u32 at = 0; at < n_tiles && fine; ++at) {
+            u32 v_ph, k_ph;
+            const u32 t = at & 1, v_stage = ahead(1, v_ph), k_stage = ahead(4, k_ph);
+            const bool more = at + 2 < n_tiles;
+            fine = warp_wait(&sh.kv_full[v_stage], v_ph, failed) && (!more || warp_wait(&sh.kv_full[k_stage], k_ph, failed));
+            if (!fine) break;
+            zero_rows(at, v_stage);
+            for (u32 half = 0; half < 2 && fine; ++half) {
+              fine = warp_wait(&sh.p_full[t][half], (p_phase >> t) & 1, failed);
+              if (!fine) break;
+              mma_fence_after();
+              outputs_of(t, v_stage, half, at > 1 || half > 0, half == 1 && !more, half == 1);
+            }
+            p_phase ^= 1u << t;
+            if (more && fine) scores_of(t, 0, k_stage, at + 3 == n_tiles, true, k_stage);
+            step();
+            step();
+          }
+          part_done(no);
+          continue;
         }
-        fine = fine && warp_wait(&sh.kv_full[stage], kv_phase, failed);
+        fine = fine && warp_wait(&sh.q_full[1], q_phase >> 1, failed) && warp_wait(&sh.kv_full[stage], kv_phase, failed);
+        q_phase ^= 2;
         if (!fine) break;
         mma_fence_after();
-        for (u32 t = 0; t < row_tiles; ++t) scores_of(t, stage, n_tiles == 1, t + 1 == row_tiles, stage);
+        for (u32 t = 0; t < 2; ++t) scores_of(t, t, stage, n_tiles == 1, t == 1, stage);
         step();
         fine = warp_wait(&sh.kv_full[stage], kv_phase, failed);
         for (u32 at = 0; at < n_tiles && fine; ++at) {
@@ -469,23 +545,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
           step();
           const u32 k_stage = stage;
           if (more && at == 0) fine = warp_wait(&sh.kv_full[k_stage], kv_phase, failed);
-          // rows of the tile that lie outside [lo, hi): zero, whatever the pages hold there
-          const int key0 = (p.tile + (int)at) * kTileKeys;
-          if (key0 < p.lo || key0 + kTileKeys > p.hi) {
-            const int z0 = max(0, min(kTileKeys, p.lo - key0)), z1 = max(z0, min(kTileKeys, p.hi - key0)), rows = z0 + kTileKeys - z1;
-            for (int x = lane; x < rows * 8; x += 32) {
-              const int k = (x >> 3) < z0 ? x >> 3 : (x >> 3) - z0 + z1;
-#pragma unroll
-              for (int i = 0; i < S::chunks; ++i) *(uint4 *)(sh.kv[v_stage] + i * (kTileKeys * 128) + k * 128 + (x & 7) * 16) = make_uint4(0, 0, 0, 0);
-            }
-            fence_async();
-            __syncwarp();
-          }
+          zero_rows(at, v_stage);
           if (more) step();                                           // to the next tile's values
 #pragma unroll
           for (u32 t = 0; t < 2; ++t) {
-            if (t >= row_tiles) break;
-            const bool final_t = t + 1 == row_tiles;
+            const bool final_t = t == 1;
             for (u32 half = 0; half < 2; ++half) {
               fine = fine && warp_wait(&sh.p_full[t][half], (p_phase >> t) & 1, failed);
               if (!fine) break;
@@ -495,7 +559,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
             p_phase ^= 1u << t;
             if (!fine) break;
             if (more) {
-              scores_of(t, k_stage, at + 2 == n_tiles, final_t, v_stage);
+              scores_of(t, t, k_stage, at + 2 == n_tiles, final_t, v_stage);
               // what the next tile needs, looked at while these products run: its values, then the keys after it
               if (t == 0) fine = warp_wait(&sh.kv_full[stage], kv_phase, failed);
               if (fine && final_t && at + 2 < n_tiles) {
@@ -543,85 +607,16 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
           while (!bar_try(&sh.kv_full[i], i < stage ? phase ^ 1 : phase) && now_ns() - t0 < kWaitLimitNs) {}
       }
     } else if (warp == 10) {
-      // ---------------------------------------------------------------- values that are not finite
+      // ---------------------------------------------------------------- the queries, values that are not finite
       int stage = 0;
-      u32 phase = 0;
+      u32 phase = 0, q_phase = 3;                                     // bit t: the first round finds both tiles free
       bool fine = true;
       PartInfo p;
       for (u32 no = 0; fine && take_part(no, p); ++no) {
-        // keys that all rows see: [last row's first, first row's last]
-        const Row first = row_of(a, p, (u32)p.row0), last = row_of(a, p, (u32)(p.row0 + p.rows - 1));
-        u32 odd = 0;
-        for (int at = 0; at < p.tiles && fine; ++at) {
-          const int key0 = (p.tile + at) * kTileKeys, z0 = max(key0, p.lo), z1 = min(key0 + kTileKeys, p.hi);
-          const bool look = z0 < last.lo || z1 > first.hi;
-#pragma unroll
-          for (int kv = 0; kv < 2; ++kv) {
-            fine = fine && bar_wait(&sh.kv_full[stage], phase, failed);
-            if (!fine) break;
-            if (kv && look) {
-              for (int x = lane; x < S::chunks * kTileKeys * 8; x += 32) {
-                const int k = key0 + ((x >> 3) & (kTileKeys - 1));
-                if (k >= z0 && k < z1 && not_finite8<T>(*(const uint4 *)(sh.kv[stage] + x * 16))) odd = 1;
-              }
-            }
-            __syncwarp();
-            if (lane == 0) bar_arrive(&sh.kv_empty[stage]);
-            if (++stage == S::stages) { stage = 0; phase ^= 1; }
-          }
-        }
-        odd = __any_sync(0xffffffffu, odd);
-        if (lane == 0) {
-          sh.odd[no % kScans] = odd;
-          bar_arrive(&sh.scanned[no % kScans]);
-        }
-        part_done(no);
-      }
-    } else {
-      // ---------------------------------------------------------------- the parts and their queries
-      Cursor c = plan.first;
-      u64 left = plan.end - plan.begin;
-      u32 told = 0;
-      auto tell = [&]() {                                             // the part at c, or the end
-        const u32 slot = told % kParts;
-        const bool ok = bar_wait(&sh.part_empty[slot], ((told / kParts) & 1) ^ 1, failed);
-        ++told;
-        if (!ok) return false;
-        PartInfo p{};
-        if (left) {
-          p.r = (int)c.r; p.h = (int)c.h; p.len = c.req.len; p.n = c.req.n; p.q0 = c.req.q0;
-          p.row0 = c.m * kRows;
-          p.rows = (int)min((i64)kRows, (i64)c.req.n * a.group - p.row0);
-          const int to = (int)min((u64)c.span.tiles, (u64)c.at + left);
-          p.tile = c.span.first + c.at;
-          p.tiles = to - c.at;
-          p.lo = c.span.lo; p.hi = c.span.hi;
-          p.whole = c.at == 0 && to == c.span.tiles;
-          if (!p.whole) {
-            const u64 unit0 = plan.end - left - (u64)c.at;
-            p.i0 = part_owner(plan.total, unit0, plan.parts);
-            p.i1 = part_owner(plan.total, unit0 + (u64)c.span.tiles - 1, plan.parts);
-          }
-          left -= (u64)p.tiles;
-        }
-        if (lane == 0) {
-          sh.part[slot] = p;
-          bar_arrive(&sh.part_full[slot]);
-        }
-        __syncwarp();
-        return true;
-      };
-      u32 phase = 3;                                                  // bit t: the first round finds both tiles free
-      bool more = left != 0, fine = tell();
-      for (u32 no = 0; fine && more; ++no) {
-        const PartInfo p = sh.part[no % kParts];                      // stays until all warps are done with it
-        more = left != 0;
-        if (more) next_unit<kRows, kTileKeys>(a, c);
-        fine = tell();
         const int tiles = p.rows > kTileRows ? 2 : 1;
         for (int t = 0; t < tiles && fine; ++t) {
-          fine = bar_wait(&sh.q_empty[t], (phase >> t) & 1, failed);
-          phase ^= 1u << t;
+          fine = bar_wait(&sh.q_empty[t], (q_phase >> t) & 1, failed);
+          q_phase ^= 1u << t;
           if (!fine) break;
           for (int r = lane >> 2; r < kTileRows; r += 8) {            // four lanes a row; zeros past the last row
             const bool valid = t * kTileRows + r < p.rows;
@@ -640,6 +635,67 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
         __syncwarp();
         if (lane == 0 && fine)
           for (int t = 0; t < tiles; ++t) bar_arrive(&sh.q_full[t]);
+        // all rows see the keys from the last row's first to the first row's last; others of [lo, hi) are looked at
+        const Row first = row_of(a, p, (u32)p.row0), last = row_of(a, p, (u32)(p.row0 + p.rows - 1));
+        u32 odd = 0;
+        for (int at = 0; at < p.tiles && fine; ++at) {
+          const int key0 = (p.tile + at) * kTileKeys, z0 = max(key0, p.lo), z1 = min(key0 + kTileKeys, p.hi);
+          const bool look = z0 < last.lo || z1 > first.hi;
+#pragma unroll
+          for (int kv = 0; kv < 2; ++kv) {
+            fine = fine && bar_wait(&sh.kv_full[stage], phase, failed);
+            if (!fine) break;
+            if (kv && look) {
+              for (int x = lane; x < S::chunks * kTileKeys * 8; x += 32) {
+                const int k = key0 + ((x >> 3) & (kTileKeys - 1));
+                if (k >= z0 && k < z1 && (k < last.lo || k >= first.hi) && not_finite8<T>(*(const uint4 *)(sh.kv[stage] + x * 16))) odd = 1;
+              }
+            }
+            __syncwarp();
+            if (lane == 0) bar_arrive(&sh.kv_empty[stage]);
+            if (++stage == S::stages) { stage = 0; phase ^= 1; }
+          }
+        }
+        odd = __any_sync(0xffffffffu, odd);
+        if (lane == 0) {
+          sh.odd[no % kScans] = odd;
+          bar_arrive(&sh.scanned[no % kScans]);
+        }
+        part_done(no);
+      }
+    } else {
+      // ---------------------------------------------------------------- the parts
+      Cursor c = plan.first;
+      u64 left = plan.end - plan.begin;
+      bool more = true;
+      for (u32 told = 0; more; ++told) {
+        settle<kRows, kTileKeys, kOver>(a, c, left);
+        const u32 slot = told % kParts;
+        PartInfo p{};
+        more = left != 0;
+        if (more) {
+          p.r = (int)c.r; p.h = (int)c.h; p.len = c.req.len; p.n = c.req.n; p.q0 = c.req.q0;
+          p.row0 = c.m * kRows;
+          p.rows = (int)min((i64)kRows, (i64)c.req.n * a.group - p.row0);
+          const int to = (int)min((u64)c.span.tiles, (u64)c.at + left);
+          p.tile = c.span.first + c.at;
+          p.tiles = to - c.at;
+          p.lo = c.span.lo; p.hi = c.span.hi;
+          p.whole = c.at == 0 && to == c.span.tiles;
+          if (!p.whole) {
+            const u64 unit0 = plan.end - left - (u64)c.at;
+            p.i0 = part_owner(plan.total, unit0, plan.parts);
+            p.i1 = part_owner(plan.total, unit0 + (u64)c.span.tiles - 1, plan.parts);
+          }
+          left -= (u64)p.tiles;
+          c.at = to;
+        }
+        if (!bar_wait(&sh.part_empty[slot], ((told / kParts) & 1) ^ 1, failed)) break;
+        if (lane == 0) {
+          sh.part[slot] = p;
+          bar_arrive(&sh.part_full[slot]);
+        }
+        __syncwarp();
       }
     }
   }

@@ -27,6 +27,7 @@ constexpr int kThreads = kWarps * 32;
 constexpr int kWarpKeys = 16;
 constexpr int kTile = kWarps * kWarpKeys;
 constexpr int kStages = 3;
+constexpr int kOver = 1;            // a unit's start and end cost about what a tile does
 constexpr int kBlocksPerSm = 2;
 
 template <int D>
@@ -49,11 +50,11 @@ __device__ __forceinline__ int piece_at(int row, int piece) {
 }
 
 template <typename T, int D, bool SCORED>
-__global__ void __launch_bounds__(kThreads, kBlocksPerSm) attention_rows_kernel(const Attn a, const u32 min_tiles) {
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm) attention_rows_kernel(const Attn a, const u32 least) {
   extern __shared__ __align__(128) unsigned char raw[];
   RowsShared<D> &sh = *(RowsShared<D> *)raw;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const Plan plan = make_plan<kRows, kTile, kThreads>(a, sh.plan, min_tiles);
+  const Plan plan = make_plan<kRows, kTile, kOver, kThreads>(a, sh.plan, least);
   if (plan.begin >= plan.end) return;
 
   constexpr int P = D / 8;                       // 16-byte pieces of a row
@@ -63,6 +64,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) attention_rows_kernel(
   // --- the loading side: a cursor that runs ahead, and the cache row of the next tile's key that this lane looks up
   Cursor ld = plan.first;
   u64 ld_left = plan.end - plan.begin;
+  settle<kRows, kTile, kOver>(a, ld, ld_left);
   int key_page = -1, key_in = 0;                 // of key (lane & 15) of the tile at ld; -1: zeros
   auto look_up = [&]() {
     if (ld_left == 0) return;
@@ -89,7 +91,8 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) attention_rows_kernel(
         cp_async16(vs + piece_at<D>(row, piece) * 8, vh + page * a.v_p + tok * a.v_t + piece * 8, bytes);
       }
       --ld_left;
-      if (++ld.at == ld.span.tiles && ld_left) next_unit<kRows, kTile>(a, ld);
+      ++ld.at;
+      settle<kRows, kTile, kOver>(a, ld, ld_left);
       look_up();
     }
     cp_async_commit();
@@ -102,7 +105,8 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) attention_rows_kernel(
   Cursor c = plan.first;
   int stage = 0;
   const int g = lane >> 2, t4 = lane & 3;
-  for (u64 left = plan.end - plan.begin; left;) {
+  u64 left = plan.end - plan.begin;
+  for (settle<kRows, kTile, kOver>(a, c, left); left; settle<kRows, kTile, kOver>(a, c, left)) {
     const int from = c.at;
     const int to = (int)min((u64)c.span.tiles, (u64)from + left);
     const i64 row0 = (i64)c.m * kRows;
@@ -237,6 +241,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) attention_rows_kernel(
       }
     }
     left -= (u64)(to - from);
+    c.at = to;
 
     // --- join the four warps
     float *mine = (float *)sh.ring[warp][stage];
@@ -294,7 +299,6 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) attention_rows_kernel(
     __syncthreads();
     issue(stage);
     stage = stage + 1 == kStages ? 0 : stage + 1;
-    if (left) next_unit<kRows, kTile>(a, c);
   }
   cp_async_wait<0>();
 }
