@@ -62,8 +62,7 @@ struct Span {
 
 template <int ROWS, int TK>
 __device__ __forceinline__ Span unit_span(const Attn &a, int len, int n, int m) {
-  const i64 rows = (i64)n * a.group;
-  const i64 r0 = (i64)m * ROWS, r1 = min(rows, r0 + ROWS);
+  const u32 r0 = (u32)m * ROWS, r1 = min((u32)n * a.group, r0 + ROWS);      // n * group < 2^31
   const int ta = (int)(r0 / a.group), tb = (int)((r1 - 1) / a.group);
   Span s;
   s.hi = a.causal ? min(len, len - n + tb + 1) : len;
@@ -76,7 +75,7 @@ __device__ __forceinline__ Span unit_span(const Attn &a, int len, int n, int m) 
 
 template <int ROWS>
 __device__ __forceinline__ int unit_count(const Attn &a, int n) {
-  return (int)(((i64)n * a.group + ROWS - 1) / ROWS);
+  return (int)(((u32)n * a.group + ROWS - 1) / ROWS);
 }
 
 // The plan.  All tiles of a call, in the order (request, key head, unit, tile), are one line; a unit's tiles are followed
@@ -94,15 +93,20 @@ struct Cursor {
 };
 
 struct PlanShared {
-  u64 warp_sum[32];
-  u64 found_before;
-  u32 found_r;
-  u32 pad;
+  u32 warp_sum[32];
+  u32 found_r, found_before;
 };
 
-__device__ __forceinline__ u64 part_begin(u64 total, u32 i, u32 n) { return total * i / n; }
-// the block that owns place x: the largest i with total*i/n <= x
-__device__ __forceinline__ u32 part_owner(u64 total, u64 x, u32 n) { return (u32)(((x + 1) * n - 1) / total); }
+// Block i's share of `total` places begins here: the first total % n blocks have one place more than the others.
+__device__ __forceinline__ u32 part_begin(u32 total, u32 i, u32 n) {
+  const u32 each = total / n, more = total - each * n;
+  return each * i + min(i, more);
+}
+// the block that owns place x
+__device__ __forceinline__ u32 part_owner(u32 total, u32 x, u32 n) {
+  const u32 each = total / n, more = total - each * n, first = more * (each + 1);
+  return x < first ? x / (each + 1) : more + (x - first) / each;
+}
 
 // Places of request r over all its units (of one key head).  Warp-collective; lane's own request is r
 // (in range where `have`); requests of many units are summed by the whole warp.
@@ -130,23 +134,28 @@ __device__ __forceinline__ u32 request_places(const Attn &a, u32 r, bool have) {
   return sum;
 }
 
-// Inclusive sum over the block of one value a thread; `all` is the block's sum.  Two barriers.
-template <int NT>
-__device__ __forceinline__ u64 block_scan(u64 v, PlanShared &sh, u64 &all) {
-  const u32 lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  u64 x = v;
+__device__ __forceinline__ u32 warp_scan(u32 x) {
+  const u32 lane = threadIdx.x & 31;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const u64 y = __shfl_up_sync(0xffffffffu, x, d);
+    const u32 y = __shfl_up_sync(0xffffffffu, x, d);
     if ((int)lane >= d) x += y;
   }
+  return x;
+}
+
+// Inclusive sum over the block of one value a thread; `all` is the block's sum.  Two barriers.
+template <int NT>
+__device__ __forceinline__ u32 block_scan(u32 v, PlanShared &sh, u32 &all) {
+  const u32 lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const u32 x = warp_scan(v);
   if (lane == 31) sh.warp_sum[warp] = x;
   __syncthreads();
-  u64 before = 0;
+  u32 before = 0;
   all = 0;
 #pragma unroll
   for (int w = 0; w < NT / 32; ++w) {
-    const u64 s = sh.warp_sum[w];
+    const u32 s = sh.warp_sum[w];
     if (w < (int)warp) before += s;
     all += s;
   }
@@ -157,7 +166,7 @@ __device__ __forceinline__ u64 block_scan(u64 v, PlanShared &sh, u64 &all) {
 // Sets the cursor to the place `offset` places after the first of request r.  Warp-collective, the same
 // for all warps.
 template <int ROWS, int TK, int OVER>
-__device__ __forceinline__ Cursor cursor_in(const Attn &a, u32 r, u64 offset) {
+__device__ __forceinline__ Cursor cursor_in(const Attn &a, u32 r, u32 offset) {
   const u32 lane = threadIdx.x & 31;
   Cursor c;
   c.r = r;
@@ -166,19 +175,14 @@ __device__ __forceinline__ Cursor cursor_in(const Attn &a, u32 r, u64 offset) {
   u32 per_head = 0;
   for (int m = (int)lane; m < units; m += 32) per_head += (u32)unit_span<ROWS, TK>(a, c.req.len, c.req.n, m).tiles + OVER;
   per_head = __reduce_add_sync(0xffffffffu, per_head);
-  c.h = (u32)(offset / per_head);
-  u32 o = (u32)(offset % per_head);
+  c.h = offset / per_head;
+  u32 o = offset - c.h * per_head;
   c.m = 0;
   c.at = 0;
   for (int base = 0; base < units; base += 32) {
     const int m = base + (int)lane;
     const u32 t = m < units ? (u32)unit_span<ROWS, TK>(a, c.req.len, c.req.n, m).tiles + OVER : 0u;
-    u32 x = t;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const u32 y = __shfl_up_sync(0xffffffffu, x, d);
-      if ((int)lane >= d) x += y;
-    }
+    const u32 x = warp_scan(t);
     const u32 hit = __ballot_sync(0xffffffffu, o < x);
     if (hit) {
       const int src = __ffs(hit) - 1;
@@ -216,9 +220,9 @@ __device__ __forceinline__ bool next_unit(const Attn &a, Cursor &c) {
 // Moves the cursor from a place without work, or past the unit's last tile, to the next tile; `left`: places of the block's
 // share from the cursor on, 0 at its end.
 template <int ROWS, int TK, int OVER>
-__device__ __forceinline__ void settle(const Attn &a, Cursor &c, u64 &left) {
+__device__ __forceinline__ void settle(const Attn &a, Cursor &c, u32 &left) {
   while (left && c.at >= c.span.tiles) {
-    const u64 skip = (u64)(c.span.tiles + OVER - c.at);
+    const u32 skip = (u32)(c.span.tiles + OVER - c.at);
     if (skip >= left) { left = 0; return; }
     left -= skip;
     if (!next_unit<ROWS, TK>(a, c)) left = 0;
@@ -226,45 +230,41 @@ __device__ __forceinline__ void settle(const Attn &a, Cursor &c, u64 &left) {
 }
 
 struct Plan {
-  u64 total, begin, end;   // places; [begin, end) is this block's
+  u32 total, begin, end;   // places; [begin, end) is this block's
   u32 parts;               // blocks that take part
   Cursor first;
 };
 
-// Block-collective (NT threads).  At least `least` places a block (where there are as many).
+__device__ __forceinline__ bool share(Plan &p, u32 total, u32 least) {
+  p.total = total;
+  p.parts = max(1u, min(gridDim.x, (total + least - 1) / least));
+  p.begin = p.end = 0;
+  if (blockIdx.x >= p.parts || total == 0) return false;
+  p.begin = part_begin(total, blockIdx.x, p.parts);
+  p.end = part_begin(total, blockIdx.x + 1, p.parts);
+  return p.begin < p.end;
+}
+
+// By a block of NT threads; at least `least` places a block, where there are as many.  (One warp alone, without the
+// barriers, took longer even for one request.)
 template <int ROWS, int TK, int OVER, int NT>
-__device__ __forceinline__ Plan make_plan(const Attn &a, PlanShared &sh, u32 least) {
-  Plan p;
+__device__ __forceinline__ Plan block_plan(const Attn &a, PlanShared &sh, u32 least) {
   const u32 tid = threadIdx.x;
-  u64 all = 0, mine = 0, upto = 0;
+  u32 all = 0;
   for (u32 base = 0; base < a.n_req; base += NT) {
-    const u32 r = base + tid;
-    u64 sum;
-    mine = (u64)request_places<ROWS, TK, OVER>(a, r, r < a.n_req) * a.hkv;
-    upto = block_scan<NT>(mine, sh, sum) + all;
+    u32 sum;
+    block_scan<NT>(request_places<ROWS, TK, OVER>(a, base + tid, base + tid < a.n_req) * a.hkv, sh, sum);
     all += sum;
   }
-  p.total = all;
-  u64 want = (all + least - 1) / least;
-  p.parts = (u32)min((u64)gridDim.x, max(want, (u64)1));
-  p.begin = p.end = 0;
-  if (blockIdx.x >= p.parts || all == 0) return p;
-  p.begin = part_begin(all, blockIdx.x, p.parts);
-  p.end = part_begin(all, blockIdx.x + 1, p.parts);
-  if (p.begin >= p.end) return p;
-  if (a.n_req <= NT) {
-    if (upto - mine <= p.begin && p.begin < upto) { sh.found_r = tid; sh.found_before = upto - mine; }
-  } else {                                              // the first pass kept only its last round
-    u64 before = 0;
-    for (u32 base = 0; base < a.n_req; base += NT) {
-      const u32 r = base + tid;
-      u64 sum;
-      mine = (u64)request_places<ROWS, TK, OVER>(a, r, r < a.n_req) * a.hkv;
-      upto = block_scan<NT>(mine, sh, sum) + before;
-      if (upto - mine <= p.begin && p.begin < upto) { sh.found_r = r; sh.found_before = upto - mine; }
-      before += sum;
-      if (before > p.begin) break;
-    }
+  Plan p;
+  if (!share(p, all, least)) return p;
+  u32 before = 0;
+  for (u32 base = 0; before <= p.begin; base += NT) {
+    u32 sum;
+    const u32 r = base + tid, mine = request_places<ROWS, TK, OVER>(a, r, r < a.n_req) * a.hkv;
+    const u32 upto = before + block_scan<NT>(mine, sh, sum);
+    if (upto - mine <= p.begin && p.begin < upto) { sh.found_r = r; sh.found_before = upto - mine; }
+    before += sum;
   }
   __syncthreads();
   p.first = cursor_in<ROWS, TK, OVER>(a, sh.found_r, p.begin - sh.found_before);

@@ -81,13 +81,17 @@ __device__ __forceinline__ float exp2_approx(float x) {
   return y;
 }
 
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // cap * tanh(x / cap) as cap * (1 - 2 / (1 + e^(2x/cap))): the error is some 1e-7 of the cap, where the
 // hardware's tanh is good to 5e-4 of it only, which would show in the weights.
 // Result in units of log2; `in` is scale * 2 log2(e) / cap, `out` is cap * log2(e).
 __device__ __forceinline__ float capped_log2(float dot, float in, float out) {
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + exp2_approx(dot * in)));
-  return fmaf(-2.0f * out, r, out);
+  return fmaf(-2.0f * out, rcp_approx(1.0f + exp2_approx(dot * in)), out);
 }
 
 // Writes four columns of a finished row: acc / sum, rounded once.  A row that sees no key has sum 0 and gives 0 and

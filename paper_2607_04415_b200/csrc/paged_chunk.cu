@@ -20,7 +20,7 @@
 // costs a pass over the output in tensor memory; weights are then at most 2^8, far inside both types.
 // The sum of the weights is held unrounded in 32 bits, the weights are rounded once to the cache's type.
 //
-// Blocks take equal shares of all key tiles of the call (make_plan), cut units are joined by their last block.
+// Blocks take equal shares of all key tiles of the call (the plan), cut units are joined by their last block.
 // Values that are not finite (and masked for some rows) would reach rows that do not see them, as 0 * inf in the
 // product: a unit that meets one is computed again row by row from the cache, slowly, in plain_row.
 #include "paged/common.cuh"
@@ -149,21 +149,21 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
   ChunkShared<D> &sh = *(ChunkShared<D> *)(raw + ((1024 - (smem_addr(raw) & 1023)) & 1023));
   typedef Shape<D> S;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (tid == 0) {
-    for (int i = 0; i < S::stages; ++i) { bar_init(&sh.kv_full[i], 1); bar_init(&sh.kv_empty[i], 2); }
-    for (int i = 0; i < kParts; ++i) { bar_init(&sh.part_full[i], 1); bar_init(&sh.part_empty[i], 11); }
-    for (int t = 0; t < 2; ++t) {
-      bar_init(&sh.q_full[t], 1); bar_init(&sh.q_empty[t], 1); bar_init(&sh.s_full[t], 1); bar_init(&sh.o_full[t], 1);
-      bar_init(&sh.p_full[t][0], 4); bar_init(&sh.p_full[t][1], 4);
+  if (warp == 8) {
+    for (int i = lane; i < S::stages; i += 32) { bar_init(&sh.kv_full[i], 1); bar_init(&sh.kv_empty[i], 2); }
+    if (lane < kParts) { bar_init(&sh.part_full[lane], 1); bar_init(&sh.part_empty[lane], 11); }
+    if (lane < kScans) { bar_init(&sh.scanned[lane], 1); sh.odd[lane] = 0; }
+    if (lane < 2) {
+      bar_init(&sh.q_full[lane], 1); bar_init(&sh.q_empty[lane], 1); bar_init(&sh.s_full[lane], 1); bar_init(&sh.o_full[lane], 1);
+      bar_init(&sh.p_full[lane][0], 4); bar_init(&sh.p_full[lane][1], 4);
     }
-    for (int i = 0; i < kScans; ++i) { bar_init(&sh.scanned[i], 1); sh.odd[i] = 0; }
-    bar_init(&sh.meet, 8);
-    sh.failed = 0;
+    if (lane == 0) { bar_init(&sh.meet, 8); sh.failed = 0; }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async();
+    __syncwarp();
+    tmem_alloc(&sh.tmem, 512);
   }
-  if (warp == 8) tmem_alloc(&sh.tmem, 512);
-  const Plan plan = make_plan<kRows, kTileKeys, kOver, kThreads>(a, sh.plan, 1);
+  const Plan plan = block_plan<kRows, kTileKeys, kOver, kThreads>(a, sh.plan, 1);
   mma_fence_before();
   __syncthreads();
   mma_fence_after();
@@ -217,19 +217,24 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
 #pragma unroll
           for (int i = 0; i < 4; ++i) keep(s + 32 * i);
           const int key0 = (p.tile + at) * kTileKeys;
-          if (SCORED) {
-            if (a.softcap > 0.0f) {
-              const float in = a.scale * (2.0f * kLog2e / a.softcap), out = a.softcap * kLog2e;
+          if (SCORED) {                                      // to units of log2, with cap and bias
+            const float far = slope * (float)(key0 - r.pos), in = a.softcap > 0.0f ? a.scale * (2.0f * kLog2e / a.softcap) : a.scale * kLog2e;
+            const f32x2 in2 = pack_f32(in, in), slope2 = pack_f32(slope, slope), one2 = pack_f32(1.0f, 1.0f);
+            const float cap = a.softcap * kLog2e;
+            const f32x2 twice2 = pack_f32(-2.0f * cap, -2.0f * cap), cap2 = pack_f32(cap + far, cap + far), far2 = pack_f32(far, far);
 #pragma unroll
-              for (int i = 0; i < 128; ++i) s[i] = capped_log2(s[i], in, out);
-            } else {
-              const float in = a.scale * kLog2e;
-#pragma unroll
-              for (int i = 0; i < 128; ++i) s[i] *= in;
+            for (int i = 0; i < 128; i += 2) {
+              f32x2 x = pack_f32(s[i], s[i + 1]);
+              if (a.softcap > 0.0f) {                        // cap * tanh(x / cap), see capped_log2
+                float e0, e1;
+                unpack_f32(fma_f32x2(x, in2, pack_f32(0.0f, 0.0f)), e0, e1);
+                unpack_f32(add_f32x2(pack_f32(exp2_approx(e0), exp2_approx(e1)), one2), e0, e1);
+                x = fma_f32x2(twice2, pack_f32(rcp_approx(e0), rcp_approx(e1)), cap2);
+              } else {
+                x = fma_f32x2(x, in2, far2);
+              }
+              unpack_f32(fma_f32x2(slope2, pack_f32((float)i, (float)(i + 1)), x), s[i], s[i + 1]);
             }
-            const float far = (float)(key0 - r.pos);
-#pragma unroll
-            for (int i = 0; i < 128; ++i) s[i] = fmaf(slope, far + (float)i, s[i]);
           }
           if (__any_sync(0xffffffffu, key0 < r.lo || key0 + kTileKeys > r.hi)) {
             const int lo = r.lo - key0, hi = r.hi - key0;
@@ -646,9 +651,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
             fine = fine && bar_wait(&sh.kv_full[stage], phase, failed);
             if (!fine) break;
             if (kv && look) {
-              for (int x = lane; x < S::chunks * kTileKeys * 8; x += 32) {
-                const int k = key0 + ((x >> 3) & (kTileKeys - 1));
-                if (k >= z0 && k < z1 && (k < last.lo || k >= first.hi) && not_finite8<T>(*(const uint4 *)(sh.kv[stage] + x * 16))) odd = 1;
+              // two ranges of rows: [z0, last.lo) and [first.hi, z1)
+              const int n0 = max(0, min(z1, last.lo) - z0), from1 = max(z0 + n0, first.hi), rows = n0 + max(0, z1 - from1);
+#pragma unroll 4
+              for (int x = lane; x < rows * 8; x += 32) {
+                const int k = ((x >> 3) < n0 ? z0 + (x >> 3) : from1 + (x >> 3) - n0) - key0;
+#pragma unroll
+                for (int i = 0; i < S::chunks; ++i) odd |= (u32)not_finite8<T>(*(const uint4 *)(sh.kv[stage] + i * (kTileKeys * 128) + k * 128 + (x & 7) * 16));
               }
             }
             __syncwarp();
@@ -666,7 +675,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
     } else {
       // ---------------------------------------------------------------- the parts
       Cursor c = plan.first;
-      u64 left = plan.end - plan.begin;
+      u32 left = plan.end - plan.begin;
       bool more = true;
       for (u32 told = 0; more; ++told) {
         settle<kRows, kTileKeys, kOver>(a, c, left);
@@ -677,17 +686,17 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
           p.r = (int)c.r; p.h = (int)c.h; p.len = c.req.len; p.n = c.req.n; p.q0 = c.req.q0;
           p.row0 = c.m * kRows;
           p.rows = (int)min((i64)kRows, (i64)c.req.n * a.group - p.row0);
-          const int to = (int)min((u64)c.span.tiles, (u64)c.at + left);
+          const int to = (int)min((u32)c.span.tiles, (u32)c.at + left);
           p.tile = c.span.first + c.at;
           p.tiles = to - c.at;
           p.lo = c.span.lo; p.hi = c.span.hi;
           p.whole = c.at == 0 && to == c.span.tiles;
           if (!p.whole) {
-            const u64 unit0 = plan.end - left - (u64)c.at;
+            const u32 unit0 = plan.end - left - (u32)c.at;
             p.i0 = part_owner(plan.total, unit0, plan.parts);
-            p.i1 = part_owner(plan.total, unit0 + (u64)c.span.tiles - 1, plan.parts);
+            p.i1 = part_owner(plan.total, unit0 + (u32)c.span.tiles - 1, plan.parts);
           }
-          left -= (u64)p.tiles;
+          left -= (u32)p.tiles;
           c.at = to;
         }
         if (!bar_wait(&sh.part_empty[slot], ((told / kParts) & 1) ^ 1, failed)) break;

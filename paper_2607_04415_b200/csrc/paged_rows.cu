@@ -7,7 +7,7 @@
 // into a ring of its own (cp.async, three tiles deep, 16 bytes a lane) and keeps its own running
 // maximum, sum and output, so that no barrier stands in the loop.  The warps' four partial results
 // are joined at the end of a unit, in the ring slot that each warp has just used up.
-// Blocks take equal shares of all keys of the call (see make_plan); a unit that is cut between blocks
+// Blocks take equal shares of all keys of the call (the plan); a unit that is cut between blocks
 // leaves parts in the workspace that its last block joins.
 //
 // Scores: s = q.k (16-bit operands, 32-bit sums), then in 32 bits the scale, cap, bias and mask, the running
@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) attention_rows_kernel(
   extern __shared__ __align__(128) unsigned char raw[];
   RowsShared<D> &sh = *(RowsShared<D> *)raw;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const Plan plan = make_plan<kRows, kTile, kOver, kThreads>(a, sh.plan, least);
+  const Plan plan = block_plan<kRows, kTile, kOver, kThreads>(a, sh.plan, least);
   if (plan.begin >= plan.end) return;
 
   constexpr int P = D / 8;                       // 16-byte pieces of a row
@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) attention_rows_kernel(
 
   // --- the loading side: a cursor that runs ahead, and the cache row of the next tile's key that this lane looks up
   Cursor ld = plan.first;
-  u64 ld_left = plan.end - plan.begin;
+  u32 ld_left = plan.end - plan.begin;
   settle<kRows, kTile, kOver>(a, ld, ld_left);
   int key_page = -1, key_in = 0;                 // of key (lane & 15) of the tile at ld; -1: zeros
   auto look_up = [&]() {
@@ -105,10 +105,10 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) attention_rows_kernel(
   Cursor c = plan.first;
   int stage = 0;
   const int g = lane >> 2, t4 = lane & 3;
-  u64 left = plan.end - plan.begin;
+  u32 left = plan.end - plan.begin;
   for (settle<kRows, kTile, kOver>(a, c, left); left; settle<kRows, kTile, kOver>(a, c, left)) {
     const int from = c.at;
-    const int to = (int)min((u64)c.span.tiles, (u64)from + left);
+    const int to = (int)min((u32)c.span.tiles, (u32)from + left);
     const i64 row0 = (i64)c.m * kRows;
     const int rows = (int)min((i64)kRows, (i64)c.req.n * a.group - row0);
     // this lane's two rows: g and g + 8
@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) attention_rows_kernel(
         stage = stage + 1 == kStages ? 0 : stage + 1;
       }
     }
-    left -= (u64)(to - from);
+    left -= (u32)(to - from);
     c.at = to;
 
     // --- join the four warps
@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) attention_rows_kernel(
     }
     __syncthreads();
     const bool whole = from == 0 && to == c.span.tiles;
-    const u64 unit0 = plan.end - left - (u64)to;   // the unit's place on the line
+    const u32 unit0 = plan.end - left - (u32)to;   // the unit's place on the line
     const u32 i0 = whole ? 0 : part_owner(plan.total, unit0, plan.parts);
     const u32 slot = 2 * blockIdx.x + (blockIdx.x == i0 ? 1 : 0);
     for (int x = tid; x < rows * (D / 4); x += kThreads) {
@@ -284,7 +284,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) attention_rows_kernel(
       }
     }
     if (!whole) {
-      const u32 i1 = part_owner(plan.total, unit0 + (u64)c.span.tiles - 1, plan.parts);
+      const u32 i1 = part_owner(plan.total, unit0 + (u32)c.span.tiles - 1, plan.parts);
       __threadfence();
       __syncthreads();
       if (tid == 0) {

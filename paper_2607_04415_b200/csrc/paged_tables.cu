@@ -17,6 +17,16 @@ struct ScanShared {
   u64 fresh[kTabThreads];
 };
 
+__device__ __forceinline__ u64 scan_warp(u64 x) {
+  const u32 lane = threadIdx.x & 31;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const u64 y = __shfl_up_sync(0xffffffffu, x, d);
+    if ((int)lane >= d) x += y;
+  }
+  return x;
+}
+
 // Request r: c cached tokens, n new ones, page size s.  need = ceil((c+n)/s) - ceil(c/s) pages, taken from
 // the top of the stack of free pages in request order; the sums over the requests that this needs are
 // prefix sums, which every block makes for itself over all requests (8 bytes each, out of L2 after the
@@ -25,7 +35,9 @@ struct ScanShared {
 // and a running maximum over the marks tells each token its request.  Each new page has exactly one
 // new token at its start, whose thread writes the table entry, so tables cost no pass of their own.
 // Bound by the latency of four dependent steps (lengths, sums, table entry, stores) for the sizes of a
-// decode step; by the 16 bytes written a token for the largest.
+// decode step.  EACH consecutive requests a thread and round: 1 where one round of a block holds all, as a
+// thread's divisions then take least; 8 beyond, where rounds count.
+template <int EACH>
 __global__ void __launch_bounds__(kTabThreads) page_tables_kernel(const gorio_page_tables_desc a) {
   __shared__ ScanShared sh;
   const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -36,52 +48,51 @@ __global__ void __launch_bounds__(kTabThreads) page_tables_kernel(const gorio_pa
   const i64 fc = fc_in < 0 ? 0 : (u32)fc_in > a.free_capacity ? (i64)a.free_capacity : (i64)fc_in;
   u64 sum_n = 0, sum_need = 0;   // over the rounds before
   u64 top = 0;                   // pages taken by the last served request's end
-  u32 mark = 0;
   sh.req[tid] = -1;
-  __syncthreads();
-  for (u32 round = 0, r0 = 0; r0 < a.n_requests; ++round, r0 += kTabThreads) {
-    const u32 r = r0 + tid;
-    i64 c = 0, n = 0;
-    if (r < a.n_requests) { c = a.lengths[r]; n = a.new_lens[r]; }
-    const i64 brought = n < 0 ? 0 : n > n_tok ? n_tok + 1 : n;     // the sums stay small whatever comes in
-    const bool ok = c >= 0 && n >= 0 && c + n <= (i64)a.table_width * s;      // width * s < 2^31
-    const u64 need = ok ? (u64)((u32)(c + n + s - 1) / s - (u32)(c + s - 1) / s) : 0;
-    u64 x = (u64)brought, y = need;
+  for (u32 round = 0, r0 = 0; r0 < a.n_requests; ++round, r0 += kTabThreads * EACH) {
+    i64 c[EACH], n[EACH];
+    u64 x = 0, y = 0;
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const u64 xs = __shfl_up_sync(0xffffffffu, x, d), ys = __shfl_up_sync(0xffffffffu, y, d);
-      if ((int)lane >= d) { x += xs; y += ys; }
+    for (int k = 0; k < EACH; ++k) {
+      const u32 r = r0 + tid * EACH + k;
+      c[k] = n[k] = 0;
+      if (r < a.n_requests) { c[k] = a.lengths[r]; n[k] = a.new_lens[r]; }
     }
-    if (lane == 31) { sh.n[warp] = x; sh.need[warp] = y; }
-    __syncthreads();
-    u64 wn = sh.n[lane], wy = sh.need[lane];
+    auto brought = [&](int k) { return (u64)(n[k] < 0 ? 0 : n[k] > n_tok ? n_tok + 1 : n[k]); };     // the sums stay small whatever comes in
+    auto fits = [&](int k) { return c[k] >= 0 && n[k] >= 0 && c[k] + n[k] <= (i64)a.table_width * s; };   // width * s < 2^31
+    auto need = [&](int k) { return fits(k) ? (u64)((u32)(c[k] + n[k] + s - 1) / s - (u32)(c[k] + s - 1) / s) : 0; };
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const u64 xs = __shfl_up_sync(0xffffffffu, wn, d), ys = __shfl_up_sync(0xffffffffu, wy, d);
-      if ((int)lane >= d) { wn += xs; wy += ys; }
-    }
-    const u64 all_n = __shfl_sync(0xffffffffu, wn, 31), all_need = __shfl_sync(0xffffffffu, wy, 31);
+    for (int k = 0; k < EACH; ++k) { x += brought(k); y += need(k); }
+    const u64 xw = scan_warp(x), yw = scan_warp(y);
+    if (lane == 31) { sh.n[warp] = xw; sh.need[warp] = yw; }
+    __syncthreads();                                   // also after the marks were cleared
+    const u64 wn = scan_warp(sh.n[lane]), wy = scan_warp(sh.need[lane]);
     const u64 pn = __shfl_sync(0xffffffffu, wn, warp ? warp - 1 : 0), py = __shfl_sync(0xffffffffu, wy, warp ? warp - 1 : 0);
-    x += sum_n + (warp ? pn : 0);          // tokens of requests 0..r
-    y += sum_need + (warp ? py : 0);       // pages of requests 0..r
-    sum_n += all_n;
-    sum_need += all_need;
-    const bool served = ok && y <= (u64)fc && x <= (u64)n_tok && r < a.n_requests;
-    const u64 start = x - (u64)brought;
-    if (served) top = y;
-    if (r < a.n_requests) {
+    u64 upto_n = sum_n + (warp ? pn : 0) + xw - x;     // tokens and pages of the requests before this thread's
+    u64 upto_need = sum_need + (warp ? py : 0) + yw - y;
+    sum_n += __shfl_sync(0xffffffffu, wn, 31);
+    sum_need += __shfl_sync(0xffffffffu, wy, 31);
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+      const u32 r = r0 + tid * EACH + k;
+      if (r >= a.n_requests) break;
+      const u64 start = upto_n, first = upto_need;
+      upto_n += brought(k);
+      upto_need += need(k);
+      const bool served = fits(k) && upto_need <= (u64)fc && upto_n <= (u64)n_tok;
+      if (served) top = upto_need;
       if (round % gridDim.x == blockIdx.x) {
         if (r == 0) a.starts[0] = 0;
-        a.starts[r + 1] = (int)(x > (u64)n_tok ? (u64)n_tok : x);
-        a.out_lengths[r] = (int)(served ? c + n : c);
+        a.starts[r + 1] = (int)(upto_n > (u64)n_tok ? (u64)n_tok : upto_n);
+        a.out_lengths[r] = (int)(served ? c[k] + n[k] : c[k]);
         a.out_served[r] = served ? 1 : 0;
       }
-      if (brought > 0 && (i64)start < base + kTabThreads && (i64)x > base) {
+      if (upto_n > start && (i64)start < base + kTabThreads && (i64)upto_n > base) {
         const u32 at = (i64)start > base ? (u32)((i64)start - base) : 0u;
         sh.req[at] = (int)r;
         sh.served[at] = served;
         sh.start[at] = (u32)start;
-        sh.fresh[at] = y - need;
+        sh.fresh[at] = first;
       }
     }
     __syncthreads();
@@ -90,6 +101,7 @@ __global__ void __launch_bounds__(kTabThreads) page_tables_kernel(const gorio_pa
     // pages taken in all: the served requests' last sum
 #pragma unroll
     for (int d = 16; d; d >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+    __syncthreads();
     if (lane == 0) sh.need[warp] = top;
     __syncthreads();
     if (warp == 0) {
@@ -103,7 +115,7 @@ __global__ void __launch_bounds__(kTabThreads) page_tables_kernel(const gorio_pa
     }
   }
   // the last mark at or before each token
-  mark = sh.req[tid] >= 0 ? tid + 1 : 0;
+  u32 mark = sh.req[tid] >= 0 ? tid + 1 : 0;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
     const u32 y = __shfl_up_sync(0xffffffffu, mark, d);
@@ -111,11 +123,7 @@ __global__ void __launch_bounds__(kTabThreads) page_tables_kernel(const gorio_pa
   }
   if (lane == 31) sh.mark[warp] = mark;
   __syncthreads();
-  {
-    u32 w = lane < warp ? sh.mark[lane] : 0;
-    w = __reduce_max_sync(0xffffffffu, w);
-    mark = max(mark, w);
-  }
+  mark = max(mark, __reduce_max_sync(0xffffffffu, lane < warp ? sh.mark[lane] : 0u));
   const i64 t = base + tid;
   if (t >= n_tok) return;
   i64 slot = -1;
@@ -126,7 +134,7 @@ __global__ void __launch_bounds__(kTabThreads) page_tables_kernel(const gorio_pa
     const int c = a.lengths[req];
     pos = c + (int)((u32)t - sh.start[at]);
     if (sh.served[at]) {
-      const u32 page_at = (u32)pos / s, in_page = (u32)pos - page_at * s, held = (u32)(((u64)(u32)c + s - 1) / s);
+      const u32 page_at = (u32)pos / s, in_page = (u32)pos - page_at * s, held = ((u32)c + s - 1) / s;
       int page;
       if (page_at < held) {
         page = a.tables[(i64)req * a.table_stride + page_at];
@@ -142,61 +150,64 @@ __global__ void __launch_bounds__(kTabThreads) page_tables_kernel(const gorio_pa
   a.requests[t] = req;
 }
 
-// 16 bytes a thread and step: chunk (token, key or value, head, piece of a head) -> its slot.  A copy: each
-// byte is read once and written once.
+// 16 bytes a thread and step, (token, key or value, head, piece of a head) -> its slot: a copy, in which each byte is read once and
+// written once.  A thread keeps its (key or value, head, piece) and goes through four tokens, all their loads in flight
+// at once, so that all divisions but the slot's are made once.
 struct StoreArgs {
   gorio_cache_store_desc d;
   u32 pieces;        // 16-byte pieces of a head
-  u32 per_token;     // heads * pieces
-  u64 chunks;        // n_tokens * 2 * per_token
+  u32 columns;       // 2 * heads * pieces
+  u32 side;          // tokens side by side in a block
 };
 
 constexpr int kStoreThreads = 256;
-constexpr int kStoreEach = 4;          // chunks in flight a thread
+constexpr int kStoreEach = 4;          // tokens a thread
 
 __global__ void __launch_bounds__(kStoreThreads) cache_store_kernel(const StoreArgs a) {
-  const u64 first = (u64)blockIdx.x * (kStoreThreads * kStoreEach) + threadIdx.x;
-  uint4 v[kStoreEach];
-  uint4 *to[kStoreEach];
+  const u32 sub = a.side > 1 ? threadIdx.x / a.columns : 0;
+  if (sub >= a.side) return;
+  const u32 first = blockIdx.x * a.side * kStoreEach + sub;
+  const u32 places = a.d.n_pages * a.d.page_size;
+  for (u32 c = threadIdx.x - sub * a.columns; c < a.columns; c += kStoreThreads) {
+    const u32 half = a.columns / 2, v = c >= half, h = (c - v * half) / a.pieces, piece = c - v * half - h * a.pieces;
+    const u16 *src = (const u16 *)(v ? a.d.values : a.d.keys) + (i64)h * (v ? a.d.v_head_stride : a.d.k_head_stride) + piece * 8;
+    u16 *dst = (u16 *)(v ? a.d.value_pages : a.d.key_pages) + (i64)h * (v ? a.d.vp_head_stride : a.d.kp_head_stride) + piece * 8;
+    const i64 src_t = v ? a.d.v_token_stride : a.d.k_token_stride;
+    const i64 dst_p = v ? a.d.vp_page_stride : a.d.kp_page_stride, dst_t = v ? a.d.vp_token_stride : a.d.kp_token_stride;
+    uint4 x[kStoreEach];
+    i64 slot[kStoreEach];
 #pragma unroll
-  for (int i = 0; i < kStoreEach; ++i) {
-    const u64 x = first + (u64)i * kStoreThreads;
-    to[i] = nullptr;
-    if (x >= a.chunks) continue;
-    const u32 row = (u32)(x / a.per_token), c = (u32)(x - (u64)row * a.per_token);
-    const u32 t = row >> 1, h = c / a.pieces, piece = c - h * a.pieces;
-    const i64 slot = a.d.slots[t];
-    if (slot < 0 || slot >= (i64)a.d.n_pages * a.d.page_size) continue;
-    const u32 page = (u32)slot / a.d.page_size, in_page = (u32)slot - page * a.d.page_size;
-    const u16 *src, *dst;
-    if (row & 1) {
-      src = (const u16 *)a.d.values + (i64)t * a.d.v_token_stride + (i64)h * a.d.v_head_stride;
-      dst = (const u16 *)a.d.value_pages + (i64)page * a.d.vp_page_stride + (i64)h * a.d.vp_head_stride + (i64)in_page * a.d.vp_token_stride;
-    } else {
-      src = (const u16 *)a.d.keys + (i64)t * a.d.k_token_stride + (i64)h * a.d.k_head_stride;
-      dst = (const u16 *)a.d.key_pages + (i64)page * a.d.kp_page_stride + (i64)h * a.d.kp_head_stride + (i64)in_page * a.d.kp_token_stride;
+    for (int i = 0; i < kStoreEach; ++i) {
+      const u32 t = first + i * a.side;
+      slot[i] = -1;
+      if (t < a.d.n_tokens) {
+        slot[i] = a.d.slots[t];
+        x[i] = __ldcs((const uint4 *)(src + (i64)t * src_t));
+      }
     }
-    v[i] = __ldcs((const uint4 *)(src + piece * 8));
-    to[i] = (uint4 *)(dst + piece * 8);
-  }
 #pragma unroll
-  for (int i = 0; i < kStoreEach; ++i)
-    if (to[i]) *to[i] = v[i];
+    for (int i = 0; i < kStoreEach; ++i) {
+      if ((u64)slot[i] >= (u64)places) continue;           // negative ones too
+      const u32 page = (u32)slot[i] / a.d.page_size, in_page = (u32)slot[i] - page * a.d.page_size;
+      *(uint4 *)(dst + (i64)page * dst_p + (i64)in_page * dst_t) = x[i];
+    }
+  }
 }
 
 }  // namespace
 
 cudaError_t launch_page_tables(const gorio_page_tables_desc &d, cudaStream_t s) {
   const u32 blocks = d.n_tokens > 0 ? (d.n_tokens + kTabThreads - 1) / kTabThreads : 1;
-  page_tables_kernel<<<blocks, kTabThreads, 0, s>>>(d);
+  if (d.n_requests <= (u32)kTabThreads) page_tables_kernel<1><<<blocks, kTabThreads, 0, s>>>(d);
+  else page_tables_kernel<8><<<blocks, kTabThreads, 0, s>>>(d);
   return cudaGetLastError();
 }
 
 cudaError_t launch_cache_store(const gorio_cache_store_desc &d, cudaStream_t s) {
-  StoreArgs a{d, d.dim / 8, d.n_heads * (d.dim / 8), 0};
-  a.chunks = (u64)d.n_tokens * 2 * a.per_token;
-  const u64 per_block = kStoreThreads * kStoreEach;
-  cache_store_kernel<<<(u32)((a.chunks + per_block - 1) / per_block), kStoreThreads, 0, s>>>(a);
+  StoreArgs a{d, d.dim / 8, 2 * d.n_heads * (d.dim / 8), 1};
+  if (a.columns < (u32)kStoreThreads) a.side = kStoreThreads / a.columns;
+  const u32 tokens = a.side * kStoreEach;
+  cache_store_kernel<<<(d.n_tokens + tokens - 1) / tokens, kStoreThreads, 0, s>>>(a);
   return cudaGetLastError();
 }
 
