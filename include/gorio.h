@@ -445,6 +445,13 @@ typedef struct {
 } gorio_paged_attention_desc;
 int gorio_paged_attention(const gorio_paged_attention_desc *d, void *cuda_stream);
 
+/*
+ * Whether every call with this workspace went well so far: OK, or TIMEOUT if a wait inside a kernel passed
+ * its limit of 10 s (the kernel then ends, its results are not valid; no such case is known).  Waits for the
+ * stream; makes the workspace ready for use again.
+ */
+int gorio_attention_check(void *workspace, void *cuda_stream);
+
 /* Bytes of the workspace above on CUDA device `cuda_device`; 0 if there is no such device. */
 uint64_t gorio_attention_workspace_bytes(int cuda_device);
 

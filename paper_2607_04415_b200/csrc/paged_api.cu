@@ -80,6 +80,19 @@ extern "C" uint64_t gorio_attention_workspace_bytes(int cuda_device) {
   return sms ? kCounterBytes + part_bytes((u32)sms) : 0;
 }
 
+extern "C" int gorio_attention_check(void *workspace, void *cuda_stream) {
+  if (!workspace) return bad("attention check: null argument");
+  u32 word = 0;
+  const cudaStream_t s = (cudaStream_t)cuda_stream;
+  cudaError_t e = cudaMemcpyAsync(&word, (u32 *)workspace + kErrorWord, sizeof word, cudaMemcpyDeviceToHost, s);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+  if (e != cudaSuccess || word == 0) return launched(e, "attention check");
+  e = cudaMemsetAsync(workspace, 0, kCounterBytes, s);
+  if (e != cudaSuccess) return launched(e, "attention check");
+  gorio::set_global_error("paged attention: a wait inside a kernel lasted longer than 10 s; the results of calls with this workspace are not valid");
+  return GORIO_ERR_TIMEOUT;
+}
+
 extern "C" int gorio_paged_attention(const gorio_paged_attention_desc *d, void *cuda_stream) {
   if (!d) return bad("paged attention: null argument");
   if (d->n_requests == 0 || d->n_tokens == 0) return GORIO_OK;

@@ -35,11 +35,11 @@ constexpr int kRows = 256;
 constexpr int kTileRows = 128;
 constexpr int kTileKeys = 128;
 constexpr int kThreads = 384;
-constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;   // a thread, of 168 * 3 = 208 * 2 + 88 at launch
+constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;   // a thread, of 168 * 3 = 216 * 2 + 72 at launch
 constexpr u32 kScores = 0, kOutputs = 256;           // columns of tensor memory
 constexpr int kParts = 4;                            // parts that have been told and not yet finished
 constexpr int kScans = 8;                            // more parts than the ring of stages lets warp 10 run ahead
-constexpr int kOver = 2;                             // a unit's start and end cost about what two tiles do
+constexpr int kOver = 3;                             // a unit's start and end cost about what three tiles do
 
 template <int D>
 struct Shape {
@@ -126,9 +126,12 @@ __device__ __noinline__ void plain_row(const Attn &a, u32 req, u32 h, const Row 
   }
 }
 
+// the lowest n bits, n cut to [0, 32]
+__device__ __forceinline__ u32 bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+
 // 64 of a row's scores to weights: 2^(x * mul - base), summed unrounded into `sum`, rounded to the cache's type in w.  All
 // exponentials go to the special function units: computing some of them in the multiply-add units (a polynomial, two numbers an
-// instruction) was slower at every share tried, 1/8 to 1/2, as a warp then waits for its own multiply-adds instead.
+// instruction) was slower at every share tried, 1/8 to 1/2, here and in the cap's exponentials.
 template <typename T>
 __device__ __forceinline__ void weights64(const float *s, f32x2 mul, f32x2 minus_base, f32x2 (&sum)[2], u32 *w) {
 #pragma unroll
@@ -227,7 +230,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
               f32x2 x = pack_f32(s[i], s[i + 1]);
               if (a.softcap > 0.0f) {                        // cap * tanh(x / cap), see capped_log2
                 float e0, e1;
-                unpack_f32(fma_f32x2(x, in2, pack_f32(0.0f, 0.0f)), e0, e1);
+                x = fma_f32x2(x, in2, pack_f32(0.0f, 0.0f));
+                unpack_f32(x, e0, e1);
                 unpack_f32(add_f32x2(pack_f32(exp2_approx(e0), exp2_approx(e1)), one2), e0, e1);
                 x = fma_f32x2(twice2, pack_f32(rcp_approx(e0), rcp_approx(e1)), cap2);
               } else {
@@ -239,8 +243,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
           if (__any_sync(0xffffffffu, key0 < r.lo || key0 + kTileKeys > r.hi)) {
             const int lo = r.lo - key0, hi = r.hi - key0;
 #pragma unroll
-            for (int i = 0; i < 128; ++i)
-              if (i < lo || i >= hi) s[i] = -INFINITY;
+            for (int w = 0; w < 4; ++w) {                    // a bit for each of 32 keys
+              const u32 seen = bits_below(hi - 32 * w) & ~bits_below(lo - 32 * w);
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (!(seen & (1u << i))) s[32 * w + i] = -INFINITY;
+            }
           }
           float tops[4] = {s[0], s[1], s[2], s[3]};          // four chains of three-way maxima
 #pragma unroll
@@ -256,7 +264,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
             m = to;
             l *= f;
             if (at > first) {                                // the scores' arrival says that the product before is done
-#pragma unroll
+#pragma unroll 2
               for (int i = 0; i < D / 32; ++i) {
                 float o[32];
                 tmem_ld32(o, outputs + 32 * i);

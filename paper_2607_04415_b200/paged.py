@@ -187,6 +187,20 @@ def attention_workspace(device=None) -> torch.Tensor:
 
 
 @_on_stream
+def attention_check(workspace: Optional[torch.Tensor] = None) -> None:
+    """Raises GorioError if a paged_attention call with this workspace (default: the current stream's) ran into the time
+    limit of a wait inside its kernel (gorio_attention_check).  Waits for the stream."""
+    lib = load_library()
+    if workspace is None:
+        workspace = _WORKSPACES.get((torch.cuda.current_device(), _raw_stream(torch.cuda.current_device())))
+        if workspace is None:
+            return
+    st = _call(lib.gorio_attention_check, workspace.data_ptr(), workspace.device.index)
+    if st:
+        _fail(lib, st)
+
+
+@_on_stream
 def paged_attention(q: torch.Tensor, key_pages: torch.Tensor, value_pages: torch.Tensor, tables: torch.Tensor, lengths: torch.Tensor,
                     starts: torch.Tensor, max_new: int, scale: Optional[float] = None, causal: bool = True, window: int = 0,
                     softcap: float = 0.0, slopes: Optional[torch.Tensor] = None, want_lse: bool = False,

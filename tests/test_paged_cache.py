@@ -336,6 +336,21 @@ def test_attention_max_new_is_a_hint(gorio):
         c.check(gorio, max_new=max_new)
 
 
+def test_attention_check_reports_a_wait_that_ran_out(gorio):
+    c = Case([40, 1], [100, 200])
+    ws = gorio.attention_workspace()
+    c.run(gorio, workspace=ws)
+    gorio.attention_check(ws)
+    gorio.attention_check()
+    ws[(1 << 16) - 4] = 1                                      # what a kernel leaves when a wait passes its limit
+    with pytest.raises(gorio.GorioError) as e:
+        gorio.attention_check(ws)
+    assert e.value.status == 5
+    gorio.attention_check(ws)
+    c.compare(c.run(gorio, workspace=ws))
+    assert (ws[: 1 << 16] == 0).all()
+
+
 def test_attention_into_a_given_tensor(gorio):
     c = Case([5, 1], [300, 200], heads=4, dim=64)
     wide = torch.zeros((6, 4, 72), dtype=BF16, device="cuda")

@@ -81,6 +81,7 @@ def test_c_entries_refuse_bad_numbers(gorio):
     lib = gorio.load_library()
     for e in (lib.gorio_page_tables, lib.gorio_cache_store, lib.gorio_paged_attention):
         assert e(None, None) == 1
+    assert lib.gorio_attention_check(None, None) == 1
     #         12 pointers, row stride; requests, width, capacity, page size, tokens, reserved
     tables = [A] * 12 + [4, 2, 4, 8, 16, 5, 0]
     _refused(lib, lib.gorio_page_tables, p._TABLES, tables,
