@@ -15,6 +15,9 @@ typedef uint32_t u32;
 typedef uint64_t u64;
 typedef int64_t i64;
 
+constexpr u64 kCounterBytes = 64u << 10;   // arrival counters, one a block; zero between calls
+constexpr u32 kErrorWord = (u32)(kCounterBytes / 4) - 1;   // set by a block whose waits ran out
+
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -78,12 +81,16 @@ __device__ __forceinline__ int unit_count(const Attn &a, int n) {
   return (int)(((u32)n * a.group + ROWS - 1) / ROWS);
 }
 
-// The plan.  All tiles of a call, in the order (request, key head, unit, tile), are one line; a unit's tiles are followed
-// by OVER places without work, for what a unit costs besides its tiles (a block with many short units got as many
-// tiles as one with a single long unit, and took twice as long).  Block i of N takes places [total*i/N,
-// total*(i+1)/N).  Every block finds its own from the lengths alone, so no host step and no extra launch stands
-// between the lengths and the work.  A unit that is cut by a block boundary is computed in parts, which the last of
-// its blocks to finish joins in the order of the key axis: results do not depend on which block that is.
+// The plan.  All tiles of a call, in the order (request, key head, unit, tile), are one line that the blocks take equal
+// shares of.  Every block finds its own from the lengths alone, so no host step and no extra launch stands between the
+// lengths and the work.  A unit that is cut by a block boundary is computed in parts, which the last of its blocks to
+// finish joins in the order of the key axis: results do not depend on which block that is.
+// Between units the line has places without work.  Where there are fewer units than blocks, each unit is filled up to
+// whole shares: then no block has pieces of two units, whose starts and ends would come one after the other.  A share
+// then holds at least a multiple of the square root of the longest unit's tiles, which balances the time for a share's tiles
+// against the time to join a unit's parts.  Otherwise a unit's tiles are followed by OVER places, for what a unit costs
+// besides its tiles (a block with many short units got as many tiles as one with a single long unit, and took twice as
+// long).
 struct Cursor {
   u32 r, h;
   int m;           // unit of (r, h)
@@ -93,45 +100,61 @@ struct Cursor {
 };
 
 struct PlanShared {
-  u32 warp_sum[32];
+  u64 warp_tiles[32];
+  u32 warp_sum[32], warp_longest[32];
   u32 found_r, found_before;
 };
 
-// Block i's share of `total` places begins here: the first total % n blocks have one place more than the others.
-__device__ __forceinline__ u32 part_begin(u32 total, u32 i, u32 n) {
-  const u32 each = total / n, more = total - each * n;
-  return each * i + min(i, more);
-}
-// the block that owns place x
-__device__ __forceinline__ u32 part_owner(u32 total, u32 x, u32 n) {
-  const u32 each = total / n, more = total - each * n, first = more * (each + 1);
-  return x < first ? x / (each + 1) : more + (x - first) / each;
-}
+// Shares of places: block i's begins at each * i + min(i, more).
+struct Shares {
+  u32 each, more;
+  __device__ __forceinline__ u32 begin(u32 i) const { return each * i + min(i, more); }
+  __device__ __forceinline__ u32 owner(u32 x) const {              // the block that owns place x
+    const u32 first = more * (each + 1);
+    return x < first ? x / (each + 1) : more + (x - first) / each;
+  }
+};
 
-// Places of request r over all its units (of one key head).  Warp-collective; lane's own request is r
-// (in range where `have`); requests of many units are summed by the whole warp.
+// Places of a unit; fill > 0: whole shares of that many.
+template <int OVER>
+__device__ __forceinline__ u32 unit_places(u32 tiles, u32 fill) { return fill ? (tiles + fill - 1) / fill * fill : tiles + OVER; }
+
+// Places of request r over all its units (of one key head), its units and the most tiles of one.  Warp-collective; lane's own
+// request is r (in range where `have`); requests of many units are summed by the whole warp.  Sums are cut near 2^31,
+// where the plan gives up.
+struct Places {
+  u32 sum, units, longest;
+};
 template <int ROWS, int TK, int OVER>
-__device__ __forceinline__ u32 request_places(const Attn &a, u32 r, bool have) {
+__device__ __forceinline__ Places request_places(const Attn &a, u32 r, bool have, u32 fill) {
   const u32 lane = threadIdx.x & 31;
   Request q{0, 0, 0};
   if (have) q = request_at(a, r);
-  const int units = have ? unit_count<ROWS>(a, q.n) : 0;
-  u32 sum = 0;
-  if (units <= 2) {
-    for (int m = 0; m < units; ++m) sum += (u32)unit_span<ROWS, TK>(a, q.len, q.n, m).tiles + OVER;
+  Places p{0, have ? (u32)unit_count<ROWS>(a, q.n) : 0u, 0};
+  if (p.units <= 4) {
+    for (u32 m = 0; m < p.units; ++m) {
+      const u32 t = (u32)unit_span<ROWS, TK>(a, q.len, q.n, (int)m).tiles;
+      p.sum += unit_places<OVER>(t, fill);
+      p.longest = max(p.longest, t);
+    }
   }
-  u32 big = __ballot_sync(0xffffffffu, units > 2);
+  u32 big = __ballot_sync(0xffffffffu, p.units > 4);
   while (big) {
     const int src = __ffs(big) - 1;
     big &= big - 1;
     const int len = __shfl_sync(0xffffffffu, q.len, src), n = __shfl_sync(0xffffffffu, q.n, src);
-    const int cnt = __shfl_sync(0xffffffffu, units, src);
-    u32 s = 0;
-    for (int m = (int)lane; m < cnt; m += 32) s += (u32)unit_span<ROWS, TK>(a, len, n, m).tiles + OVER;
+    const int cnt = (int)__shfl_sync(0xffffffffu, p.units, src);
+    u32 s = 0, most = 0;
+    for (int m = (int)lane; m < cnt; m += 32) {
+      const u32 t = (u32)unit_span<ROWS, TK>(a, len, n, m).tiles;
+      s = min(s + unit_places<OVER>(t, fill), 1u << 26);
+      most = max(most, t);
+    }
     s = __reduce_add_sync(0xffffffffu, s);
-    if ((int)lane == src) sum = s;
+    most = __reduce_max_sync(0xffffffffu, most);
+    if ((int)lane == src) { p.sum = s; p.longest = most; }
   }
-  return sum;
+  return p;
 }
 
 __device__ __forceinline__ u32 warp_scan(u32 x) {
@@ -144,36 +167,17 @@ __device__ __forceinline__ u32 warp_scan(u32 x) {
   return x;
 }
 
-// Inclusive sum over the block of one value a thread; `all` is the block's sum.  Two barriers.
-template <int NT>
-__device__ __forceinline__ u32 block_scan(u32 v, PlanShared &sh, u32 &all) {
-  const u32 lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const u32 x = warp_scan(v);
-  if (lane == 31) sh.warp_sum[warp] = x;
-  __syncthreads();
-  u32 before = 0;
-  all = 0;
-#pragma unroll
-  for (int w = 0; w < NT / 32; ++w) {
-    const u32 s = sh.warp_sum[w];
-    if (w < (int)warp) before += s;
-    all += s;
-  }
-  __syncthreads();
-  return x + before;
-}
-
 // Sets the cursor to the place `offset` places after the first of request r.  Warp-collective, the same
 // for all warps.
 template <int ROWS, int TK, int OVER>
-__device__ __forceinline__ Cursor cursor_in(const Attn &a, u32 r, u32 offset) {
+__device__ __forceinline__ Cursor cursor_in(const Attn &a, u32 r, u32 offset, u32 fill) {
   const u32 lane = threadIdx.x & 31;
   Cursor c;
   c.r = r;
   c.req = request_at(a, r);
   const int units = unit_count<ROWS>(a, c.req.n);
   u32 per_head = 0;
-  for (int m = (int)lane; m < units; m += 32) per_head += (u32)unit_span<ROWS, TK>(a, c.req.len, c.req.n, m).tiles + OVER;
+  for (int m = (int)lane; m < units; m += 32) per_head += unit_places<OVER>((u32)unit_span<ROWS, TK>(a, c.req.len, c.req.n, m).tiles, fill);
   per_head = __reduce_add_sync(0xffffffffu, per_head);
   c.h = offset / per_head;
   u32 o = offset - c.h * per_head;
@@ -181,7 +185,7 @@ __device__ __forceinline__ Cursor cursor_in(const Attn &a, u32 r, u32 offset) {
   c.at = 0;
   for (int base = 0; base < units; base += 32) {
     const int m = base + (int)lane;
-    const u32 t = m < units ? (u32)unit_span<ROWS, TK>(a, c.req.len, c.req.n, m).tiles + OVER : 0u;
+    const u32 t = m < units ? unit_places<OVER>((u32)unit_span<ROWS, TK>(a, c.req.len, c.req.n, m).tiles, fill) : 0u;
     const u32 x = warp_scan(t);
     const u32 hit = __ballot_sync(0xffffffffu, o < x);
     if (hit) {
@@ -220,9 +224,9 @@ __device__ __forceinline__ bool next_unit(const Attn &a, Cursor &c) {
 // Moves the cursor from a place without work, or past the unit's last tile, to the next tile; `left`: places of the block's
 // share from the cursor on, 0 at its end.
 template <int ROWS, int TK, int OVER>
-__device__ __forceinline__ void settle(const Attn &a, Cursor &c, u32 &left) {
+__device__ __forceinline__ void settle(const Attn &a, Cursor &c, u32 &left, u32 fill) {
   while (left && c.at >= c.span.tiles) {
-    const u32 skip = (u32)(c.span.tiles + OVER - c.at);
+    const u32 skip = unit_places<OVER>((u32)c.span.tiles, fill) - (u32)c.at;
     if (skip >= left) { left = 0; return; }
     left -= skip;
     if (!next_unit<ROWS, TK>(a, c)) left = 0;
@@ -230,44 +234,91 @@ __device__ __forceinline__ void settle(const Attn &a, Cursor &c, u32 &left) {
 }
 
 struct Plan {
-  u32 total, begin, end;   // places; [begin, end) is this block's
-  u32 parts;               // blocks that take part
+  u32 begin, end;          // this block's places; equal: no work
+  u32 fill;                // see unit_places
+  Shares shares;
   Cursor first;
 };
 
-__device__ __forceinline__ bool share(Plan &p, u32 total, u32 least) {
-  p.total = total;
-  p.parts = max(1u, min(gridDim.x, (total + least - 1) / least));
-  p.begin = p.end = 0;
-  if (blockIdx.x >= p.parts || total == 0) return false;
-  p.begin = part_begin(total, blockIdx.x, p.parts);
-  p.end = part_begin(total, blockIdx.x + 1, p.parts);
-  return p.begin < p.end;
-}
-
-// By a block of NT threads; at least `least` places a block, where there are as many.  (One warp alone, without the
-// barriers, took longer even for one request.)
+// By a block of NT threads.  `spread` times the square root of the longest unit: the least share of filled-up units.
+// Requests are dealt out to all warps, each a run of consecutive ones, since a warp takes those of many units one by one.
 template <int ROWS, int TK, int OVER, int NT>
-__device__ __forceinline__ Plan block_plan(const Attn &a, PlanShared &sh, u32 least) {
-  const u32 tid = threadIdx.x;
-  u32 all = 0;
-  for (u32 base = 0; base < a.n_req; base += NT) {
-    u32 sum;
-    block_scan<NT>(request_places<ROWS, TK, OVER>(a, base + tid, base + tid < a.n_req) * a.hkv, sh, sum);
-    all += sum;
-  }
+__device__ __forceinline__ Plan block_plan(const Attn &a, PlanShared &sh, float spread) {
+  constexpr u32 kWarpsHere = NT / 32;
+  const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const u32 run = min(32u, (a.n_req + kWarpsHere - 1) / kWarpsHere), round = run * kWarpsHere;
+  const u32 mine_r = lane < run ? warp * run + lane : a.n_req;       // of the first round
   Plan p;
-  if (!share(p, all, least)) return p;
+  p.begin = p.end = 0;
+  // all tiles and units, the longest unit
+  u64 tiles = 0;
+  u32 units = 0, longest = 0;
+  Places got{0, 0, 0};
+  for (u32 base = 0; base < a.n_req; base += round) {
+    const u32 r = base + mine_r;
+    got = request_places<ROWS, TK, OVER>(a, r, r < a.n_req, 1);
+    tiles += got.sum;
+    units += got.units;
+    longest = max(longest, got.longest);
+  }
+#pragma unroll
+  for (int d = 16; d; d >>= 1) tiles += __shfl_xor_sync(0xffffffffu, tiles, d);
+  units = __reduce_add_sync(0xffffffffu, units);
+  longest = __reduce_max_sync(0xffffffffu, longest);
+  if (lane == 0) { sh.warp_tiles[warp] = tiles; sh.warp_sum[warp] = units; sh.warp_longest[warp] = longest; }
+  if (tid == 0) sh.found_r = a.n_req;
+  __syncthreads();
+  tiles = 0;
+  u64 all_units = 0;
+#pragma unroll
+  for (u32 w = 0; w < kWarpsHere; ++w) { tiles += sh.warp_tiles[w]; all_units += sh.warp_sum[w]; longest = max(longest, sh.warp_longest[w]); }
+  tiles *= a.hkv;
+  all_units *= a.hkv;
+  const u64 line = tiles + all_units * OVER;
+  if (line >= (1ull << 31)) {                            // a call of hours
+    if (tid == 0) a.arrived[kErrorWord] = 2;
+    return p;
+  }
+  if (tiles == 0) return p;
+  const u32 grid = gridDim.x, line_each = ((u32)line + grid - 1) / grid;
+  p.fill = 0;
+  if ((u32)all_units < grid) {
+    const u32 room = grid - (u32)all_units, each = ((u32)tiles + room - 1) / room;      // all units' whole shares fit the grid then
+    if (each <= line_each + 1) p.fill = max(each, (u32)(spread * sqrtf((float)longest)));
+  }
+  if (p.fill) {
+    p.shares.each = p.fill;
+    p.shares.more = 0;
+  } else {
+    const u32 parts = min(grid, (u32)line);
+    p.shares.each = (u32)line / parts;
+    p.shares.more = (u32)line - p.shares.each * parts;
+    if (blockIdx.x >= parts) return p;
+  }
+  const u32 begin = p.shares.begin(blockIdx.x);
   u32 before = 0;
-  for (u32 base = 0; before <= p.begin; base += NT) {
-    u32 sum;
-    const u32 r = base + tid, mine = request_places<ROWS, TK, OVER>(a, r, r < a.n_req) * a.hkv;
-    const u32 upto = before + block_scan<NT>(mine, sh, sum);
-    if (upto - mine <= p.begin && p.begin < upto) { sh.found_r = r; sh.found_before = upto - mine; }
-    before += sum;
+  for (u32 base = 0; base < a.n_req && before <= begin; base += round) {
+    const u32 r = base + mine_r;
+    if (p.fill || a.n_req > round) got = request_places<ROWS, TK, OVER>(a, r, r < a.n_req, p.fill);
+    else got.sum += got.units * OVER;                    // what the one round above has found
+    const u32 mine = got.sum * a.hkv;
+    u32 upto = warp_scan(mine);
+    __syncthreads();                                     // warp_sum has been read
+    if (lane == 31) sh.warp_sum[warp] = upto;
+    __syncthreads();
+    upto += before;
+#pragma unroll
+    for (u32 w = 0; w < kWarpsHere; ++w) {
+      if (w < warp) upto += sh.warp_sum[w];
+      before += sh.warp_sum[w];
+    }
+    if (upto - mine <= begin && begin < upto) { sh.found_r = r; sh.found_before = upto - mine; }
   }
   __syncthreads();
-  p.first = cursor_in<ROWS, TK, OVER>(a, sh.found_r, p.begin - sh.found_before);
+  if (sh.found_r >= a.n_req) return p;                   // filled-up units may leave blocks without any
+  p.begin = begin;
+  p.end = p.fill ? begin + p.fill : p.shares.begin(blockIdx.x + 1);
+  p.first = cursor_in<ROWS, TK, OVER>(a, sh.found_r, begin - sh.found_before, p.fill);
   return p;
 }
 
@@ -276,9 +327,6 @@ constexpr u32 kPartRowsPerSm = 2 * 256;
 constexpr u32 kMaxDim = 128;
 inline u64 part_ml_bytes(u32 sms) { return (u64)sms * kPartRowsPerSm * 2 * sizeof(float); }
 inline u64 part_bytes(u32 sms) { return part_ml_bytes(sms) + (u64)sms * kPartRowsPerSm * kMaxDim * sizeof(float); }
-
-constexpr u64 kCounterBytes = 64u << 10;   // arrival counters, one a block; zero between calls
-constexpr u32 kErrorWord = (u32)(kCounterBytes / 4) - 1;   // set by a block whose waits ran out
 
 // launchers
 // False where no tensor map of the pages can be made (strides or addresses that it does not hold): nothing ran.

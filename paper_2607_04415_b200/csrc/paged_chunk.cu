@@ -40,6 +40,7 @@ constexpr u32 kScores = 0, kOutputs = 256;           // columns of tensor memory
 constexpr int kParts = 4;                            // parts that have been told and not yet finished
 constexpr int kScans = 8;                            // more parts than the ring of stages lets warp 10 run ahead
 constexpr int kOver = 3;                             // a unit's start and end cost about what three tiles do
+constexpr float kSpread = 1.0f;                      // joining a part takes about what a tile does
 
 template <int D>
 struct Shape {
@@ -66,9 +67,11 @@ struct ChunkShared {
   u64 part_full[kParts], part_empty[kParts];
   u64 q_full[2], q_empty[2], s_full[2], p_full[2][2], o_full[2], scanned[kScans], meet;
   u32 odd[kScans];
-  float2 half_ml[kTileRows];
   u32 tmem, failed, last;
-  PlanShared plan;
+  union {
+    PlanShared plan;                 // until the parts begin
+    float2 half_ml[kTileRows];
+  };
 };
 
 // What one row sees.
@@ -166,7 +169,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
     __syncwarp();
     tmem_alloc(&sh.tmem, 512);
   }
-  const Plan plan = block_plan<kRows, kTileKeys, kOver, kThreads>(a, sh.plan, 1);
+  const Plan plan = block_plan<kRows, kTileKeys, kOver, kThreads>(a, sh.plan, kSpread);
   mma_fence_before();
   __syncthreads();
   mma_fence_after();
@@ -188,6 +191,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
     more_registers<kSoftmaxRegs>();
     const int t = warp >> 2, row = tid & (kTileRows - 1);
     constexpr int kCols = D % 64 == 0 ? 64 : 32;             // columns of the output that are worked on at a time
+    constexpr int kAhead = 2;                                // parts of a cut unit that are fetched at a time, 32 columns of each
     const u32 lanes = (u32)(warp & 3) << 21;                 // this warp's 32 lanes of tensor memory
     const u32 scores = tmem + kScores + t * 128 + lanes, outputs = tmem + kOutputs + t * D + lanes;
     u32 s_phase = 0, o_phase = 0, meet_phase = 0;            // o_phase: a bit for each row tile's output
@@ -327,39 +331,44 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
           l = sum;
         }
       }
-      auto output = [&](float *o, int col) {                 // kCols columns of the row's output, not yet divided by l
+      auto output32 = [&](float *o, int col) {               // 32 columns of the row's output, not yet divided by l
+        if (odd) {
+          float x[32], top = m, sum = l;                     // not o itself, which stays in registers
 #pragma unroll
-        for (int i = 0; i < kCols / 32; ++i) {
-          if (!odd) {
-            tmem_ld32(o + 32 * i, outputs + col + 32 * i);
-          } else {
-            float x[32], top = m, sum = l;                   // not o itself, which stays in registers
+          for (int k = 0; k < 32; ++k) x[k] = 0.0f;
+          plain_row<T, D>(a, p.r, p.h, r, k0, k1, col, x, top, sum);
 #pragma unroll
-            for (int k = 0; k < 32; ++k) x[k] = 0.0f;
-            plain_row<T, D>(a, p.r, p.h, r, k0, k1, col + 32 * i, x, top, sum);
-#pragma unroll
-            for (int k = 0; k < 32; ++k) o[32 * i + k] = x[k];
-          }
+          for (int k = 0; k < 32; ++k) o[k] = x[k];
+          return;
         }
+        tmem_ld32(o, outputs + col);
         tmem_wait_ld();
+        keep(o);
+        if (two) {
+          float x[32];
+          tmem_ld32(x, outputs + D + col);
+          tmem_wait_ld();
+          keep(x);
 #pragma unroll
-        for (int i = 0; i < kCols / 32; ++i) keep(o + 32 * i);
-        if (two && !odd) {
-#pragma unroll
-          for (int i = 0; i < kCols / 32; ++i) {
-            float x[32];
-            tmem_ld32(x, outputs + D + col + 32 * i);
-            tmem_wait_ld();
-            keep(x);
-#pragma unroll
-            for (int k = 0; k < 32; ++k) o[32 * i + k] = f0 * o[32 * i + k] + f1 * x[k];
-          }
+          for (int k = 0; k < 32; ++k) o[k] = f0 * o[k] + f1 * x[k];
         }
       };
-      auto write = [&](const float *o, int col, float f) {
+      auto output = [&](float *o, int col) {                 // the same for kCols columns, with one wait where it can be
+        if (odd || two) {
+#pragma unroll
+          for (int k = 0; k < kCols; k += 32) output32(o + k, col + k);
+          return;
+        }
+#pragma unroll
+        for (int k = 0; k < kCols; k += 32) tmem_ld32(o + k, outputs + col + k);
+        tmem_wait_ld();
+#pragma unroll
+        for (int k = 0; k < kCols; k += 32) keep(o + k);
+      };
+      auto write32 = [&](const float *o, int col, float f) {
         uint4 *to = (uint4 *)((u16 *)a.out + r.tok * a.o_t + (i64)r.head * a.o_h + col);
 #pragma unroll
-        for (int k = 0; k < kCols / 8; ++k)
+        for (int k = 0; k < 4; ++k)
           to[k] = make_uint4(pack2<T>(o[8 * k] * f, o[8 * k + 1] * f), pack2<T>(o[8 * k + 2] * f, o[8 * k + 3] * f), pack2<T>(o[8 * k + 4] * f, o[8 * k + 5] * f),
                              pack2<T>(o[8 * k + 6] * f, o[8 * k + 7] * f));
       };
@@ -371,7 +380,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
           for (int col = 0; col < D; col += kCols) {
             float o[kCols];
             output(o, col);
-            if (valid) write(o, col, f);
+#pragma unroll
+            for (int k = 0; k < kCols; k += 32)
+              if (valid) write32(o + k, col + k, f);
           }
         }
       } else {
@@ -419,29 +430,37 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
             const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
             if (valid && a.lse) a.lse[r.tok * a.hq + r.head] = sum == 0.0f ? -INFINITY : top * kLn2 + logf(sum);
 #pragma unroll 1
-            for (int col = 0; col < D; col += kCols) {
-              float acc[kCols];
+            for (int col = 0; col < D; col += 32) {
+              float acc[32];
 #pragma unroll
-              for (int k = 0; k < kCols; ++k) acc[k] = 0.0f;
+              for (int k = 0; k < 32; ++k) acc[k] = 0.0f;
 #pragma unroll 1
-              for (u32 i = p.i0; i <= p.i1; ++i) {
-                float o[kCols], g;
-                if (i == own) {
-                  g = exp2_approx(m - base);
-                  output(o, col);
-                } else {
-                  const float4 *from = (const float4 *)a.part_o + (place(i) * (D / 4) + col / 4) * kRows + unit_row;
+              for (u32 i = p.i0; i <= p.i1; i += kAhead) {
+                float o[kAhead][32], g[kAhead];
 #pragma unroll
-                  for (int k = 0; k < kCols / 4; ++k) {
-                    const float4 x = __ldcg(from + k * kRows);
-                    o[4 * k] = x.x; o[4 * k + 1] = x.y; o[4 * k + 2] = x.z; o[4 * k + 3] = x.w;
+                for (u32 j = 0; j < kAhead; ++j) {
+                  const bool there = i + j <= p.i1 && i + j != own;
+                  const i64 at = place(i + j);
+                  const float4 *from = (const float4 *)a.part_o + (at * (D / 4) + col / 4) * kRows + unit_row;
+                  g[j] = there ? __ldcg(a.part_ml + (at * kRows + unit_row) * 2) : -INFINITY;
+#pragma unroll
+                  for (int k = 0; k < 8; ++k) {
+                    const float4 x = there ? __ldcg(from + k * kRows) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    o[j][4 * k] = x.x; o[j][4 * k + 1] = x.y; o[j][4 * k + 2] = x.z; o[j][4 * k + 3] = x.w;
                   }
-                  g = exp2_approx(__ldcg(a.part_ml + (place(i) * kRows + unit_row) * 2) - base);
                 }
 #pragma unroll
-                for (int k = 0; k < kCols; ++k) acc[k] += g * o[k];
+                for (u32 j = 0; j < kAhead; ++j) {
+                  if (i + j == own) {
+                    g[j] = m;
+                    output32(o[j], col);
+                  }
+                  g[j] = exp2_approx(g[j] - base);
+#pragma unroll
+                  for (int k = 0; k < 32; ++k) acc[k] += g[j] * o[j][k];
+                }
               }
-              if (valid) write(acc, col, f);
+              if (valid) write32(acc, col, f);
             }
           }
         }
@@ -686,7 +705,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
       u32 left = plan.end - plan.begin;
       bool more = true;
       for (u32 told = 0; more; ++told) {
-        settle<kRows, kTileKeys, kOver>(a, c, left);
+        settle<kRows, kTileKeys, kOver>(a, c, left, plan.fill);
         const u32 slot = told % kParts;
         PartInfo p{};
         more = left != 0;
@@ -701,8 +720,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
           p.whole = c.at == 0 && to == c.span.tiles;
           if (!p.whole) {
             const u32 unit0 = plan.end - left - (u32)c.at;
-            p.i0 = part_owner(plan.total, unit0, plan.parts);
-            p.i1 = part_owner(plan.total, unit0 + (u32)c.span.tiles - 1, plan.parts);
+            p.i0 = plan.shares.owner(unit0);
+            p.i1 = plan.shares.owner(unit0 + (u32)c.span.tiles - 1);
           }
           left -= (u32)p.tiles;
           c.at = to;

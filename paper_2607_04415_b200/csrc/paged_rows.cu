@@ -28,6 +28,7 @@ constexpr int kWarpKeys = 16;
 constexpr int kTile = kWarps * kWarpKeys;
 constexpr int kStages = 3;
 constexpr int kOver = 1;            // a unit's start and end cost about what a tile does
+constexpr float kSpread = 0.25f;    // joining 16 parts takes about what a tile does
 constexpr int kBlocksPerSm = 2;
 
 template <int D>
@@ -50,11 +51,11 @@ __device__ __forceinline__ int piece_at(int row, int piece) {
 }
 
 template <typename T, int D, bool SCORED>
-__global__ void __launch_bounds__(kThreads, kBlocksPerSm) attention_rows_kernel(const Attn a, const u32 least) {
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm) attention_rows_kernel(const Attn a) {
   extern __shared__ __align__(128) unsigned char raw[];
   RowsShared<D> &sh = *(RowsShared<D> *)raw;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const Plan plan = block_plan<kRows, kTile, kOver, kThreads>(a, sh.plan, least);
+  const Plan plan = block_plan<kRows, kTile, kOver, kThreads>(a, sh.plan, kSpread);
   if (plan.begin >= plan.end) return;
 
   constexpr int P = D / 8;                       // 16-byte pieces of a row
@@ -64,7 +65,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) attention_rows_kernel(
   // --- the loading side: a cursor that runs ahead, and the cache row of the next tile's key that this lane looks up
   Cursor ld = plan.first;
   u32 ld_left = plan.end - plan.begin;
-  settle<kRows, kTile, kOver>(a, ld, ld_left);
+  settle<kRows, kTile, kOver>(a, ld, ld_left, plan.fill);
   int key_page = -1, key_in = 0;                 // of key (lane & 15) of the tile at ld; -1: zeros
   auto look_up = [&]() {
     if (ld_left == 0) return;
@@ -92,7 +93,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) attention_rows_kernel(
       }
       --ld_left;
       ++ld.at;
-      settle<kRows, kTile, kOver>(a, ld, ld_left);
+      settle<kRows, kTile, kOver>(a, ld, ld_left, plan.fill);
       look_up();
     }
     cp_async_commit();
@@ -106,7 +107,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) attention_rows_kernel(
   int stage = 0;
   const int g = lane >> 2, t4 = lane & 3;
   u32 left = plan.end - plan.begin;
-  for (settle<kRows, kTile, kOver>(a, c, left); left; settle<kRows, kTile, kOver>(a, c, left)) {
+  for (settle<kRows, kTile, kOver>(a, c, left, plan.fill); left; settle<kRows, kTile, kOver>(a, c, left, plan.fill)) {
     const int from = c.at;
     const int to = (int)min((u32)c.span.tiles, (u32)from + left);
     const i64 row0 = (i64)c.m * kRows;
@@ -259,7 +260,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) attention_rows_kernel(
     __syncthreads();
     const bool whole = from == 0 && to == c.span.tiles;
     const u32 unit0 = plan.end - left - (u32)to;   // the unit's place on the line
-    const u32 i0 = whole ? 0 : part_owner(plan.total, unit0, plan.parts);
+    const u32 i0 = whole ? 0 : plan.shares.owner(unit0);
     const u32 slot = 2 * blockIdx.x + (blockIdx.x == i0 ? 1 : 0);
     for (int x = tid; x < rows * (D / 4); x += kThreads) {
       const int row = x / (D / 4), col = (x - row * (D / 4)) * 4;
@@ -284,7 +285,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) attention_rows_kernel(
       }
     }
     if (!whole) {
-      const u32 i1 = part_owner(plan.total, unit0 + (u32)c.span.tiles - 1, plan.parts);
+      const u32 i1 = plan.shares.owner(unit0 + (u32)c.span.tiles - 1);
       __threadfence();
       __syncthreads();
       if (tid == 0) {
@@ -314,7 +315,7 @@ cudaError_t launch(const Attn &a, u32 sms, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     ready[dev] = true;
   }
-  attention_rows_kernel<T, D, SCORED><<<sms * kBlocksPerSm, kThreads, sizeof(RowsShared<D>), s>>>(a, 1u);
+  attention_rows_kernel<T, D, SCORED><<<sms * kBlocksPerSm, kThreads, sizeof(RowsShared<D>), s>>>(a);
   return cudaGetLastError();
 }
 

@@ -272,6 +272,9 @@ def test_attention_long_cache_in_parts(gorio):
     """One request over a long cache is cut between all blocks; more requests than threads of a block."""
     Case([1], [40000], dim=128, heads=8, kv_heads=2, page=64).check(gorio)
     Case([1, 1], [9000, 3], dim=64, heads=5, kv_heads=1).check(gorio)
+    Case([60], [20000], dim=64, heads=8, kv_heads=1, page=64).check(gorio)            # units of both sizes, cut often
+    Case([20], [9000], dim=128, heads=6, kv_heads=1).check(gorio)
+    Case([300, 40, 7], [4000, 900, 2500], dim=96, heads=4, kv_heads=2).check(gorio)
     rng = random.Random(5)
     Case([1] * 1500, [rng.randint(0, 40) for _ in range(1500)], dim=64, heads=2, kv_heads=1).check(gorio)
     Case([rng.randint(0, 3) for _ in range(700)], [rng.randint(0, 90) for _ in range(700)], dim=64, heads=2, kv_heads=1).check(gorio)
