@@ -29,7 +29,10 @@ constexpr int kTile = kWarps * kWarpKeys;
 constexpr int kStages = 3;
 constexpr int kOver = 1;            // a unit's start and end cost about what a tile does
 constexpr float kSpread = 0.25f;    // joining 16 parts takes about what a tile does
-constexpr int kBlocksPerSm = 2;
+// As many as shared memory (24 KB a warp at head size 128) and registers hold: at head size 64, 64 ragged single-token requests take
+// 96 us with four blocks, 101 with three, 122 with two; more stages instead did nothing.
+template <int D>
+constexpr int kBlocksPerSm = D == 64 ? 4 : D == 96 ? 3 : 2;
 
 template <int D>
 struct RowsShared {
@@ -51,7 +54,7 @@ __device__ __forceinline__ int piece_at(int row, int piece) {
 }
 
 template <typename T, int D, bool SCORED>
-__global__ void __launch_bounds__(kThreads, kBlocksPerSm) attention_rows_kernel(const Attn a) {
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm<D>) attention_rows_kernel(const Attn a) {
   extern __shared__ __align__(128) unsigned char raw[];
   RowsShared<D> &sh = *(RowsShared<D> *)raw;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -333,7 +336,7 @@ cudaError_t launch(const Attn &a, u32 sms, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     ready[dev] = true;
   }
-  attention_rows_kernel<T, D, SCORED><<<sms * kBlocksPerSm, kThreads, sizeof(RowsShared<D>), s>>>(a);
+  attention_rows_kernel<T, D, SCORED><<<sms * kBlocksPerSm<D>, kThreads, sizeof(RowsShared<D>), s>>>(a);
   return cudaGetLastError();
 }
 
