@@ -389,3 +389,16 @@ def test_tables_store_and_attention_together(gorio):
     out, _, tol, _ = plain_attention(q, torch.cat([dense_k, pad], 2), torch.cat([kv_new[:, 1].transpose(0, 1).reshape(1, kv, total, dim), pad], 2),
                                      _i32([[0]]), _i32([total]), _i32([0, total]))
     assert ((whole.double() - out).abs() <= tol).all() and ((pieces.double() - out).abs() <= tol).all()
+
+
+def test_example_from_a_search_to_attention(gorio):
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "retrieve_and_attend.py")
+    spec = importlib.util.spec_from_file_location("retrieve_and_attend", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    r = example.main(questions=9, steps=2, heads=8, kv_heads=2)
+    assert r["served"].tolist() == [1] * 9
+    out, lse, out_tol, lse_tol = plain_attention(r["q"], r["key_pages"], r["value_pages"], r["tables"], r["lengths"], r["starts"])
+    assert ((r["out"].double() - out).abs() <= out_tol).all() and ((r["lse"].double() - lse).abs() <= lse_tol).all()
