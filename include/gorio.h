@@ -419,7 +419,8 @@ int gorio_cache_store(const gorio_cache_store_desc *d, void *cuda_stream);
  *   if slopes: x_j += slopes[h] * (j - p);   out = sum_j softmax(x)_j v_j;   lse = log sum_j exp(x_j).
  * A query that sees no key gets out = 0 and lse = -inf.  Sums, maxima and the softmax are held in 32
  * bits; the weights are rounded to the cache's type for the sum over values, and out once at the end.
- * Keys and values that no query of the request sees are not read into any result, whatever they hold.
+ * What a query does not see has no effect on its result, whatever it holds (NaN included).  Rows of q that
+ * belong to no request are not read and their results not written.
  *   q, out        [n_tokens][n_heads][dim]; key_pages, value_pages [n_pages][n_kv_heads][page_size][dim],
  *                 in any order of the outer axes (strides); lse f32 [n_tokens][n_heads] or NULL.
  *   tables        i32 [n_requests] rows of table_width entries, table_stride apart.
@@ -428,7 +429,8 @@ int gorio_cache_store(const gorio_cache_store_desc *d, void *cuda_stream);
  *                 its first use.  Each call leaves them zero; calls that may overlap need one each.
  * Preconditions: dtype one of GORIO_KV_*, dim 64, 96 or 128, n_heads a multiple of n_kv_heads, every
  * stride a multiple of 8 and pointer 16-byte aligned, scale > 0 and finite, softcap >= 0 and finite,
- * page_size a multiple of 8, table_width * page_size < 2^31, n_requests <= 2^20.
+ * page_size a multiple of 8, table_width * page_size, n_pages * page_size and n_tokens * n_heads < 2^31,
+ * n_requests <= 2^20.
  */
 typedef struct {
   const void *q, *key_pages, *value_pages;
@@ -446,9 +448,10 @@ typedef struct {
 int gorio_paged_attention(const gorio_paged_attention_desc *d, void *cuda_stream);
 
 /*
- * Whether every call with this workspace went well so far: OK, or TIMEOUT if a wait inside a kernel passed
- * its limit of 10 s (the kernel then ends, its results are not valid; no such case is known).  Waits for the
- * stream; makes the workspace ready for use again.
+ * Whether every call with this workspace went well so far: OK; TIMEOUT if a wait inside a kernel passed its
+ * limit of 10 s (the kernel then ends, its results are not valid; no such case is known); CAPACITY if a call had 2^31
+ * or more tiles of keys, hours of work, and was not computed.  Waits for the stream; makes the workspace
+ * ready for use again.
  */
 int gorio_attention_check(void *workspace, void *cuda_stream);
 

@@ -89,6 +89,10 @@ extern "C" int gorio_attention_check(void *workspace, void *cuda_stream) {
   if (e != cudaSuccess || word == 0) return launched(e, "attention check");
   e = cudaMemsetAsync(workspace, 0, kCounterBytes, s);
   if (e != cudaSuccess) return launched(e, "attention check");
+  if (word == 2) {
+    gorio::set_global_error("paged attention: a call had 2^31 or more tiles of keys and was not computed");
+    return GORIO_ERR_CAPACITY;
+  }
   gorio::set_global_error("paged attention: a wait inside a kernel lasted longer than 10 s; the results of calls with this workspace are not valid");
   return GORIO_ERR_TIMEOUT;
 }

@@ -120,8 +120,8 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<D>) attention_rows_kern
     cp_async_commit();
   };
   look_up();
-#pragma unroll
-  for (int s = 0; s < kStages; ++s) issue(s);
+#pragma unroll 1
+  for (int s = 0; s < kStages - 1; ++s) issue(s);
 
   // --- the computing side
   Cursor c = plan.first;
@@ -162,6 +162,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<D>) attention_rows_kern
       for (int x = 0; x < 4; ++x) o[n][x] = 0.0f;
 
     for (int at = from; at < to; ++at) {
+      issue(stage == 0 ? kStages - 1 : stage - 1);          // the slot that the tile before has left
       cp_async_wait<kStages - 1>();
       __syncwarp();
       const u16 *ks = sh.ring[warp][stage][0], *vs = sh.ring[warp][stage][1];
@@ -257,10 +258,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<D>) attention_rows_kern
         }
       }
       __syncwarp();
-      if (at + 1 < to) {                          // at the unit's end the slot is needed below first
-        issue(stage);
-        stage = stage + 1 == kStages ? 0 : stage + 1;
-      }
+      if (at + 1 < to) stage = stage + 1 == kStages ? 0 : stage + 1;     // at the unit's end the slot is needed below
     }
     left -= (u32)(to - from);
     c.at = to;
@@ -319,7 +317,6 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<D>) attention_rows_kern
       if (sh.last) join_parts<T, D, kRows, kThreads, 1, 8>(a, c, row0, rows, i0, i1);
     }
     __syncthreads();
-    issue(stage);
     stage = stage + 1 == kStages ? 0 : stage + 1;
   }
   cp_async_wait<0>();

@@ -280,6 +280,35 @@ def test_attention_long_cache_in_parts(gorio):
     Case([rng.randint(0, 3) for _ in range(700)], [rng.randint(0, 90) for _ in range(700)], dim=64, heads=2, kv_heads=1).check(gorio)
 
 
+def test_attention_of_many_requests_with_chunks(gorio):
+    """More requests than threads of a block, most of them of more rows than the single-token form takes."""
+    rng = random.Random(6)
+    Case([rng.randint(0, 20) for _ in range(500)], [rng.randint(0, 150) for _ in range(500)], dim=64, heads=2, kv_heads=1, page=8).check(gorio)
+    Case([3] * 40 + [200], [200] * 41, dim=128, heads=8, kv_heads=1, causal=False).check(gorio)
+
+
+@pytest.mark.parametrize("new", [1, 50])
+def test_attention_scale(gorio, new):
+    c = Case([new], [300], dim=64, heads=4, kv_heads=2)
+    got = c.run(gorio, scale=0.03)
+    out, lse, out_tol, lse_tol = plain_attention(c.q, c.kp, c.vp, c.tables, c.lengths, c.starts, scale=0.03)
+    assert ((got["out"].double() - out).abs() <= out_tol).all() and ((got["lse"].double() - lse).abs() <= lse_tol).all()
+    with pytest.raises(gorio.GorioError):
+        c.run(gorio, scale=0.0)
+    with pytest.raises(gorio.GorioError):
+        c.run(gorio, window=-1)
+    with pytest.raises(gorio.GorioError):
+        gorio.paged_attention(c.q[:, :3], c.kp, c.vp, c.tables, c.lengths, c.starts, new)
+    with pytest.raises(gorio.GorioError):
+        gorio.paged_attention(c.q, c.kp, c.vp.half(), c.tables, c.lengths, c.starts, new)
+    with pytest.raises(gorio.GorioError):
+        gorio.paged_attention(c.q, c.kp, c.vp, c.tables, c.lengths, c.starts[:1], new)
+    with pytest.raises(gorio.GorioError):
+        gorio.paged_attention(c.q, c.kp, c.vp, c.tables, c.lengths, c.starts, new, workspace=torch.zeros(100, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(gorio.GorioError):
+        gorio.cache_store(c.q, c.q, c.kp, c.vp, torch.zeros(c.q.shape[0], dtype=torch.int64, device="cuda"))
+
+
 def test_attention_offsets_past_32_bits(gorio):
     """The pages in use lie behind the 2^31st element (and the 2^32nd byte) of the cache."""
     spare = (1 << 31) // (2 * 64 * 128) + 8
