@@ -139,8 +139,11 @@ extern "C" int gorio_paged_attention(const gorio_paged_attention_desc *d, void *
   a.arrived = (u32 *)d->workspace;
   a.part_ml = (float *)((char *)d->workspace + kCounterBytes);
   a.part_o = (float *)((char *)a.part_ml + part_ml_bytes((u32)sms));
-  // Up to 16 rows share a key head in a request: the rows kernel, which is bound by the cache's bytes.  More: the chunk kernel.
-  if ((uint64_t)d->max_new * a.group > 16) {
+  // Up to 16 rows share a key head in a request: the rows kernel, which is bound by the cache's bytes.  More: the chunk
+  // kernel, unless the rows kernel has at most 48 units of 16 rows to do in all, when its shorter start counts for more
+  // than its reading keys once for every 16 rows (8 key heads of 128: 64 rows each over 1000 keys 15 us against 22 in the
+  // chunk kernel, 96 rows over 8000 keys 37 against 39; in 8 requests 48 rows each over 8000 keys 114 against 77).
+  if ((uint64_t)d->max_new * a.group > 16 && (uint64_t)d->n_tokens * d->n_heads > 48 * 16) {
     cudaError_t e = cudaSuccess;
     if (launch_chunk(a, (int)d->dtype, (int)d->dim, (u32)sms, (cudaStream_t)cuda_stream, &e)) return launched(e, "paged attention");
   }

@@ -144,7 +144,7 @@ def test_cache_store(gorio, dtype, tokens, heads, dim, page, layout):
 class Case:
     """A cache with the given requests in scattered pages; whatever no query sees is NaN."""
 
-    def __init__(self, new, lens, heads=4, kv_heads=2, dim=64, page=16, dtype=BF16, seed=0, layout="heads", causal=True, window=0, softcap=0.0,
+    def __init__(self, new, lens, heads=8, kv_heads=4, dim=64, page=16, dtype=BF16, seed=0, layout="heads", causal=True, window=0, softcap=0.0,
                  slopes=False, spare=0, sharp=2.0, freed=False):
         g = torch.Generator(device="cuda").manual_seed(seed)
         width = max(1, max(ceil_div(n, page) for n in lens)) + 1
@@ -210,7 +210,7 @@ def test_attention_types_and_lengths(gorio, dtype, dim, new, lens):
 
 
 @pytest.mark.parametrize("heads,kv_heads", [(1, 1), (8, 1), (3, 3), (10, 2), (14, 2), (32, 2), (40, 1), (9, 3)])
-@pytest.mark.parametrize("new", [1, 3, 70])
+@pytest.mark.parametrize("new", [1, 3, 70, 900])
 def test_attention_head_layouts(gorio, heads, kv_heads, new):
     Case([new, 1], [max(new, 211), 90], heads=heads, kv_heads=kv_heads, dim=128, seed=heads).check(gorio)
 
@@ -241,19 +241,19 @@ def test_attention_rows_without_keys(gorio):
     Case([1, 0, 1], [40, 30, 20]).check(gorio)
     Case([0, 0, 70], [40, 30, 100]).check(gorio)
     c = Case([0, 0], [4, 5])
-    assert c.run(gorio)["out"].shape == (0, 4, 64)
+    assert c.run(gorio)["out"].shape == (0, 8, 64)
 
 
 @pytest.mark.parametrize("new", [[4], [1], [150]])
 @pytest.mark.parametrize("bad", [math.inf, math.nan])
 def test_attention_values_that_are_not_finite_reach_only_who_sees_them(gorio, new, bad):
-    c = Case(new, [200], dim=64, heads=2, kv_heads=1)
+    c = Case(new, [200], dim=64, heads=8, kv_heads=2)
     page = c.tables[0, 198 // 16].item()
     c.vp[page, :, 198 % 16, 3] = bad                           # all but the last two tokens' queries do not see it
     got = c.check(gorio)
     assert torch.isfinite(got["out"][: max(0, new[0] - 2)]).all()
     assert not torch.isfinite(got["out"][-1, :, 3]).any() and torch.isfinite(got["out"][-1, :, 4]).all()
-    c = Case(new, [200], dim=64, heads=2, kv_heads=1)
+    c = Case(new, [200], dim=64, heads=8, kv_heads=2)
     c.kp[page, :, 198 % 16, 3] = math.nan                      # a score that is not a number
     got = c.run(gorio)
     assert torch.isfinite(got["out"][: max(0, new[0] - 2)]).all() and torch.isnan(got["out"][-1]).all()
@@ -262,8 +262,8 @@ def test_attention_values_that_are_not_finite_reach_only_who_sees_them(gorio, ne
 @pytest.mark.parametrize("new", [1, 100])
 def test_attention_extreme_scores(gorio, new):
     # weights that all but vanish beside one key's, and scores far from 0
-    Case([new], [500], sharp=60.0, dim=128, heads=4, kv_heads=1).check(gorio)
-    c = Case([new], [500], dim=128, heads=4, kv_heads=1)
+    Case([new], [500], sharp=60.0, dim=128, heads=16, kv_heads=4).check(gorio)
+    c = Case([new], [500], dim=128, heads=16, kv_heads=4)
     c.q.zero_()                                                # even weights: the mean of the values
     c.check(gorio)
 
@@ -272,8 +272,10 @@ def test_attention_long_cache_in_parts(gorio):
     """One request over a long cache is cut between all blocks; more requests than threads of a block."""
     Case([1], [40000], dim=128, heads=8, kv_heads=2, page=64).check(gorio)
     Case([1, 1], [9000, 3], dim=64, heads=5, kv_heads=1).check(gorio)
-    Case([60], [20000], dim=64, heads=8, kv_heads=1, page=64).check(gorio)            # units of both sizes, cut often
-    Case([20], [9000], dim=128, heads=6, kv_heads=1).check(gorio)
+    Case([60], [20000], dim=64, heads=8, kv_heads=1, page=64).check(gorio)
+    Case([150], [20000], dim=64, heads=8, kv_heads=1, page=64).check(gorio)           # units of both sizes, cut often
+    Case([150], [9000], dim=128, heads=6, kv_heads=1).check(gorio)
+    Case([30] * 7, [9000, 100, 300, 5, 2000, 700, 30], dim=128, heads=6, kv_heads=2).check(gorio)
     Case([300, 40, 7], [4000, 900, 2500], dim=96, heads=4, kv_heads=2).check(gorio)
     rng = random.Random(5)
     Case([1] * 1500, [rng.randint(0, 40) for _ in range(1500)], dim=64, heads=2, kv_heads=1).check(gorio)
@@ -287,7 +289,7 @@ def test_attention_of_many_requests_with_chunks(gorio):
     Case([3] * 40 + [200], [200] * 41, dim=128, heads=8, kv_heads=1, causal=False).check(gorio)
 
 
-@pytest.mark.parametrize("new", [1, 50])
+@pytest.mark.parametrize("new", [1, 50, 250])
 def test_attention_scale(gorio, new):
     c = Case([new], [300], dim=64, heads=4, kv_heads=2)
     got = c.run(gorio, scale=0.03)
@@ -312,13 +314,14 @@ def test_attention_scale(gorio, new):
 def test_attention_offsets_past_32_bits(gorio):
     """The pages in use lie behind the 2^31st element (and the 2^32nd byte) of the cache."""
     spare = (1 << 31) // (2 * 64 * 128) + 8
-    for new in (1, 60):
+    for new in (1, 250):
         Case([new, 1], [500, 300], dim=128, heads=4, kv_heads=2, page=64, spare=spare).check(gorio)
         torch.cuda.empty_cache()
 
 
-def test_attention_table_entries_outside_the_cache_read_as_zeros(gorio):
-    c = Case([1, 40], [100, 200])
+@pytest.mark.parametrize("new", [40, 140])
+def test_attention_table_entries_outside_the_cache_read_as_zeros(gorio, new):
+    c = Case([1, new], [100, 200])
     want = None
     for bad in (-1, 1 << 30):
         c.tables[0, 2] = bad
@@ -337,8 +340,9 @@ def test_attention_table_entries_outside_the_cache_read_as_zeros(gorio):
     torch.cuda.synchronize()
 
 
-def test_attention_does_not_change_between_calls_streams_and_graphs(gorio):
-    c = Case([1, 30, 1], [5000, 900, 77], dim=128, heads=8, kv_heads=2)
+@pytest.mark.parametrize("new", [30, 130])
+def test_attention_does_not_change_between_calls_streams_and_graphs(gorio, new):
+    c = Case([1, new, 1], [5000, 900, 77], dim=128, heads=8, kv_heads=2)
     first = c.run(gorio)
     for _ in range(3):
         again = c.run(gorio)
@@ -363,13 +367,13 @@ def test_attention_does_not_change_between_calls_streams_and_graphs(gorio):
 
 
 def test_attention_max_new_is_a_hint(gorio):
-    c = Case([1, 30], [300, 200], dim=128)
-    for max_new in (0, 1, 30, 5000):
+    c = Case([1, 130], [300, 200], dim=128)
+    for max_new in (0, 1, 130, 5000):
         c.check(gorio, max_new=max_new)
 
 
 def test_attention_check_reports_a_wait_that_ran_out(gorio):
-    c = Case([40, 1], [100, 200])
+    c = Case([140, 1], [160, 200])
     ws = gorio.attention_workspace()
     c.run(gorio, workspace=ws)
     gorio.attention_check(ws)
