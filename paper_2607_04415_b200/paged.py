@@ -7,7 +7,6 @@ not wait for the GPU and may be captured into a CUDA graph.  A tensor last used 
 ready for this one by the caller, as for any torch operation."""
 from __future__ import annotations
 
-import functools
 import math
 import struct
 from typing import Optional
@@ -30,54 +29,60 @@ def _fail(lib, status):
     raise GorioError(status, lib.gorio_last_error(None).decode())
 
 
-def _vector(name, t, device, length=None, dtype=torch.int32):
+def _vector(name, t, index, length=None, dtype=torch.int32):
     if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.dim() != 1 or not t.is_contiguous():
         raise _invalid(f"{name} must be a contiguous 1-D {dtype} tensor")
-    if t.device != device:
-        raise _invalid(f"{name} must live on {device}")
+    if t.get_device() != index:
+        raise _invalid(f"{name} must live on cuda:{index}")
     if length is not None and t.shape[0] != length:
         raise _invalid(f"{name} has {t.shape[0]} elements, expected {length}")
 
 
-def _tables_2d(tables, rows, device):
+def _tables_2d(tables, rows, index):
     if not isinstance(tables, torch.Tensor) or tables.dtype is not torch.int32 or tables.dim() != 2:
         raise _invalid("tables must be a 2-D int32 tensor [requests, pages]")
-    if tables.device != device:
-        raise _invalid(f"tables must live on {device}")
-    if tables.shape[0] != rows:
-        raise _invalid(f"tables have {tables.shape[0]} rows, expected {rows}")
-    if tables.shape[1] < 1 or (tables.shape[1] > 1 and tables.stride(1) != 1):
+    if tables.get_device() != index:
+        raise _invalid(f"tables must live on cuda:{index}")
+    b, width = tables.shape
+    if b != rows:
+        raise _invalid(f"tables have {b} rows, expected {rows}")
+    row, one = tables.stride()
+    if width < 1 or (width > 1 and one != 1):
         raise _invalid("tables need at least one page and contiguous rows")
+    return width, row
 
 
-def _page_pair(key_pages, value_pages, device):
-    """Shapes of the two page tensors [pages, heads, page size, head size]; returns their strides."""
+def _page_pair(key_pages, value_pages, index):
+    """Checks the two page tensors [pages, heads, page size, head size]; returns their shape and strides."""
     for name, t in (("key_pages", key_pages), ("value_pages", value_pages)):
         if not isinstance(t, torch.Tensor) or t.dim() != 4 or t.dtype not in _DTYPES:
             raise _invalid(f"{name} must be a 4-D bfloat16 or float16 tensor [pages, heads, page size, head size]")
-        if t.device != device:
-            raise _invalid(f"{name} must live on {device}")
-    if key_pages.shape != value_pages.shape or key_pages.dtype is not value_pages.dtype:
+        if t.get_device() != index:
+            raise _invalid(f"{name} must live on cuda:{index}")
+    shape = key_pages.shape
+    if shape != value_pages.shape or key_pages.dtype is not value_pages.dtype:
         raise _invalid("key_pages and value_pages differ in shape or type")
     ks, vs = key_pages.stride(), value_pages.stride()
     if ks[3] != 1 or vs[3] != 1:
         raise _invalid("the elements of a head must be contiguous in the pages")
-    return ks, vs
+    return shape, ks, vs
 
 
-def _rows_3d(name, t, device, dtype):
+def _rows_3d(name, t, index, dtype):
     if not isinstance(t, torch.Tensor) or t.dim() != 3 or t.dtype is not dtype:
         raise _invalid(f"{name} must be a 3-D {dtype} tensor [tokens, heads, head size]")
-    if t.device != device:
-        raise _invalid(f"{name} must live on {device}")
-    if t.stride(2) != 1:
+    if t.get_device() != index:
+        raise _invalid(f"{name} must live on cuda:{index}")
+    strides = t.stride()
+    if strides[2] != 1:
         raise _invalid(f"the elements of a head must be contiguous in {name}")
+    return strides
 
 
-def _cuda_device(name, t):
+def _cuda_index(name, t):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise _invalid(f"{name} must be a CUDA tensor")
-    return t.device
+    return t.get_device()
 
 
 def _call(entry, desc, device_index):
@@ -93,20 +98,8 @@ def _call(entry, desc, device_index):
         torch._C._cuda_setDevice(was)
 
 
-def _on_stream(f):
-    """A `stream` argument for f, which runs on the current stream: results are then allocated there too."""
-    @functools.wraps(f)
-    def g(*args, stream=None, **more):
-        if stream is None:
-            return f(*args, **more)
-        with torch.cuda.stream(stream):
-            return f(*args, **more)
-    return g
-
-
-@_on_stream
 def page_tables(lengths: torch.Tensor, new_lens: torch.Tensor, tables: torch.Tensor, free_pages: torch.Tensor,
-                free_count: torch.Tensor, page_size: int, n_tokens: int) -> dict:
+                free_count: torch.Tensor, page_size: int, n_tokens: int, stream=None) -> dict:
     """Gives the new tokens of a step their pages and slots (gorio_page_tables).
 
     lengths, new_lens: int32 [requests], cached and new tokens; tables: int32 [requests, pages], updated in
@@ -114,61 +107,65 @@ def page_tables(lengths: torch.Tensor, new_lens: torch.Tensor, tables: torch.Ten
     from the top; n_tokens: the sum of new_lens.  Returns a dict of tensors: slots (int64) and
     positions, requests of each new token, starts [requests + 1], lengths after the step, served,
     free_count after the step, and tables.  Requests that find no pages are not served: slots -1."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return page_tables(lengths, new_lens, tables, free_pages, free_count, page_size, n_tokens)
     lib = load_library()
-    dev = _cuda_device("lengths", lengths)
+    index = _cuda_index("lengths", lengths)
     b = lengths.shape[0] if lengths.dim() == 1 else -1
-    _vector("lengths", lengths, dev)
-    _vector("new_lens", new_lens, dev, b)
-    _tables_2d(tables, b, dev)
-    _vector("free_pages", free_pages, dev)
-    _vector("free_count", free_count, dev, 1)
+    _vector("lengths", lengths, index)
+    _vector("new_lens", new_lens, index, b)
+    width, row = _tables_2d(tables, b, index)
+    _vector("free_pages", free_pages, index)
+    _vector("free_count", free_count, index, 1)
     if n_tokens < 0 or page_size < 1 or n_tokens >= 1 << 31 or page_size >= 1 << 31:
         raise _invalid("n_tokens must not be negative and page_size must be positive")
-    slots = torch.empty(n_tokens, dtype=torch.int64, device=dev)
+    slots = lengths.new_empty(n_tokens, dtype=torch.int64)
     # one allocation for the int32 results: their views cost less than an allocation each
-    ints = torch.empty(2 * n_tokens + 3 * b + 2, dtype=torch.int32, device=dev)
-    positions, requests, starts, out_lengths, served, left = ints.split_with_sizes((n_tokens, n_tokens, b + 1, b, b, 1))
+    ints = lengths.new_empty(2 * n_tokens + 3 * b + 2)
+    positions, requests, starts, out_lengths, served, left = torch.unsafe_split_with_sizes(ints, (n_tokens, n_tokens, b + 1, b, b, 1))
     at = ints.data_ptr()
     to_starts = at + 8 * n_tokens
     desc = _TABLES.pack(lengths.data_ptr(), new_lens.data_ptr(), tables.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(),
                         slots.data_ptr(), at, at + 4 * n_tokens, to_starts, to_starts + 4 * (b + 1), to_starts + 4 * (2 * b + 1),
-                        to_starts + 4 * (3 * b + 1), tables.stride(0), b, tables.shape[1], free_pages.shape[0], page_size, n_tokens, 0)
-    st = _call(lib.gorio_page_tables, desc, dev.index)
+                        to_starts + 4 * (3 * b + 1), row, b, width, free_pages.shape[0], page_size, n_tokens, 0)
+    st = _call(lib.gorio_page_tables, desc, index)
     if st:
         _fail(lib, st)
     return dict(tables=tables, slots=slots, positions=positions, requests=requests, starts=starts, lengths=out_lengths, served=served,
                 free_count=left)
 
 
-@_on_stream
-def cache_store(keys: torch.Tensor, values: torch.Tensor, key_pages: torch.Tensor, value_pages: torch.Tensor, slots: torch.Tensor) -> None:
+def cache_store(keys: torch.Tensor, values: torch.Tensor, key_pages: torch.Tensor, value_pages: torch.Tensor, slots: torch.Tensor,
+                stream=None) -> None:
     """Stores new keys and values, [tokens, heads, head size], to their slots of the pages in place
     (gorio_cache_store).  Tokens of a negative slot are skipped."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return cache_store(keys, values, key_pages, value_pages, slots)
     lib = load_library()
-    dev = _cuda_device("key_pages", key_pages)
-    ks, vs = _page_pair(key_pages, value_pages, dev)
-    pages, heads, page_size, dim = key_pages.shape
-    _rows_3d("keys", keys, dev, key_pages.dtype)
-    _rows_3d("values", values, dev, key_pages.dtype)
-    t = keys.shape[0]
-    if keys.shape != values.shape or keys.shape[1] != heads or keys.shape[2] != dim:
+    index = _cuda_index("key_pages", key_pages)
+    (pages, heads, page_size, dim), ks, vs = _page_pair(key_pages, value_pages, index)
+    k = _rows_3d("keys", keys, index, key_pages.dtype)
+    v = _rows_3d("values", values, index, key_pages.dtype)
+    shape = keys.shape
+    if shape != values.shape or shape[1] != heads or shape[2] != dim:
         raise _invalid(f"keys and values must be [tokens, {heads}, {dim}], as the pages")
-    _vector("slots", slots, dev, t, torch.int64)
-    k, v = keys.stride(), values.stride()
+    _vector("slots", slots, index, shape[0], torch.int64)
     desc = _STORE.pack(keys.data_ptr(), values.data_ptr(), key_pages.data_ptr(), value_pages.data_ptr(), slots.data_ptr(), k[0], k[1], v[0], v[1],
-                       ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], t, heads, dim, pages, page_size, 0)
-    st = _call(lib.gorio_cache_store, desc, dev.index)
+                       ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], shape[0], heads, dim, pages, page_size, 0)
+    st = _call(lib.gorio_cache_store, desc, index)
     if st:
         _fail(lib, st)
 
 
-def _stream_workspace(device):
+def _stream_workspace(index):
     """The workspace that this module keeps for the current stream of a device.  One made while a graph is captured
     belongs to the graph (its zeroing is captured too) and is not kept."""
-    key = (device.index, _raw_stream(device.index))
+    key = (index, _raw_stream(index))
     ws = _WORKSPACES.get(key)
     if ws is None:
-        ws = attention_workspace(device)
+        ws = attention_workspace(torch.device("cuda", index))
         if not torch.cuda.is_current_stream_capturing():
             _WORKSPACES[key] = ws
     return ws
@@ -186,10 +183,12 @@ def attention_workspace(device=None) -> torch.Tensor:
     return ws
 
 
-@_on_stream
-def attention_check(workspace: Optional[torch.Tensor] = None) -> None:
+def attention_check(workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """Raises GorioError if a paged_attention call with this workspace (default: the current stream's) ran into the time
     limit of a wait inside its kernel (gorio_attention_check).  Waits for the stream."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return attention_check(workspace)
     lib = load_library()
     if workspace is None:
         workspace = _WORKSPACES.get((torch.cuda.current_device(), _raw_stream(torch.cuda.current_device())))
@@ -200,11 +199,10 @@ def attention_check(workspace: Optional[torch.Tensor] = None) -> None:
         _fail(lib, st)
 
 
-@_on_stream
 def paged_attention(q: torch.Tensor, key_pages: torch.Tensor, value_pages: torch.Tensor, tables: torch.Tensor, lengths: torch.Tensor,
                     starts: torch.Tensor, max_new: int, scale: Optional[float] = None, causal: bool = True, window: int = 0,
                     softcap: float = 0.0, slopes: Optional[torch.Tensor] = None, want_lse: bool = False,
-                    out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> dict:
+                    out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> dict:
     """Attention of each request's new tokens over its cached keys and values (gorio_paged_attention).
 
     q: [tokens, heads, head size] of the pages' type, request r's rows starts[r]:starts[r+1]; pages:
@@ -213,40 +211,43 @@ def paged_attention(q: torch.Tensor, key_pages: torch.Tensor, value_pages: torch
     request.  scale defaults to head size ** -0.5.  Returns dict(out, lse), lse None unless wanted.
     `workspace` (attention_workspace()) defaults to one that this module keeps for each stream;
     calls that may overlap, as of graphs replayed side by side, need one each."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return paged_attention(q, key_pages, value_pages, tables, lengths, starts, max_new, scale, causal, window, softcap, slopes, want_lse,
+                                   out, workspace)
     lib = load_library()
-    dev = _cuda_device("q", q)
-    ks, vs = _page_pair(key_pages, value_pages, dev)
-    pages, kv_heads, page_size, dim = key_pages.shape
-    _rows_3d("q", q, dev, key_pages.dtype)
+    index = _cuda_index("q", q)
+    dtype = q.dtype
+    (pages, kv_heads, page_size, dim), ks, vs = _page_pair(key_pages, value_pages, index)
+    qs = _rows_3d("q", q, index, key_pages.dtype)
     t, heads, qd = q.shape
     if qd != dim:
         raise _invalid(f"q has heads of {qd} elements, the pages of {dim}")
     b = lengths.shape[0] if isinstance(lengths, torch.Tensor) and lengths.dim() == 1 else -1
-    _vector("lengths", lengths, dev)
-    _vector("starts", starts, dev, b + 1)
-    _tables_2d(tables, b, dev)
+    _vector("lengths", lengths, index)
+    _vector("starts", starts, index, b + 1)
+    width, row = _tables_2d(tables, b, index)
     if slopes is not None:
-        _vector("slopes", slopes, dev, heads, torch.float32)
+        _vector("slopes", slopes, index, heads, torch.float32)
     if not 0 <= window < 1 << 31 or not 0 <= max_new < 1 << 31:
         raise _invalid("window and max_new must not be negative")
     if out is None:
-        out = torch.empty((t, heads, dim), dtype=q.dtype, device=dev)
+        out = q.new_empty((t, heads, dim))
+        os = (heads * dim, dim)
     else:
-        _rows_3d("out", out, dev, q.dtype)
+        os = _rows_3d("out", out, index, dtype)
         if out.shape != q.shape:
             raise _invalid("out must have the shape of q")
-    lse = torch.empty((t, heads), dtype=torch.float32, device=dev) if want_lse else None
-    qs, os = q.stride(), out.stride()
-    index = dev.index
+    lse = q.new_empty((t, heads), dtype=torch.float32) if want_lse else None
     if workspace is None:
-        workspace = _stream_workspace(dev)
-    elif workspace.device != dev or workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or (
+        workspace = _stream_workspace(index)
+    elif workspace.get_device() != index or workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or (
             workspace.numel() < lib.gorio_attention_workspace_bytes(index)):
         raise _invalid("workspace must come from attention_workspace() for this device")
     desc = _ATTENTION.pack(q.data_ptr(), key_pages.data_ptr(), value_pages.data_ptr(), out.data_ptr(), lse.data_ptr() if want_lse else 0,
                            tables.data_ptr(), lengths.data_ptr(), starts.data_ptr(), 0 if slopes is None else slopes.data_ptr(),
-                           workspace.data_ptr(), qs[0], qs[1], os[0], os[1], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], tables.stride(0),
-                           b, t, heads, kv_heads, dim, pages, page_size, tables.shape[1], _DTYPES[q.dtype], 1 if causal else 0, window, max_new,
+                           workspace.data_ptr(), qs[0], qs[1], os[0], os[1], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], row,
+                           b, t, heads, kv_heads, dim, pages, page_size, width, _DTYPES[dtype], 1 if causal else 0, window, max_new,
                            1.0 / math.sqrt(dim) if scale is None else scale, softcap)
     st = _call(lib.gorio_paged_attention, desc, index)
     if st:
