@@ -27,6 +27,26 @@ __device__ __forceinline__ u64 scan_warp(u64 x) {
   return x;
 }
 
+// Division of x < 2^31 by a page size d: x * ceil(2^(31+l) / d) >> (31+l) with 2^l >= d (Granlund and Montgomery).  All
+// blocks divide for all requests; with the general division that took most of the time of a large call.
+struct Divider {
+  u32 mul, shift;
+  __device__ __forceinline__ u32 operator()(u32 x) const { return (u32)(((u64)x * mul) >> shift); }
+  __device__ __forceinline__ u32 up(u32 x) const { return x ? (*this)(x - 1) + 1 : 0u; }
+};
+
+// EACH consecutive numbers, zeros past the end
+template <int EACH>
+__device__ __forceinline__ void load_some(int (&v)[EACH], const int *p, u32 r, u32 end) {
+  if (EACH % 4 == 0 && ((uintptr_t)p & 15) == 0 && r + EACH <= end) {
+#pragma unroll
+    for (int k = 0; k < EACH / 4; ++k) *(int4 *)(v + 4 * k) = *(const int4 *)(p + r + 4 * k);
+  } else {
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) v[k] = r + k < end ? p[r + k] : 0;
+  }
+}
+
 // Request r: c cached tokens, n new ones, page size s.  need = ceil((c+n)/s) - ceil(c/s) pages, taken from
 // the top of the stack of free pages in request order; the sums over the requests that this needs are
 // prefix sums, which every block makes for itself over all requests (8 bytes each, out of L2 after the
@@ -38,7 +58,7 @@ __device__ __forceinline__ u64 scan_warp(u64 x) {
 // decode step.  EACH consecutive requests a thread and round: 1 where one round of a block holds all, as a
 // thread's divisions then take least; 8 beyond, where rounds count.
 template <int EACH>
-__global__ void __launch_bounds__(kTabThreads) page_tables_kernel(const gorio_page_tables_desc a) {
+__global__ void __launch_bounds__(kTabThreads) page_tables_kernel(const gorio_page_tables_desc a, const Divider pages_in) {
   __shared__ ScanShared sh;
   const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const u32 s = a.page_size;
@@ -50,19 +70,20 @@ __global__ void __launch_bounds__(kTabThreads) page_tables_kernel(const gorio_pa
   u64 top = 0;                   // pages taken by the last served request's end
   sh.req[tid] = -1;
   for (u32 round = 0, r0 = 0; r0 < a.n_requests; ++round, r0 += kTabThreads * EACH) {
-    i64 c[EACH], n[EACH];
+    __align__(16) int c[EACH];
+    __align__(16) int n[EACH];
+    u32 need[EACH];
+    load_some(c, a.lengths, r0 + tid * EACH, a.n_requests);
+    load_some(n, a.new_lens, r0 + tid * EACH, a.n_requests);
+    auto brought = [&](int k) { return n[k] < 0 ? 0u : min((u32)n[k], a.n_tokens + 1); };      // the sums stay small whatever comes in
+    auto fits = [&](int k) { return c[k] >= 0 && n[k] >= 0 && (u32)c[k] + (u32)n[k] <= a.table_width * s; };   // width * s < 2^31
     u64 x = 0, y = 0;
 #pragma unroll
     for (int k = 0; k < EACH; ++k) {
-      const u32 r = r0 + tid * EACH + k;
-      c[k] = n[k] = 0;
-      if (r < a.n_requests) { c[k] = a.lengths[r]; n[k] = a.new_lens[r]; }
+      need[k] = fits(k) ? pages_in.up((u32)c[k] + (u32)n[k]) - pages_in.up((u32)c[k]) : 0u;
+      x += brought(k);
+      y += need[k];
     }
-    auto brought = [&](int k) { return (u64)(n[k] < 0 ? 0 : n[k] > n_tok ? n_tok + 1 : n[k]); };     // the sums stay small whatever comes in
-    auto fits = [&](int k) { return c[k] >= 0 && n[k] >= 0 && c[k] + n[k] <= (i64)a.table_width * s; };   // width * s < 2^31
-    auto need = [&](int k) { return fits(k) ? (u64)((u32)(c[k] + n[k] + s - 1) / s - (u32)(c[k] + s - 1) / s) : 0; };
-#pragma unroll
-    for (int k = 0; k < EACH; ++k) { x += brought(k); y += need(k); }
     const u64 xw = scan_warp(x), yw = scan_warp(y);
     if (lane == 31) { sh.n[warp] = xw; sh.need[warp] = yw; }
     __syncthreads();                                   // also after the marks were cleared
@@ -72,19 +93,23 @@ __global__ void __launch_bounds__(kTabThreads) page_tables_kernel(const gorio_pa
     u64 upto_need = sum_need + (warp ? py : 0) + yw - y;
     sum_n += __shfl_sync(0xffffffffu, wn, 31);
     sum_need += __shfl_sync(0xffffffffu, wy, 31);
+    // Most blocks have nothing to do with most requests: a block looks closer at those that overlap its tokens and those whose
+    // outputs it writes (warps' requests go round the blocks); block 0 at all, for the count of pages.
+    const bool writes = (round * (kTabThreads / 32) + warp) % gridDim.x == blockIdx.x;
+    const bool overlaps = (i64)upto_n < base + kTabThreads && (i64)(upto_n + x) > base;
 #pragma unroll
     for (int k = 0; k < EACH; ++k) {
       const u32 r = r0 + tid * EACH + k;
-      if (r >= a.n_requests) break;
+      if (r >= a.n_requests || !(writes || overlaps || blockIdx.x == 0)) break;
       const u64 start = upto_n, first = upto_need;
       upto_n += brought(k);
-      upto_need += need(k);
+      upto_need += need[k];
       const bool served = fits(k) && upto_need <= (u64)fc && upto_n <= (u64)n_tok;
       if (served) top = upto_need;
-      if (round % gridDim.x == blockIdx.x) {
+      if (writes) {
         if (r == 0) a.starts[0] = 0;
         a.starts[r + 1] = (int)(upto_n > (u64)n_tok ? (u64)n_tok : upto_n);
-        a.out_lengths[r] = (int)(served ? c[k] + n[k] : c[k]);
+        a.out_lengths[r] = served ? c[k] + n[k] : c[k];
         a.out_served[r] = served ? 1 : 0;
       }
       if (upto_n > start && (i64)start < base + kTabThreads && (i64)upto_n > base) {
@@ -134,7 +159,7 @@ __global__ void __launch_bounds__(kTabThreads) page_tables_kernel(const gorio_pa
     const int c = a.lengths[req];
     pos = c + (int)((u32)t - sh.start[at]);
     if (sh.served[at]) {
-      const u32 page_at = (u32)pos / s, in_page = (u32)pos - page_at * s, held = ((u32)c + s - 1) / s;
+      const u32 page_at = pages_in((u32)pos), in_page = (u32)pos - page_at * s, held = pages_in.up((u32)c);
       int page;
       if (page_at < held) {
         page = a.tables[(i64)req * a.table_stride + page_at];
@@ -198,8 +223,11 @@ __global__ void __launch_bounds__(kStoreThreads) cache_store_kernel(const StoreA
 
 cudaError_t launch_page_tables(const gorio_page_tables_desc &d, cudaStream_t s) {
   const u32 blocks = d.n_tokens > 0 ? (d.n_tokens + kTabThreads - 1) / kTabThreads : 1;
-  if (d.n_requests <= (u32)kTabThreads) page_tables_kernel<1><<<blocks, kTabThreads, 0, s>>>(d);
-  else page_tables_kernel<8><<<blocks, kTabThreads, 0, s>>>(d);
+  u32 l = 0;
+  while ((1ull << l) < d.page_size) ++l;
+  const Divider pages_in{(u32)(((1ull << (31 + l)) + d.page_size - 1) / d.page_size), 31 + l};
+  if (d.n_requests <= (u32)kTabThreads) page_tables_kernel<1><<<blocks, kTabThreads, 0, s>>>(d, pages_in);
+  else page_tables_kernel<8><<<blocks, kTabThreads, 0, s>>>(d, pages_in);
   return cudaGetLastError();
 }
 
