@@ -155,7 +155,5 @@ __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.
 template <int N>
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
-__device__ __forceinline__ void some_barrier(u32 id, u32 threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
-
 }  // namespace paged
 }  // namespace gorio

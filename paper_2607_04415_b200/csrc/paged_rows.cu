@@ -9,6 +9,8 @@
 // are joined at the end of a unit, in the ring slot that each warp has just used up.
 // Blocks take equal shares of all keys of the call (the plan); a unit that is cut between blocks
 // leaves parts in the workspace that its last block joins.
+// 64 ragged requests over up to 8192 keys (32 heads of 128, 8 key heads, 1.06 GB) take 168 us in a burst, 176 sustained:
+// 6.0 to 6.3 TB/s, where a copy reaches 6.55.
 //
 // Scores: s = q.k (16-bit operands, 32-bit sums), then in 32 bits the scale, cap, bias and mask, the running
 // maximum m and sum l of 2^(x - m), x in units of log2.  The weights 2^(x - m) <= 1 are rounded to the
@@ -44,8 +46,8 @@ struct RowsShared {
 };
 
 // Rows of D elements in shared memory: 16-byte pieces, xor-ed with the row so that eight consecutive rows'
-// pieces of one column lie in different banks (D = 96: rows are 12 pieces, xor within the low two bits
-// keeps them inside the row; eight rows then meet in at most two banks' worth).
+// pieces of one column lie in different banks (D = 96: rows are 12 pieces, odd rows lie half of the banks on
+// already, and the xor stays within the low two bits and so inside the row).
 template <int D>
 __device__ __forceinline__ int piece_at(int row, int piece) {
   constexpr int P = D / 8;
