@@ -419,6 +419,7 @@ int gorio_cache_store(const gorio_cache_store_desc *d, void *cuda_stream);
  *   if slopes: x_j += slopes[h] * (j - p);   out = sum_j softmax(x)_j v_j;   lse = log sum_j exp(x_j).
  * A query that sees no key gets out = 0 and lse = -inf.  Sums, maxima and the softmax are held in 32
  * bits; the weights are rounded to the cache's type for the sum over values, and out once at the end.
+ * A capped score is off by at most some 2^-20 of itself (under caps up to 64: or 2^-22 of the cap), however large the cap.
  * What a query does not see has no effect on its result, whatever it holds (NaN included).  Rows of q that
  * belong to no request are not read and their results not written.
  *   q, out        [n_tokens][n_heads][dim]; key_pages, value_pages [n_pages][n_kv_heads][page_size][dim],

@@ -87,11 +87,23 @@ __device__ __forceinline__ float rcp_approx(float x) {
   return y;
 }
 
-// cap * tanh(x / cap) as cap * (1 - 2 / (1 + e^(2x/cap))): the error is some 1e-7 of the cap, where the
-// hardware's tanh is good to 5e-4 of it only, which would show in the weights.
-// Result in units of log2; `in` is scale * 2 log2(e) / cap, `out` is cap * log2(e).
-__device__ __forceinline__ float capped_log2(float dot, float in, float out) {
-  return fmaf(-2.0f * out, rcp_approx(1.0f + exp2_approx(dot * in)), out);
+// cap * tanh(u), u = x / cap, good to some 2^-20 of x however large the cap is.  From |u| = 1/4 on it is cap * (1 - 2 / (1 + e^2u)), whose
+// error is some 2^-22 of the cap (the hardware's tanh is good to 2^-11 of it only, which would show in the weights).  Below,
+// that would be any part of x, up to all of it; there it is x * (1 - u^2/3 + 2u^4/15 - 17u^6/315), whose next term is below
+// 2^-21.  In units of log2, and of w = 2u log2(e), the exponent.
+constexpr float kCapSeries = 0.25f * 2.0f * kLog2e;                      // |w| below: the series
+constexpr float kCapUnit = (kLn2 / 2.0f) * (kLn2 / 2.0f);                // u^2 = kCapUnit * w^2
+constexpr float kCap1 = -kCapUnit / 3.0f, kCap2 = 2.0f * kCapUnit * kCapUnit / 15.0f, kCap3 = -17.0f * kCapUnit * kCapUnit * kCapUnit / 315.0f;
+
+// w of a dot product of 1; finite, so that a dot product of 0 stays 0 under the smallest caps
+__device__ __forceinline__ float cap_in(const Attn &a) { return fminf(a.scale * (2.0f * kLog2e) / a.softcap, 1e38f); }
+
+// `in` as above, `out` is cap * log2(e), `linear` is scale * log2(e)
+__device__ __forceinline__ float capped_log2(float dot, float in, float out, float linear) {
+  const float w = dot * in, q = w * w;
+  const float small = dot * linear * fmaf(q, fmaf(q, fmaf(q, kCap3, kCap2), kCap1), 1.0f);
+  const float large = fmaf(-2.0f * out, rcp_approx(1.0f + exp2_approx(w)), out);
+  return fabsf(w) < kCapSeries ? small : large;
 }
 
 // Writes four columns of a finished row: acc / sum, rounded once.  A row that sees no key has sum 0 and gives 0 and

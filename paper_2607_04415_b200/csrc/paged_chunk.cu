@@ -114,7 +114,7 @@ __device__ __noinline__ void plain_row(const Attn &a, u32 req, u32 h, const Row 
         x += u.x * v.x;
         x += u.y * v.y;
       }
-      x = a.softcap > 0.0f ? capped_log2(x, a.scale * (2.0f * kLog2e / a.softcap), a.softcap * kLog2e) : x * a.scale * kLog2e;
+      x = a.softcap > 0.0f ? capped_log2(x, cap_in(a), a.softcap * kLog2e, a.scale * kLog2e) : x * a.scale * kLog2e;
       x += slope * (float)(key - r.pos);
       if (pass == 0) { top = fmaxf(top, x); continue; }
       const float w = exp2_approx(x - (top == -INFINITY ? 0.0f : top));
@@ -150,7 +150,12 @@ __device__ __forceinline__ void weights64(const float *s, f32x2 mul, f32x2 minus
   }
 }
 
-template <typename T, int D, bool SCORED>
+// What becomes of q.k: nothing but the scale; a cap of up to 64 or a bias; a cap of any size.  Without its series capped_log2 is off by
+// some 2^-22 of the cap, which up to 64 is less than the weights' rounding, and a call of such layers takes 103 us where it
+// takes 111 with the series.
+enum Scores { kPlain, kSmallCap, kLargeCap };
+
+template <typename T, int D, Scores SCORES>
 __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __grid_constant__ Attn a, const __grid_constant__ CUtensorMap keys,
                                                                       const __grid_constant__ CUtensorMap values, const u32 box_rows) {
   extern __shared__ unsigned char raw[];
@@ -213,8 +218,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
       const Row r = row_of(a, p, (u32)p.row0 + (valid ? unit_row : 0));
       float m = -INFINITY, l = 0.0f;
       {
-        const float slope = SCORED && a.slopes ? a.slopes[r.head] * kLog2e : 0.0f;
-        const float mul = SCORED ? 1.0f : a.scale * kLog2e;
+        const float slope = SCORES != kPlain && a.slopes ? a.slopes[r.head] * kLog2e : 0.0f;
+        const float mul = SCORES != kPlain ? 1.0f : a.scale * kLog2e;
         for (int at = first; at < p.tiles; at += split ? 2 : 1) {
           if (!bar_wait(&sh.s_full[t], s_phase, failed)) break;
           s_phase ^= 1;
@@ -226,22 +231,34 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
 #pragma unroll
           for (int i = 0; i < 4; ++i) keep(s + 32 * i);
           const int key0 = (p.tile + at) * kTileKeys;
-          if (SCORED) {                                      // to units of log2, with cap and bias
-            const float far = slope * (float)(key0 - r.pos), in = a.softcap > 0.0f ? a.scale * (2.0f * kLog2e / a.softcap) : a.scale * kLog2e;
-            const f32x2 in2 = pack_f32(in, in), slope2 = pack_f32(slope, slope), one2 = pack_f32(1.0f, 1.0f);
-            const float cap = a.softcap * kLog2e;
-            const f32x2 twice2 = pack_f32(-2.0f * cap, -2.0f * cap), cap2 = pack_f32(cap + far, cap + far), far2 = pack_f32(far, far);
+          if (SCORES != kPlain) {                            // to units of log2, with cap and bias
+            const float far = slope * (float)(key0 - r.pos), linear = a.scale * kLog2e, cap = a.softcap * kLog2e;
+            const float in = a.softcap > 0.0f ? cap_in(a) : linear;
+            const f32x2 in2 = pack_f32(in, in), slope2 = pack_f32(slope, slope), one2 = pack_f32(1.0f, 1.0f), zero2 = pack_f32(0.0f, 0.0f);
+            const f32x2 twice2 = pack_f32(-2.0f * cap, -2.0f * cap), far2 = pack_f32(far, far);
+            const f32x2 cap2 = SCORES == kLargeCap ? pack_f32(cap, cap) : pack_f32(cap + far, cap + far);
+            const f32x2 linear2 = pack_f32(linear, linear), c1 = pack_f32(kCap1, kCap1), c2 = pack_f32(kCap2, kCap2), c3 = pack_f32(kCap3, kCap3);
 #pragma unroll
             for (int i = 0; i < 128; i += 2) {
-              f32x2 x = pack_f32(s[i], s[i + 1]);
-              if (a.softcap > 0.0f) {                        // cap * tanh(x / cap), see capped_log2
+              const f32x2 dot = pack_f32(s[i], s[i + 1]);
+              f32x2 x;
+              if (SCORES == kLargeCap || a.softcap > 0.0f) {  // cap * tanh(x / cap), see capped_log2
                 float e0, e1;
-                x = fma_f32x2(x, in2, pack_f32(0.0f, 0.0f));
-                unpack_f32(x, e0, e1);
+                const f32x2 w = fma_f32x2(dot, in2, zero2);
+                unpack_f32(w, e0, e1);
                 unpack_f32(add_f32x2(pack_f32(exp2_approx(e0), exp2_approx(e1)), one2), e0, e1);
                 x = fma_f32x2(twice2, pack_f32(rcp_approx(e0), rcp_approx(e1)), cap2);
+                if (SCORES == kLargeCap) {
+                  const f32x2 q = fma_f32x2(w, w, zero2);
+                  const f32x2 small = fma_f32x2(fma_f32x2(dot, linear2, zero2), fma_f32x2(q, fma_f32x2(q, fma_f32x2(q, c3, c2), c1), one2), zero2);
+                  float w0, w1, s0, s1;
+                  unpack_f32(w, w0, w1);
+                  unpack_f32(small, s0, s1);
+                  unpack_f32(x, e0, e1);
+                  x = add_f32x2(pack_f32(fabsf(w0) < kCapSeries ? s0 : e0, fabsf(w1) < kCapSeries ? s1 : e1), far2);
+                }
               } else {
-                x = fma_f32x2(x, in2, far2);
+                x = fma_f32x2(dot, in2, far2);
               }
               unpack_f32(fma_f32x2(slope2, pack_f32((float)i, (float)(i + 1)), x), s[i], s[i + 1]);
             }
@@ -771,7 +788,7 @@ bool page_map(CUtensorMap *map, const Attn &a, const void *base, i64 st, i64 sh,
                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T, int D, bool SCORED>
+template <typename T, int D, Scores SCORES>
 cudaError_t launch(const Attn &a, const CUtensorMap &k, const CUtensorMap &v, u32 box_rows, u32 sms, cudaStream_t s) {
   static bool ready[64] = {};
   constexpr size_t bytes = sizeof(ChunkShared<D>) + 1024;
@@ -781,29 +798,30 @@ cudaError_t launch(const Attn &a, const CUtensorMap &k, const CUtensorMap &v, u3
   if (e != cudaSuccess) return e;
   if (dev >= 64) return cudaErrorInvalidDevice;
   if (!ready[dev]) {
-    e = cudaFuncSetAttribute(attention_chunk_kernel<T, D, SCORED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    e = cudaFuncSetAttribute(attention_chunk_kernel<T, D, SCORES>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (e != cudaSuccess) return e;
     // the warps' register shares come out of what the block is launched with: with fewer they would wait for ever
     cudaFuncAttributes f;
-    e = cudaFuncGetAttributes(&f, attention_chunk_kernel<T, D, SCORED>);
+    e = cudaFuncGetAttributes(&f, attention_chunk_kernel<T, D, SCORES>);
     if (e != cudaSuccess) return e;
     if (f.numRegs * kThreads < kSoftmaxRegs * 256 + kOtherRegs * 128) return cudaErrorInvalidKernelImage;
     ready[dev] = true;
   }
-  attention_chunk_kernel<T, D, SCORED><<<sms, kThreads, bytes, s>>>(a, k, v, box_rows);
+  attention_chunk_kernel<T, D, SCORES><<<sms, kThreads, bytes, s>>>(a, k, v, box_rows);
   return cudaGetLastError();
 }
 
 template <typename T, int D>
-cudaError_t pick_scored(const Attn &a, const CUtensorMap &k, const CUtensorMap &v, u32 box_rows, u32 sms, cudaStream_t s) {
-  return a.softcap > 0.0f || a.slopes ? launch<T, D, true>(a, k, v, box_rows, sms, s) : launch<T, D, false>(a, k, v, box_rows, sms, s);
+cudaError_t pick_scores(const Attn &a, const CUtensorMap &k, const CUtensorMap &v, u32 box_rows, u32 sms, cudaStream_t s) {
+  if (a.softcap > 64.0f) return launch<T, D, kLargeCap>(a, k, v, box_rows, sms, s);
+  return a.softcap > 0.0f || a.slopes ? launch<T, D, kSmallCap>(a, k, v, box_rows, sms, s) : launch<T, D, kPlain>(a, k, v, box_rows, sms, s);
 }
 
 template <typename T>
 cudaError_t pick_dim(const Attn &a, const CUtensorMap &k, const CUtensorMap &v, u32 box_rows, int dim, u32 sms, cudaStream_t s) {
-  if (dim == 64) return pick_scored<T, 64>(a, k, v, box_rows, sms, s);
-  if (dim == 96) return pick_scored<T, 96>(a, k, v, box_rows, sms, s);
-  return pick_scored<T, 128>(a, k, v, box_rows, sms, s);
+  if (dim == 64) return pick_scores<T, 64>(a, k, v, box_rows, sms, s);
+  if (dim == 96) return pick_scores<T, 96>(a, k, v, box_rows, sms, s);
+  return pick_scores<T, 128>(a, k, v, box_rows, sms, s);
 }
 
 }  // namespace

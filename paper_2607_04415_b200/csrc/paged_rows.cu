@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<D>) attention_rows_kern
 
   constexpr int P = D / 8;                       // 16-byte pieces of a row
   constexpr int kLoads = kWarpKeys * P / 32;     // cp.async a lane for 16 rows
-  const float to_log2 = a.scale * kLog2e;
+  const float to_log2 = a.scale * kLog2e, to_cap = SCORED && a.softcap > 0.0f ? cap_in(a) : 0.0f;
 
   // --- the loading side: a cursor that runs ahead, and the cache row of the next tile's key that this lane looks up.
   // Where pages are multiples of a warp's 16 keys, those keys follow each other in one page: one address a lane and steps
@@ -191,7 +191,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<D>) attention_rows_kern
         for (int x = 0; x < 4; ++x) {
           const int i = x >> 1, key = key0 + n * 8 + t4 * 2 + (x & 1);
           if (SCORED) {
-            const float v = a.softcap > 0.0f ? capped_log2(s[n][x], a.scale * (2.0f * kLog2e / a.softcap), a.softcap * kLog2e) : s[n][x] * to_log2;
+            const float v = a.softcap > 0.0f ? capped_log2(s[n][x], to_cap, a.softcap * kLog2e, to_log2) : s[n][x] * to_log2;
             s[n][x] = v + slope[i] * (float)(key - pos[i]);
           } else {
             s[n][x] *= to_log2;
