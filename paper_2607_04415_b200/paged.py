@@ -159,15 +159,23 @@ def cache_store(keys: torch.Tensor, values: torch.Tensor, key_pages: torch.Tenso
         _fail(lib, st)
 
 
+def _capturing(index):
+    """Whether the current stream of a device is being captured into a graph."""
+    if torch._C._cuda_getDevice() == index:
+        return torch._C._cuda_isCurrentStreamCapturing()
+    with torch.cuda.device(index):
+        return torch._C._cuda_isCurrentStreamCapturing()
+
+
 def _stream_workspace(index):
-    """The workspace that this module keeps for the current stream of a device.  One made while a graph is captured
-    belongs to the graph (its zeroing is captured too) and is not kept."""
+    """The workspace that this module keeps for the current stream of a device.  While that stream is captured, always a new one, which
+    belongs to the graph (its zeroing is captured too): a replay may run beside calls on the stream, or beside other graphs of it."""
+    if _capturing(index):
+        return attention_workspace(torch.device("cuda", index))
     key = (index, _raw_stream(index))
     ws = _WORKSPACES.get(key)
     if ws is None:
-        ws = attention_workspace(torch.device("cuda", index))
-        if not torch.cuda.is_current_stream_capturing():
-            _WORKSPACES[key] = ws
+        ws = _WORKSPACES[key] = attention_workspace(torch.device("cuda", index))
     return ws
 
 
@@ -209,8 +217,9 @@ def paged_attention(q: torch.Tensor, key_pages: torch.Tensor, value_pages: torch
     [pages, key heads, page size, head size], any strides of the outer axes; lengths: int32 [requests],
     keys of each request, the new tokens' own included; max_new: at least the most new tokens of a
     request.  scale defaults to head size ** -0.5.  Returns dict(out, lse), lse None unless wanted.
-    `workspace` (attention_workspace()) defaults to one that this module keeps for each stream;
-    calls that may overlap, as of graphs replayed side by side, need one each."""
+    `workspace` (attention_workspace()) defaults to one that this module keeps for each stream, or, in a
+    captured call, to one of the graph's own, which costs the graph a fill of 64 KB for each call and which attention_check
+    cannot see; calls that may overlap need one each."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return paged_attention(q, key_pages, value_pages, tables, lengths, starts, max_new, scale, causal, window, softcap, slopes, want_lse,

@@ -1,0 +1,76 @@
+"""Whose workspace an attention call uses, and what the checks of one refuse."""
+import types
+
+import pytest
+import torch
+
+
+@pytest.fixture(scope="module")
+def gorio():
+    from paper_2607_04415_b200 import build
+    build.build()
+    import paper_2607_04415_b200 as g
+    return g
+
+
+def test_a_captured_call_never_takes_the_streams_workspace(gorio, monkeypatch):
+    from paper_2607_04415_b200 import paged
+    made, state = [], types.SimpleNamespace(capturing=False)
+    monkeypatch.setattr(paged, "attention_workspace", lambda device=None: made.append(object()) or made[-1])
+    monkeypatch.setattr(paged, "_raw_stream", lambda index: 77)
+    monkeypatch.setattr(paged, "_WORKSPACES", {})
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_isCurrentStreamCapturing", lambda: state.capturing, raising=False)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: state.capturing)
+    kept = paged._stream_workspace(0)
+    assert paged._stream_workspace(0) is kept
+    state.capturing = True
+    first, second = paged._stream_workspace(0), paged._stream_workspace(0)
+    assert len({id(kept), id(first), id(second)}) == 3
+    state.capturing = False
+    assert paged._stream_workspace(0) is kept and len(made) == 3
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("new", [30, 130])
+def test_a_graph_beside_calls_on_the_stream_it_was_captured_on(gorio, new):
+    from test_paged_cache import Case
+    from paper_2607_04415_b200 import paged
+    c = Case([1, new, 1], [5000, 900, 77], dim=128, heads=8, kv_heads=2)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    first = c.run(gorio, stream=s)                            # a warm-up: the stream has a workspace now
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        held = c.run(gorio)
+    kept = paged._WORKSPACES[0, s.cuda_stream]
+    kept[: (1 << 16) - 4] = 1                                 # as if a call on s were halfway
+    before = kept.clone()
+    held["out"].zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    same, untouched = torch.equal(first["out"], held["out"]), torch.equal(kept, before)
+    kept[: 1 << 16] = 0
+    assert same and untouched
+
+
+@pytest.mark.gpu
+def test_calls_on_two_streams_overlap(gorio):
+    """Twenty calls on each of two streams and replays of a graph on a third, none waiting for the others."""
+    from test_paged_cache import Case
+    cases = [Case([1, 1], [9000, 3000], dim=128, heads=8, kv_heads=2), Case([130, 40], [4000, 900], dim=64, heads=8, kv_heads=2)]
+    want = [c.run(gorio) for c in cases]
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=streams[0]):
+        held = [c.run(gorio) for c in cases]
+    torch.cuda.synchronize()
+    got = []
+    for i in range(20):
+        got += [(k, cases[k].run(gorio, stream=streams[k])) for k in range(2)]
+        with torch.cuda.stream(streams[2]):
+            graph.replay()
+    torch.cuda.synchronize()
+    for k, g in got + list(enumerate(held)):
+        assert torch.equal(g["out"], want[k]["out"]) and torch.equal(g["lse"], want[k]["lse"])
