@@ -425,7 +425,8 @@ int gorio_cache_store(const gorio_cache_store_desc *d, void *cuda_stream);
  *   q, out        [n_tokens][n_heads][dim]; key_pages, value_pages [n_pages][n_kv_heads][page_size][dim],
  *                 in any order of the outer axes (strides); lse f32 [n_tokens][n_heads] or NULL.
  *   tables        i32 [n_requests] rows of table_width entries, table_stride apart.
- *   max_new       at least the most new tokens of a request: a hint for the choice of the kernel.
+ *   max_new       at least the most new tokens of a request: with table_width * page_size, the most keys of one, a hint
+ *                 for the choice of the kernel (a table no wider than the requests need makes the better choice).
  *   workspace     gorio_attention_workspace_bytes() bytes, 256-byte aligned, whose first 64 KB were zero before
  *                 its first use.  Each call leaves them zero; calls that may overlap need one each.
  * Preconditions: dtype one of GORIO_KV_*, dim 64, 96 or 128, n_heads a multiple of n_kv_heads, every

@@ -44,6 +44,26 @@ int sm_count(int dev) {
   return known[dev];
 }
 
+// Whether the rows kernel takes a call.  It reads a request's keys once for every 16 rows ((token, query head) pairs of a key head), the
+// chunk kernel once for every 256, but the chunk kernel's start and its joins cost some 14 us more.  Up to 16 rows the rows
+// kernel has no work to spare.  Beyond, the two times are compared as measured (bfloat16, head sizes 64 to 128, 1 to 8
+// key heads, 1 to 64 requests, 24 to 256 rows each, 150 to 131072 keys): a unit of 16 rows takes 0.6 ps for each element of a
+// key, and what 384 keys take besides; one of 256 rows 1 ps an element.  The host has bounds of units and keys only.
+//   8 key heads of 128, 1 request, 192 rows each:   150 keys 12 us, chunk kernel 24;     2000 keys 27 against 32
+//                                    96 rows each:  8000 keys 38 against 39;            131072 keys 482 against 150
+//   2 key heads of 64, 64 requests, 24 rows each:    150 keys 12 against 18;              8000 keys 94 against 88
+bool takes_rows(const gorio_paged_attention_desc &d) {
+  const double group = d.n_heads / d.n_kv_heads, requests = d.n_requests < d.n_tokens ? d.n_requests : d.n_tokens;
+  if ((double)d.max_new * group <= 16) return true;
+  auto units = [&](double rows) {
+    const double alike = requests * std::ceil(d.max_new * group / rows), ragged = d.n_tokens * group / rows + requests;
+    return d.n_kv_heads * (alike < ragged ? alike : ragged);
+  };
+  const double places = (double)d.table_width * d.page_size, seen = (double)d.window + d.max_new;
+  const double keys = d.window && seen < places ? seen : places;
+  return 0.6 * units(16) * (keys + 384) * d.dim <= 14e6 + units(256) * keys * d.dim;
+}
+
 }  // namespace
 
 extern "C" int gorio_page_tables(const gorio_page_tables_desc *d, void *cuda_stream) {
@@ -139,11 +159,7 @@ extern "C" int gorio_paged_attention(const gorio_paged_attention_desc *d, void *
   a.arrived = (u32 *)d->workspace;
   a.part_ml = (float *)((char *)d->workspace + kCounterBytes);
   a.part_o = (float *)((char *)a.part_ml + part_ml_bytes((u32)sms));
-  // Up to 16 rows share a key head in a request: the rows kernel, which is bound by the cache's bytes.  More: the chunk
-  // kernel, unless the rows kernel has at most 48 units of 16 rows to do in all, when its shorter start counts for more
-  // than its reading keys once for every 16 rows (8 key heads of 128: 64 rows each over 1000 keys 15 us against 22 in the
-  // chunk kernel, 96 rows over 8000 keys 37 against 39; in 8 requests 48 rows each over 8000 keys 114 against 77).
-  if ((uint64_t)d->max_new * a.group > 16 && (uint64_t)d->n_tokens * d->n_heads > 48 * 16) {
+  if (!takes_rows(*d)) {
     cudaError_t e = cudaSuccess;
     if (launch_chunk(a, (int)d->dtype, (int)d->dim, (u32)sms, (cudaStream_t)cuda_stream, &e)) return launched(e, "paged attention");
   }
