@@ -451,11 +451,17 @@ int gorio_paged_attention(const gorio_paged_attention_desc *d, void *cuda_stream
 
 /*
  * Whether every call with this workspace went well so far: OK; TIMEOUT if a wait inside a kernel passed its
- * limit of 10 s (the kernel then ends, its results are not valid; no such case is known); CAPACITY if a call had 2^31
+ * limit (the kernel then ends, its results are not valid); CAPACITY if a call had 2^31
  * or more tiles of keys, hours of work, and was not computed.  Waits for the stream; makes the workspace
  * ready for use again.
  */
 int gorio_attention_check(void *workspace, void *cuda_stream);
+
+/*
+ * The limit of a wait inside a kernel, for the calls from now on (a captured call keeps the one it was captured with): 10 s unless
+ * set, 0 sets that again.  Steps of 1024 ns, at most 73 minutes; a wait sleeps for some time before it looks at its limit.
+ */
+int gorio_attention_wait_limit(uint64_t nanoseconds);
 
 /* Bytes of the workspace above on CUDA device `cuda_device`; 0 if there is no such device. */
 uint64_t gorio_attention_workspace_bytes(int cuda_device);

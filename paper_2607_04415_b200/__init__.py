@@ -13,4 +13,6 @@ from .binding import (  # noqa: F401
     EXPORTED_SYMBOLS,
     search_resident_noalloc,
 )
-from .paged import attention_check, attention_workspace, cache_store, page_tables, paged_attention  # noqa: F401
+from .paged import (  # noqa: F401
+    attention_check, attention_wait_limit, attention_workspace, cache_store, page_tables, paged_attention,
+)

@@ -16,7 +16,7 @@ EXPORTED_SYMBOLS = [
     "gorio_stats", "gorio_stats_reset", "gorio_index_close", "gorio_status_str", "gorio_last_error",
     "gorio_search_resident_noalloc", "gorio_link_probe",
     "gorio_page_tables", "gorio_cache_store", "gorio_paged_attention", "gorio_attention_check",
-    "gorio_attention_workspace_bytes",
+    "gorio_attention_workspace_bytes", "gorio_attention_wait_limit",
 ]
 
 STATUS_NAMES = {0: "OK", 1: "INVALID_ARG", 2: "CUDA", 3: "NOMEM", 4: "STATE", 5: "TIMEOUT",
@@ -102,6 +102,7 @@ def load_library():
     for name in ("gorio_page_tables", "gorio_cache_store", "gorio_paged_attention"):
         getattr(lib, name).argtypes = [ctypes.c_char_p, vp]      # a packed descriptor, a stream
     lib.gorio_attention_check.argtypes = [vp, vp]
+    lib.gorio_attention_wait_limit.argtypes = [ctypes.c_uint64]
     lib.gorio_attention_workspace_bytes.argtypes = [ctypes.c_int]
     lib.gorio_attention_workspace_bytes.restype = ctypes.c_uint64
     _LIB = lib

@@ -36,6 +36,7 @@ struct Attn {
   // workspace: two partial results for every block, and a counter of arrivals for each
   float *part_o, *part_ml;
   u32 *arrived;
+  u32 wait_ticks;              // of 1024 ns: a wait inside the chunk kernel gives up when it has lasted as long
 };
 
 // One request as the kernels see it: keys it can have at most, its new tokens and where their rows

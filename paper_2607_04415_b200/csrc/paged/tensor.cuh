@@ -8,7 +8,7 @@
 namespace gorio {
 namespace paged {
 
-constexpr u64 kWaitLimitNs = 10ull * 1000000000ull;   // a wait that lasts longer has failed
+constexpr u32 kDrainTicks = 10000000;                   // of 1024 ns: of the waits for a block's own copies and products, at its end
 
 __device__ __forceinline__ u64 now_ns() {
   u64 t;
@@ -26,20 +26,31 @@ __device__ __forceinline__ bool bar_try(u64 *bar, u32 parity) {
   asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(ok) : "r"(smem_addr(bar)), "r"(parity) : "memory");
   return ok != 0;
 }
-// Waits for the phase of the given parity.  False once a wait of this block has lasted too long: the caller
-// then leaves its loops, and the block ends with its error word set.
-__device__ __forceinline__ bool bar_wait(u64 *bar, u32 parity, volatile u32 *failed) {
-  if (bar_try(bar, parity)) return true;
-  const u64 t0 = now_ns();
-  while (!bar_try(bar, parity)) {
-    if (*failed) return false;
-    if (now_ns() - t0 > kWaitLimitNs) { *failed = 1; return false; }
+// Waits of a whole warp for the phase of the given parity, with one answer for all its lanes: what follows a wait (tensor memory,
+// votes) needs them together, and decided lane by lane some could see the phase end and others the limit pass.  False once a
+// wait of this block has lasted longer than its limit: the warp then leaves its loops, and the block ends with its error word set.
+struct WaitLimit {
+  u32 ticks;               // of 1024 ns
+  volatile u32 *failed;    // of the block
+};
+__device__ __forceinline__ u32 now_ticks() { return (u32)(now_ns() >> 10); }
+__device__ __forceinline__ bool warp_wait(u64 *bar, u32 parity, const WaitLimit &limit) {
+  bool ok = bar_try(bar, parity);
+  if (!__all_sync(0xffffffffu, ok)) {
+    const u32 t0 = now_ticks();
+    do {
+      if (now_ticks() - t0 >= limit.ticks) *limit.failed = 1;
+      if (__any_sync(0xffffffffu, *limit.failed)) return false;
+      ok = bar_try(bar, parity);
+    } while (!__all_sync(0xffffffffu, ok));
   }
   return true;
 }
-
-// The same for a whole warp, with one answer that the compiler knows to be one.
-__device__ __forceinline__ bool warp_wait(u64 *bar, u32 parity, volatile u32 *failed) { return __all_sync(0xffffffffu, bar_wait(bar, parity, failed)); }
+// A wait for what this block itself has set going and nothing can hold up: no reason to give up early.
+__device__ __forceinline__ void drain(u64 *bar, u32 parity) {
+  const u32 t0 = now_ticks();
+  while (!bar_try(bar, parity) && now_ticks() - t0 < kDrainTicks) {}
+}
 __device__ __forceinline__ u32 uniform(u32 v) { return __shfl_sync(0xffffffffu, v, 0); }
 __device__ __forceinline__ bool one_lane() {
   u32 yes;

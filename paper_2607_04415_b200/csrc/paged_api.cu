@@ -1,4 +1,5 @@
 // C entry points of the paged key/value cache: checks of arguments, then one launch.
+#include <atomic>
 #include <cmath>
 #include <cstdio>
 #include <mutex>
@@ -43,6 +44,9 @@ int sm_count(int dev) {
   }
   return known[dev];
 }
+
+constexpr uint64_t kWaitLimitNs = 10ull * 1000000000ull;
+std::atomic<uint64_t> wait_limit{kWaitLimitNs};
 
 // Whether the rows kernel takes a call.  It reads a request's keys once for every 16 rows ((token, query head) pairs of a key head), the
 // chunk kernel once for every 256, but the chunk kernel's start and its joins cost some 14 us more.  Up to 16 rows the rows
@@ -100,6 +104,11 @@ extern "C" uint64_t gorio_attention_workspace_bytes(int cuda_device) {
   return sms ? kCounterBytes + part_bytes((u32)sms) : 0;
 }
 
+extern "C" int gorio_attention_wait_limit(uint64_t nanoseconds) {
+  wait_limit.store(nanoseconds ? nanoseconds : kWaitLimitNs, std::memory_order_relaxed);
+  return GORIO_OK;
+}
+
 extern "C" int gorio_attention_check(void *workspace, void *cuda_stream) {
   if (!workspace) return bad("attention check: null argument");
   u32 word = 0;
@@ -113,7 +122,7 @@ extern "C" int gorio_attention_check(void *workspace, void *cuda_stream) {
     gorio::set_global_error("paged attention: a call had 2^31 or more tiles of keys and was not computed");
     return GORIO_ERR_CAPACITY;
   }
-  gorio::set_global_error("paged attention: a wait inside a kernel lasted longer than 10 s; the results of calls with this workspace are not valid");
+  gorio::set_global_error("paged attention: a wait inside a kernel lasted longer than its limit; the results of calls with this workspace are not valid");
   return GORIO_ERR_TIMEOUT;
 }
 
@@ -156,6 +165,8 @@ extern "C" int gorio_paged_attention(const gorio_paged_attention_desc *d, void *
   a.page = d->page_size; a.n_pages = d->n_pages; a.width = d->table_width;
   a.causal = d->causal != 0; a.window = d->window;
   a.scale = d->scale; a.softcap = d->softcap;
+  const uint64_t ticks = wait_limit.load(std::memory_order_relaxed) >> 10;
+  a.wait_ticks = ticks < 0xffffffffu ? (u32)ticks : 0xffffffffu;
   a.arrived = (u32 *)d->workspace;
   a.part_ml = (float *)((char *)d->workspace + kCounterBytes);
   a.part_o = (float *)((char *)a.part_ml + part_ml_bytes((u32)sms));

@@ -67,7 +67,7 @@ struct ChunkShared {
   PartInfo part[kParts];
   u64 kv_full[Shape<D>::stages], kv_empty[Shape<D>::stages];
   u64 part_full[kParts], part_empty[kParts];
-  u64 q_full[2], q_empty[2], s_full[2], p_full[2][2], o_full[2], scanned[kScans], meet;
+  u64 q_full[2], q_empty[2], s_full[2], p_full[2][2], o_full[2], scanned[kScans], meet, drained;
   u32 odd[kScans];
   u32 tmem, failed, last;
   union {
@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
       bar_init(&sh.q_full[lane], 1); bar_init(&sh.q_empty[lane], 1); bar_init(&sh.s_full[lane], 1); bar_init(&sh.o_full[lane], 1);
       bar_init(&sh.p_full[lane][0], 4); bar_init(&sh.p_full[lane][1], 4);
     }
-    if (lane == 0) { bar_init(&sh.meet, 8); sh.failed = 0; }
+    if (lane == 0) { bar_init(&sh.meet, 8); bar_init(&sh.drained, 1); sh.failed = 0; }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async();
     __syncwarp();
@@ -181,10 +181,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
   __syncthreads();
   mma_fence_after();
   const u32 tmem = sh.tmem;
-  volatile u32 *failed = &sh.failed;
+  const WaitLimit limit{a.wait_ticks, &sh.failed};
+  auto wait = [&](u64 *bar, u32 parity) { return warp_wait(bar, parity, limit); };
   // the part that is told `no`-th; false at the end
   auto take_part = [&](u32 no, PartInfo &p) {
-    if (!bar_wait(&sh.part_full[no % kParts], (no / kParts) & 1, failed)) return false;
+    if (!wait(&sh.part_full[no % kParts], (no / kParts) & 1)) return false;
     p = sh.part[no % kParts];
     return p.tiles != 0;
   };
@@ -205,12 +206,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
     auto meet = [&]() {                                      // all eight warps, with the limit of every other wait
       __syncwarp();
       if (lane == 0) bar_arrive(&sh.meet);
-      const bool ok = bar_wait(&sh.meet, meet_phase, failed);
+      const bool ok = wait(&sh.meet, meet_phase);
       meet_phase ^= 1;
       return ok;
     };
     PartInfo p;
-    for (u32 no = 0; take_part(no, p); ++no) {
+    bool fine = true;                                        // no wait of this warp has run out
+    for (u32 no = 0; fine && take_part(no, p); ++no) {
       const bool split = p.rows <= kTileRows;                // one row tile: key tiles by turns
       const bool mine = t == 0 || !split;                    // whose rows this warpgroup writes
       const int unit_row = (split ? 0 : t * kTileRows) + row, first = split ? t : 0;
@@ -221,7 +223,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
         const float slope = SCORES != kPlain && a.slopes ? a.slopes[r.head] * kLog2e : 0.0f;
         const float mul = SCORES != kPlain ? 1.0f : a.scale * kLog2e;
         for (int at = first; at < p.tiles; at += split ? 2 : 1) {
-          if (!bar_wait(&sh.s_full[t], s_phase, failed)) break;
+          fine = wait(&sh.s_full[t], s_phase);
+          if (!fine) break;
           s_phase ^= 1;
           mma_fence_after();
           float s[128];
@@ -318,20 +321,20 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
           l = l0 + l1;
         }
       }
-      bool fine = true, odd = false;
+      bool odd = false;
       const int k0 = p.tile * kTileKeys, k1 = (p.tile + p.tiles) * kTileKeys;
       const bool two = split && p.tiles > 1;                 // both warpgroups have a part of the same rows
       if (two && t == 1) sh.half_ml[row] = make_float2(m, l);
-      if (mine) fine = bar_wait(&sh.scanned[no % kScans], (no / kScans) & 1, failed);
+      if (mine) fine = fine && wait(&sh.scanned[no % kScans], (no / kScans) & 1);
       for (int u = 0; u < 2; ++u) {                          // each keeps count of both outputs' phases
         if (u == 1 && split && !two) continue;
-        if (u == t || two) fine = bar_wait(&sh.o_full[u], (o_phase >> u) & 1, failed) && fine;
+        if (u == t || two) fine = fine && wait(&sh.o_full[u], (o_phase >> u) & 1);
         o_phase ^= 1u << u;
       }
       mma_fence_after();
       float f0 = 1.0f, f1 = 0.0f;
       if (two) {
-        fine = meet() && fine;
+        fine = fine && meet();
         if (t == 0) {
           const float2 other = sh.half_ml[row];
           const float top = fmaxf(m, other.x), base = top == -INFINITY ? 0.0f : top;
@@ -404,16 +407,16 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
               if (valid) write32(o + k, col + k, f);
           }
         }
-      } else {
+      } else if (fine) {
         // A cut unit.  The last block to get here joins the parts, its own out of tensor memory; the others leave theirs in
         // the workspace: [part][column / 4][row][4], so that neighbouring threads' rows lie side by side.
         const u32 own = blockIdx.x, others = p.i1 - p.i0;
         if (tid == 0) sh.last = load_acquire(a.arrived + p.i0) == others;
-        fine = meet() && fine;
-        bool join = sh.last != 0;
-        if (!join) {
+        fine = meet();
+        bool join = fine && sh.last != 0;
+        if (fine && !join) {
           const i64 slot = 2 * own + (own == p.i0 ? 1 : 0);
-          if (mine && fine) {
+          if (mine) {
             *(float2 *)(a.part_ml + (slot * kRows + unit_row) * 2) = make_float2(m, l);
 #pragma unroll 1
             for (int col = 0; col < D; col += kCols) {
@@ -425,14 +428,14 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
             }
           }
           __threadfence();
-          fine = meet() && fine;
-          if (tid == 0) { sh.last = atomicAdd(a.arrived + p.i0, 1u) == others; __threadfence(); }
-          fine = meet() && fine;
-          join = sh.last != 0;
+          fine = meet();
+          if (tid == 0 && fine) { sh.last = atomicAdd(a.arrived + p.i0, 1u) == others; __threadfence(); }
+          fine = fine && meet();
+          join = fine && sh.last != 0;
         }
         if (join) {
           if (tid == 0) a.arrived[p.i0] = 0;                 // ready for the next call
-          if (mine && fine) {
+          if (mine) {
             auto place = [&](u32 i) { return (i64)(2 * i + (i == p.i0 ? 1 : 0)); };
             float top = -INFINITY, sum = 0.0f;
 #pragma unroll 4
@@ -485,7 +488,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
         }
       }
       mma_fence_before();
-      if (two || !p.whole) meet();                           // sh.last and the other's output are free again
+      if (two || !p.whole) fine = fine && meet();            // sh.last and the other's output are free again
       part_done(no);
     }
   } else {
@@ -545,7 +548,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
           fence_async();
           __syncwarp();
         };
-        fine = warp_wait(&sh.q_full[0], q_phase & 1, failed);
+        fine = wait(&sh.q_full[0], q_phase & 1);
         q_phase ^= 1;
         if (uniform(p.rows <= kTileRows)) {
           // one row tile: key tile i goes to place i & 1; the ring holds key, value, key, value ...
@@ -557,7 +560,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
           for (u32 i = 0; i < 2 && i < n_tiles && fine; ++i) {
             u32 ph;
             const u32 k_stage = ahead(2 * i, ph);
-            fine = warp_wait(&sh.kv_full[k_stage], ph, failed);
+            fine = wait(&sh.kv_full[k_stage], ph);
             if (!fine) break;
             mma_fence_after();
             scores_of(i, 0, k_stage, i + 1 == n_tiles, true, k_stage);
@@ -566,11 +569,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
             u32 v_ph, k_ph;
             const u32 t = at & 1, v_stage = ahead(1, v_ph), k_stage = ahead(4, k_ph);
             const bool more = at + 2 < n_tiles;
-            fine = warp_wait(&sh.kv_full[v_stage], v_ph, failed) && (!more || warp_wait(&sh.kv_full[k_stage], k_ph, failed));
+            fine = wait(&sh.kv_full[v_stage], v_ph) && (!more || wait(&sh.kv_full[k_stage], k_ph));
             if (!fine) break;
             zero_rows(at, v_stage);
             for (u32 half = 0; half < 2 && fine; ++half) {
-              fine = warp_wait(&sh.p_full[t][half], (p_phase >> t) & 1, failed);
+              fine = wait(&sh.p_full[t][half], (p_phase >> t) & 1);
               if (!fine) break;
               mma_fence_after();
               outputs_of(t, v_stage, half, at > 1 || half > 0, half == 1 && !more, half == 1);
@@ -583,27 +586,27 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
           part_done(no);
           continue;
         }
-        fine = fine && warp_wait(&sh.q_full[1], q_phase >> 1, failed) && warp_wait(&sh.kv_full[stage], kv_phase, failed);
+        fine = fine && wait(&sh.q_full[1], q_phase >> 1) && wait(&sh.kv_full[stage], kv_phase);
         q_phase ^= 2;
         if (!fine) break;
         mma_fence_after();
         for (u32 t = 0; t < 2; ++t) scores_of(t, t, stage, n_tiles == 1, t == 1, stage);
         step();
-        fine = warp_wait(&sh.kv_full[stage], kv_phase, failed);
+        fine = wait(&sh.kv_full[stage], kv_phase);
         for (u32 at = 0; at < n_tiles && fine; ++at) {
           // here stage holds the tile's values, and they have arrived
           const u32 v_stage = stage;
           const bool more = at + 1 < n_tiles;
           step();
           const u32 k_stage = stage;
-          if (more && at == 0) fine = warp_wait(&sh.kv_full[k_stage], kv_phase, failed);
+          if (more && at == 0) fine = wait(&sh.kv_full[k_stage], kv_phase);
           zero_rows(at, v_stage);
           if (more) step();                                           // to the next tile's values
 #pragma unroll
           for (u32 t = 0; t < 2; ++t) {
             const bool final_t = t == 1;
             for (u32 half = 0; half < 2; ++half) {
-              fine = fine && warp_wait(&sh.p_full[t][half], (p_phase >> t) & 1, failed);
+              fine = fine && wait(&sh.p_full[t][half], (p_phase >> t) & 1);
               if (!fine) break;
               mma_fence_after();
               outputs_of(t, v_stage, half, at > 0 || half > 0, half == 1 && !more, half == 1 && !more && final_t);
@@ -613,16 +616,20 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
             if (more) {
               scores_of(t, t, k_stage, at + 2 == n_tiles, final_t, v_stage);
               // what the next tile needs, looked at while these products run: its values, then the keys after it
-              if (t == 0) fine = warp_wait(&sh.kv_full[stage], kv_phase, failed);
+              if (t == 0) fine = wait(&sh.kv_full[stage], kv_phase);
               if (fine && final_t && at + 2 < n_tiles) {
                 const u32 after = stage + 1 == (u32)S::stages ? 0 : stage + 1;
-                fine = warp_wait(&sh.kv_full[after], after ? kv_phase : kv_phase ^ 1, failed);
+                fine = wait(&sh.kv_full[after], after ? kv_phase : kv_phase ^ 1);
               }
             }
           }
         }
         part_done(no);
       }
+      // tensor memory is given back, and shared memory left, only when no product uses them any more
+      if (one_lane()) mma_commit(&sh.drained);
+      __syncwarp();
+      drain(&sh.drained, 0);
     } else if (warp == 9) {
       // ---------------------------------------------------------------- the copies
       const int boxes = kTileKeys / (int)box_rows * S::chunks;       // at most 32: a lane each
@@ -642,7 +649,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
           }
 #pragma unroll
           for (int kv = 0; kv < 2; ++kv) {
-            fine = fine && bar_wait(&sh.kv_empty[stage], phase, failed);
+            fine = fine && wait(&sh.kv_empty[stage], phase);
             if (!fine) break;
             if (lane == 0) bar_expect(&sh.kv_full[stage], (u32)S::tile_bytes);
             __syncwarp();
@@ -653,11 +660,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
         }
         part_done(no);
       }
-      if (*failed) {                                                  // leave no copy in flight behind: wait for each stage's last one
-        const u64 t0 = now_ns();
-        for (int i = 0; i < S::stages; ++i)
-          while (!bar_try(&sh.kv_full[i], i < stage ? phase ^ 1 : phase) && now_ns() - t0 < kWaitLimitNs) {}
-      }
+      // No copy is left in flight, even where the warps that wait for it have given up: each stage's last one.
+      for (int i = 0; i < S::stages; ++i) drain(&sh.kv_full[i], i < stage ? phase ^ 1 : phase);
     } else if (warp == 10) {
       // ---------------------------------------------------------------- the queries, values that are not finite
       int stage = 0;
@@ -667,7 +671,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
       for (u32 no = 0; fine && take_part(no, p); ++no) {
         const int tiles = p.rows > kTileRows ? 2 : 1;
         for (int t = 0; t < tiles && fine; ++t) {
-          fine = bar_wait(&sh.q_empty[t], (q_phase >> t) & 1, failed);
+          fine = wait(&sh.q_empty[t], (q_phase >> t) & 1);
           q_phase ^= 1u << t;
           if (!fine) break;
           for (int r = lane >> 2; r < kTileRows; r += 8) {            // four lanes a row; zeros past the last row
@@ -695,7 +699,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
           const bool look = z0 < last.lo || z1 > first.hi;
 #pragma unroll
           for (int kv = 0; kv < 2; ++kv) {
-            fine = fine && bar_wait(&sh.kv_full[stage], phase, failed);
+            fine = fine && wait(&sh.kv_full[stage], phase);
             if (!fine) break;
             if (kv && look) {
               // two ranges of rows: [z0, last.lo) and [first.hi, z1)
@@ -746,7 +750,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
           left -= (u32)p.tiles;
           c.at = to;
         }
-        if (!bar_wait(&sh.part_empty[slot], ((told / kParts) & 1) ^ 1, failed)) break;
+        if (!wait(&sh.part_empty[slot], ((told / kParts) & 1) ^ 1)) break;
         if (lane == 0) {
           sh.part[slot] = p;
           bar_arrive(&sh.part_full[slot]);

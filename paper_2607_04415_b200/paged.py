@@ -207,6 +207,14 @@ def attention_check(workspace: Optional[torch.Tensor] = None, stream=None) -> No
         _fail(lib, st)
 
 
+def attention_wait_limit(seconds: float = 0.0) -> None:
+    """The limit of a wait inside a paged_attention kernel, for calls from now on (gorio_attention_wait_limit); 0: the 10 s it has
+    unless set.  A call whose wait passes it ends, and attention_check raises."""
+    if not 0.0 <= seconds < 1e9:
+        raise _invalid("the limit of a wait must not be negative, nor longer than 1e9 s")
+    load_library().gorio_attention_wait_limit(math.ceil(seconds * 1e9))
+
+
 def paged_attention(q: torch.Tensor, key_pages: torch.Tensor, value_pages: torch.Tensor, tables: torch.Tensor, lengths: torch.Tensor,
                     starts: torch.Tensor, max_new: int, scale: Optional[float] = None, causal: bool = True, window: int = 0,
                     softcap: float = 0.0, slopes: Optional[torch.Tensor] = None, want_lse: bool = False,
