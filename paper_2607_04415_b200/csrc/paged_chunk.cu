@@ -17,7 +17,8 @@
 // Tensor memory, 512 columns: scores of tile 0 and 1 (128 each), outputs of tile 0 and 1 (head size each).
 //
 // Running maximum: a row's reference only moves when its maximum passes it by more than 2^8, since moving it
-// costs a pass over the output in tensor memory; weights are then at most 2^8, far inside both types.
+// costs a pass over the output in tensor memory; weights are then at most 2^8 (float16: 2^15, see
+// WeightLift), inside both types.
 // The sum of the weights is held unrounded in 32 bits, the weights are rounded once to the cache's type.
 //
 // Blocks take equal shares of all key tiles of the call (the plan), cut units are joined by their last block.
@@ -199,6 +200,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
     more_registers<kSoftmaxRegs>();
     const int t = warp >> 2, row = tid & (kTileRows - 1);
     constexpr int kCols = D % 64 == 0 ? 64 : 32;             // columns of the output that are worked on at a time
+    constexpr float kLift = WeightLift<T, 8>::value;
     constexpr int kAhead = 2;                                // parts of a cut unit that are fetched at a time, 32 columns of each
     const u32 lanes = (u32)(warp & 3) << 21;                 // this warp's 32 lanes of tensor memory
     const u32 scores = tmem + kScores + t * 128 + lanes, outputs = tmem + kOutputs + t * D + lanes;
@@ -303,7 +305,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
               }
             }
           }
-          const float minus_base = m == -INFINITY ? 0.0f : -m;
+          const float minus_base = m == -INFINITY ? 0.0f : kLift - m;
           const f32x2 mul2 = pack_f32(mul, mul), base2 = pack_f32(minus_base, minus_base);
           f32x2 sum[2] = {pack_f32(l, 0.0f), pack_f32(0.0f, 0.0f)};
 #pragma unroll
@@ -321,6 +323,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
           l = l0 + l1;
         }
       }
+      m -= kLift;                                            // what the weights and their sum count from
       bool odd = false;
       const int k0 = p.tile * kTileKeys, k1 = (p.tile + p.tiles) * kTileKeys;
       const bool two = split && p.tiles > 1;                 // both warpgroups have a part of the same rows

@@ -13,7 +13,7 @@
 // 6.0 to 6.3 TB/s, where a copy reaches 6.55.
 //
 // Scores: s = q.k (16-bit operands, 32-bit sums), then in 32 bits the scale, cap, bias and mask, the running
-// maximum m and sum l of 2^(x - m), x in units of log2.  The weights 2^(x - m) <= 1 are rounded to the
+// maximum m and sum l of 2^(x - m), x in units of log2.  The weights 2^(x - m) <= 1 (float16: <= 2^15, see WeightLift) are rounded to the
 // cache's type for the second product, whose error that doubles at most; l sums them unrounded.
 #include "paged/common.cuh"
 #include "paged/mma.cuh"
@@ -65,6 +65,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<D>) attention_rows_kern
 
   constexpr int P = D / 8;                       // 16-byte pieces of a row
   constexpr int kLoads = kWarpKeys * P / 32;     // cp.async a lane for 16 rows
+  constexpr float kLift = WeightLift<T, 0>::value;
   const float to_log2 = a.scale * kLog2e, to_cap = SCORED && a.softcap > 0.0f ? cap_in(a) : 0.0f;
 
   // --- the loading side: a cursor that runs ahead, and the cache row of the next tile's key that this lane looks up.
@@ -205,9 +206,9 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<D>) attention_rows_kern
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
         const float was = m[i];
         m[i] = fmaxf(was, top);
-        const float base = m[i] == -INFINITY ? 0.0f : m[i];   // nothing seen yet: every weight is 2^-inf = 0
+        const float most = m[i] == -INFINITY ? 0.0f : m[i], base = most - kLift;   // nothing seen yet: every weight is 2^-inf = 0
         if (__any_sync(0xffffffffu, m[i] != was)) {
-          const float f = exp2_approx(was - base);
+          const float f = exp2_approx(was - most);
           l[i] *= f;
 #pragma unroll
           for (int n = 0; n < D / 8; ++n) { o[n][2 * i] *= f; o[n][2 * i + 1] *= f; }
@@ -272,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<D>) attention_rows_kern
       l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
       l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
       const int row = g + 8 * i;
-      if (t4 == 0) { sh.m[warp][row] = m[i]; sh.l[warp][row] = l[i]; }
+      if (t4 == 0) { sh.m[warp][row] = m[i] - kLift; sh.l[warp][row] = l[i]; }
       if (row < rows) {
 #pragma unroll
         for (int n = 0; n < D / 8; ++n) *(float2 *)(mine + row * D + (n ^ (row & 3)) * 8 + t4 * 2) = make_float2(o[n][2 * i], o[n][2 * i + 1]);

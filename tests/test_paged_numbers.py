@@ -97,3 +97,28 @@ def test_attention_caps_far_above_the_scores(gorio, new, lens, cap, dtype, dim, 
 def test_attention_caps_across_the_scores(gorio, new, lens, cap, dtype, dim):
     """Scores of some hundreds, from far below the cap to far above it, in one row."""
     check(gorio, Case(new, lens, dim=dim, dtype=dtype, softcap=cap, sharp=30.0, seed=4), CAP_ERROR)
+
+
+@pytest.mark.parametrize("new", [1, 250])
+def test_attention_float16_weights_far_below_the_largest(gorio, new):
+    """Forty thousand keys of a weight 2^-25.6 each beside one of 1: together they are the whole result."""
+    c = Case([new], [40000], heads=4, kv_heads=2, dim=64, page=64, dtype=FP16)
+    c.kp.zero_(), c.vp.fill_(1.0), c.q.fill_(1.0)
+    first = c.tables[0, 0].item()
+    c.kp[first, :, 0], c.vp[first, :, 0] = 2.21875, 0.0
+    got = check(gorio, c, lambda capped, biased: 2.0 ** -21 * biased)
+    assert (got["out"] > 7e-4).all()
+
+
+@pytest.mark.parametrize("new,lens", [([1, 1], [300, 129]), ([250, 3], [430, 200]), ([250], [9000])])
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+def test_attention_of_even_and_of_rising_scores(gorio, new, lens, dtype):
+    """The largest weights the types hold: all keys alike, and keys whose scores rise along the axis, in steps that do not and that do move
+    the reference of the weights."""
+    for step in (0.0, 0.01, 0.07):
+        c = Case(new, lens, heads=4, kv_heads=2, dim=64, dtype=dtype, seed=9)
+        c.q.fill_(1.0), c.kp.zero_()
+        for r, n in enumerate(lens):
+            for i in range(ceil_div(n, 16)):
+                c.kp[c.tables[r, i].item(), :, :, 0] = 8.0 * step * (16.0 * i + torch.arange(16, device="cuda"))
+        check(gorio, c, lambda capped, biased: 2.0 ** -21 * biased)
