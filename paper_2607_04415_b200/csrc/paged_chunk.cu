@@ -10,7 +10,7 @@
 //   8         issues both products (one thread); zeros value rows that no query sees before they are used.
 //   9         copies key and value tiles, page by page (tensor copies, zeros for pages outside the cache), into a
 //             ring of stages with the 128-byte swizzle.
-//   10        gathers the queries; looks for values that are not finite in tiles that some rows see and others do not.
+//   10        gathers the queries; takes values that are not finite out of tiles that some rows see and others do not.
 //   11        walks the block's share of the work and tells the others its parts, ahead of them.
 // A unit of at most 128 rows has its even key tiles worked on as row tile 0 and its odd ones as row tile 1, with a running
 // maximum, sum and output each, which are joined at its end: otherwise one tile's softmax and products would wait for each other.
@@ -22,8 +22,9 @@
 // The sum of the weights is held unrounded in 32 bits, the weights are rounded once to the cache's type.
 //
 // Blocks take equal shares of all key tiles of the call (the plan), cut units are joined by their last block.
-// Values that are not finite (and masked for some rows) would reach rows that do not see them, as 0 * inf in the
-// product: a unit that meets one is computed again row by row from the cache, slowly, in plain_row.
+// Values that are not finite would reach rows that do not see them, as 0 * inf in the product.  In tiles that some rows
+// see and others do not, warp 10 puts zeros in their place before the product, and the rows that see them add
+// them at the end (add_odd).
 //
 // 2048 tokens over 18432 keys (32 heads of 128, 8 key heads, bfloat16) take 537 us sustained, 1.09 PFLOP/s, 476 us in a burst.
 #include "paged/common.cuh"
@@ -58,7 +59,7 @@ struct __align__(16) PartInfo {
   int q0, row0, rows, tile;
   int tiles, lo, hi, whole;
   u32 i0, i1;          // of a cut unit: the blocks that hold parts of it
-  u32 pad[2];
+  int every0, every1;  // keys that all its rows see
 };
 
 template <int D>
@@ -66,7 +67,7 @@ struct ChunkShared {
   unsigned char q[2][Shape<D>::tile_bytes];
   unsigned char kv[Shape<D>::stages][Shape<D>::tile_bytes];
   PartInfo part[kParts];
-  u64 kv_full[Shape<D>::stages], kv_empty[Shape<D>::stages];
+  u64 kv_full[Shape<D>::stages], kv_clean[Shape<D>::stages], kv_empty[Shape<D>::stages];
   u64 part_full[kParts], part_empty[kParts];
   u64 q_full[2], q_empty[2], s_full[2], p_full[2][2], o_full[2], scanned[kScans], meet, drained;
   u32 odd[kScans];
@@ -95,41 +96,39 @@ __device__ __forceinline__ Row row_of(const Attn &a, const PartInfo &p, u32 flat
   return r;
 }
 
-// One row straight from the cache, for units with values that are not finite: over the keys [k0, k1) that the row sees, with
-// col < 0 the maximum score (in units of log2) and the sum of the weights, else 32 columns of the weighted sum.
-template <typename T, int D>
-__device__ __noinline__ void plain_row(const Attn &a, u32 req, u32 h, const Row &r, int k0, int k1, int col, float *acc, float &top, float &sum) {
-  const u16 *q = (const u16 *)a.q + r.tok * a.q_t + (i64)r.head * a.q_h;
-  const float slope = a.slopes ? a.slopes[r.head] * kLog2e : 0.0f;
-  if (col < 0) { top = -INFINITY; sum = 0.0f; }
-  for (int pass = col < 0 ? 0 : 1; pass < 2; ++pass) {
-    for (int key = max(k0, r.lo); key < min(k1, r.hi); ++key) {
-      const u32 at = (u32)key / a.page;
-      const int pg = a.tables[(i64)req * a.tab_r + at];
-      const i64 in = (i64)((u32)key - at * a.page);
-      const bool there = (u32)pg < a.n_pages;
-      const u16 *k = (const u16 *)a.kp + (i64)pg * a.k_p + (i64)h * a.k_h + in * a.k_t;
-      float x = 0.0f;
-      for (int d = 0; d < D; d += 2) {
-        const float2 u = unpack2<T>(*(const u32 *)(q + d)), v = there ? unpack2<T>(*(const u32 *)(k + d)) : make_float2(0.0f, 0.0f);
-        x += u.x * v.x;
-        x += u.y * v.y;
-      }
-      x = a.softcap > 0.0f ? capped_log2(x, cap_in(a), a.softcap * kLog2e, a.scale * kLog2e) : x * a.scale * kLog2e;
-      x += slope * (float)(key - r.pos);
-      if (pass == 0) { top = fmaxf(top, x); continue; }
-      const float w = exp2_approx(x - (top == -INFINITY ? 0.0f : top));
-      if (col < 0) { sum += w; continue; }
-      if (!there) continue;
-      const u16 *v = (const u16 *)a.vp + (i64)pg * a.v_p + (i64)h * a.v_h + in * a.v_t + col;
+// Adds to 32 columns of a row's weighted sum the values that are not finite of the keys [k0, k1), which it sees, without
+// [every0, every1), which all rows of its unit see.  The product ran without them; a weight is above 0, whatever it is.
+template <typename T>
+__device__ __noinline__ void add_odd(const Attn &a, int req, int h, int k0, int k1, int every0, int every1, int col, float *acc) {
+  for (int key = k0; key < k1; ++key) {
+    if (key >= every0 && key < every1) key = every1;
+    if (key >= k1) break;
+    const u32 at = (u32)key / a.page;
+    const int pg = a.tables[(i64)req * a.tab_r + at];
+    if ((u32)pg >= a.n_pages) continue;
+    const u16 *v = (const u16 *)a.vp + (i64)pg * a.v_p + (i64)h * a.v_h + (i64)((u32)key - at * a.page) * a.v_t + col;
 #pragma unroll
-      for (int d = 0; d < 32; d += 2) {
-        const float2 u = unpack2<T>(*(const u32 *)(v + d));
-        acc[d] += w * u.x;
-        acc[d + 1] += w * u.y;
+    for (int d = 0; d < 32; d += 8) {
+      const uint4 x = *(const uint4 *)(v + d);
+      const u32 w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2 u = unpack2<T>(w[i]);
+        if (!isfinite(u.x)) acc[d + 2 * i] += u.x;
+        if (!isfinite(u.y)) acc[d + 2 * i + 1] += u.y;
       }
     }
   }
+}
+
+// eight 16-bit numbers with zeros for those that are not finite
+template <typename T>
+__device__ __forceinline__ uint4 finite8(uint4 v) {
+  auto clean = [](u32 x) {
+    constexpr u32 lo = ExponentBits<T>::mask, hi = lo << 16;
+    return ((x & lo) == lo ? 0u : x & 0xffffu) | ((x & hi) == hi ? 0u : x & 0xffff0000u);
+  };
+  return make_uint4(clean(v.x), clean(v.y), clean(v.z), clean(v.w));
 }
 
 // the lowest n bits, n cut to [0, 32]
@@ -164,7 +163,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
   typedef Shape<D> S;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (warp == 8) {
-    for (int i = lane; i < S::stages; i += 32) { bar_init(&sh.kv_full[i], 1); bar_init(&sh.kv_empty[i], 2); }
+    for (int i = lane; i < S::stages; i += 32) { bar_init(&sh.kv_full[i], 1); bar_init(&sh.kv_clean[i], 1); bar_init(&sh.kv_empty[i], 2); }
     if (lane < kParts) { bar_init(&sh.part_full[lane], 1); bar_init(&sh.part_empty[lane], 11); }
     if (lane < kScans) { bar_init(&sh.scanned[lane], 1); sh.odd[lane] = 0; }
     if (lane < 2) {
@@ -325,7 +324,6 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
       }
       m -= kLift;                                            // what the weights and their sum count from
       bool odd = false;
-      const int k0 = p.tile * kTileKeys, k1 = (p.tile + p.tiles) * kTileKeys;
       const bool two = split && p.tiles > 1;                 // both warpgroups have a part of the same rows
       if (two && t == 1) sh.half_ml[row] = make_float2(m, l);
       if (mine) fine = fine && wait(&sh.scanned[no % kScans], (no / kScans) & 1);
@@ -347,25 +345,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
           m = top;
         }
       }
-      if (mine) {
-        odd = fine && sh.odd[no % kScans] != 0;
-        if (odd) {
-          float top, sum;
-          plain_row<T, D>(a, p.r, p.h, r, k0, k1, -1, nullptr, top, sum);
-          m = top;
-          l = sum;
-        }
-      }
+      if (mine) odd = fine && sh.odd[no % kScans] != 0;
       auto output32 = [&](float *o, int col) {               // 32 columns of the row's output, not yet divided by l
-        if (odd) {
-          float x[32], top = m, sum = l;                     // not o itself, which stays in registers
-#pragma unroll
-          for (int k = 0; k < 32; ++k) x[k] = 0.0f;
-          plain_row<T, D>(a, p.r, p.h, r, k0, k1, col, x, top, sum);
-#pragma unroll
-          for (int k = 0; k < 32; ++k) o[k] = x[k];
-          return;
-        }
         tmem_ld32(o, outputs + col);
         tmem_wait_ld();
         keep(o);
@@ -376,6 +357,14 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
           keep(x);
 #pragma unroll
           for (int k = 0; k < 32; ++k) o[k] = f0 * o[k] + f1 * x[k];
+        }
+        if (odd) {
+          float x[32];                                       // not o itself, which stays in registers
+#pragma unroll
+          for (int k = 0; k < 32; ++k) x[k] = o[k];
+          add_odd<T>(a, p.r, p.h, max(p.tile * kTileKeys, r.lo), min((p.tile + p.tiles) * kTileKeys, r.hi), p.every0, p.every1, col, x);
+#pragma unroll
+          for (int k = 0; k < 32; ++k) o[k] = x[k];
         }
       };
       auto output = [&](float *o, int col) {                 // the same for kCols columns, with one wait where it can be
@@ -538,10 +527,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
         PartInfo p;
         if (!__all_sync(0xffffffffu, take_part(no, p))) break;
         const u32 n_tiles = uniform((u32)p.tiles);
-        // rows of a tile that lie outside [lo, hi): zero, whatever the pages hold there
-        auto zero_rows = [&](u32 at, u32 v_stage) {
+        // A tile's values before their product: that warp 10 is done with a tile which not all rows see all of, and zeros in the
+        // rows outside [lo, hi), whatever the pages hold there.
+        auto prepare = [&](u32 at, u32 v_stage, u32 phase) {
           const int key0 = (p.tile + (int)at) * kTileKeys;
-          if (key0 >= p.lo && key0 + kTileKeys <= p.hi) return;
+          if (key0 >= p.every0 && key0 + kTileKeys <= p.every1) return true;
+          if (!wait(&sh.kv_clean[v_stage], phase)) return false;
+          if (key0 >= p.lo && key0 + kTileKeys <= p.hi) return true;
           const int z0 = max(0, min(kTileKeys, p.lo - key0)), z1 = max(z0, min(kTileKeys, p.hi - key0)), rows = z0 + kTileKeys - z1;
           for (int x = lane; x < rows * 8; x += 32) {
             const int k = (x >> 3) < z0 ? x >> 3 : (x >> 3) - z0 + z1;
@@ -550,6 +542,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
           }
           fence_async();
           __syncwarp();
+          return true;
         };
         fine = wait(&sh.q_full[0], q_phase & 1);
         q_phase ^= 1;
@@ -573,8 +566,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
             const u32 t = at & 1, v_stage = ahead(1, v_ph), k_stage = ahead(4, k_ph);
             const bool more = at + 2 < n_tiles;
             fine = wait(&sh.kv_full[v_stage], v_ph) && (!more || wait(&sh.kv_full[k_stage], k_ph));
-            if (!fine) break;
-            zero_rows(at, v_stage);
+            fine = fine && prepare(at, v_stage, v_ph);
             for (u32 half = 0; half < 2 && fine; ++half) {
               fine = wait(&sh.p_full[t][half], (p_phase >> t) & 1);
               if (!fine) break;
@@ -598,12 +590,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
         fine = wait(&sh.kv_full[stage], kv_phase);
         for (u32 at = 0; at < n_tiles && fine; ++at) {
           // here stage holds the tile's values, and they have arrived
-          const u32 v_stage = stage;
+          const u32 v_stage = stage, v_phase = kv_phase;
           const bool more = at + 1 < n_tiles;
           step();
           const u32 k_stage = stage;
           if (more && at == 0) fine = wait(&sh.kv_full[k_stage], kv_phase);
-          zero_rows(at, v_stage);
+          fine = fine && prepare(at, v_stage, v_phase);
           if (more) step();                                           // to the next tile's values
 #pragma unroll
           for (u32 t = 0; t < 2; ++t) {
@@ -694,28 +686,38 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
         __syncwarp();
         if (lane == 0 && fine)
           for (int t = 0; t < tiles; ++t) bar_arrive(&sh.q_full[t]);
-        // all rows see the keys from the last row's first to the first row's last; others of [lo, hi) are looked at
-        const Row first = row_of(a, p, (u32)p.row0), last = row_of(a, p, (u32)(p.row0 + p.rows - 1));
         u32 odd = 0;
         for (int at = 0; at < p.tiles && fine; ++at) {
           const int key0 = (p.tile + at) * kTileKeys, z0 = max(key0, p.lo), z1 = min(key0 + kTileKeys, p.hi);
-          const bool look = z0 < last.lo || z1 > first.hi;
+          const bool look = z0 < p.every0 || z1 > p.every1;  // [lo, hi) without the keys that all rows see
 #pragma unroll
           for (int kv = 0; kv < 2; ++kv) {
             fine = fine && wait(&sh.kv_full[stage], phase);
             if (!fine) break;
             if (kv && look) {
-              // two ranges of rows: [z0, last.lo) and [first.hi, z1)
-              const int n0 = max(0, min(z1, last.lo) - z0), from1 = max(z0 + n0, first.hi), rows = n0 + max(0, z1 - from1);
+              // two ranges of rows: [z0, every0) and [every1, z1)
+              const int n0 = max(0, min(z1, p.every0) - z0), from1 = max(z0 + n0, p.every1), rows = n0 + max(0, z1 - from1);
+              u32 found = 0;
 #pragma unroll 4
               for (int x = lane; x < rows * 8; x += 32) {
                 const int k = ((x >> 3) < n0 ? z0 + (x >> 3) : from1 + (x >> 3) - n0) - key0;
 #pragma unroll
-                for (int i = 0; i < S::chunks; ++i) odd |= (u32)not_finite8<T>(*(const uint4 *)(sh.kv[stage] + i * (kTileKeys * 128) + k * 128 + (x & 7) * 16));
+                for (int i = 0; i < S::chunks; ++i) found |= (u32)not_finite8<T>(*(const uint4 *)(sh.kv[stage] + i * (kTileKeys * 128) + k * 128 + (x & 7) * 16));
               }
+              if (found) {
+                for (int x = lane; x < rows * 8; x += 32) {
+                  const int k = ((x >> 3) < n0 ? z0 + (x >> 3) : from1 + (x >> 3) - n0) - key0;
+                  for (int i = 0; i < S::chunks; ++i) {
+                    uint4 *const at = (uint4 *)(sh.kv[stage] + i * (kTileKeys * 128) + k * 128 + (x & 7) * 16);
+                    *at = finite8<T>(*at);
+                  }
+                }
+                fence_async();
+              }
+              odd |= found;
             }
             __syncwarp();
-            if (lane == 0) bar_arrive(&sh.kv_empty[stage]);
+            if (lane == 0) { bar_arrive(&sh.kv_clean[stage]); bar_arrive(&sh.kv_empty[stage]); }
             if (++stage == S::stages) { stage = 0; phase ^= 1; }
           }
         }
@@ -744,6 +746,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
           p.tile = c.span.first + c.at;
           p.tiles = to - c.at;
           p.lo = c.span.lo; p.hi = c.span.hi;
+          p.every0 = row_of(a, p, (u32)(p.row0 + p.rows - 1)).lo;
+          p.every1 = row_of(a, p, (u32)p.row0).hi;
           p.whole = c.at == 0 && to == c.span.tiles;
           if (!p.whole) {
             const u32 unit0 = plan.end - left - (u32)c.at;

@@ -68,10 +68,10 @@ def test_attention_under_limits_that_some_waits_pass(gorio, new, lens, heads, kv
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("new,lens,heads,kv_heads,dim,dtype,opts", CASES[1:4])
+@pytest.mark.parametrize("new,lens,heads,kv_heads,dim,dtype,opts", CASES[1:4] + [([250], [9000], 2, 2, 128, BF16, {})])
 def test_attention_whose_waits_run_out_says_so(gorio, new, lens, heads, kv_heads, dim, dtype, opts):
-    """A value that is not finite and that some rows do not see: the warps that compute its part again keep others waiting for far longer
-    than the limit."""
+    """A value that is not finite and that some rows do not see: the warps whose rows read the cache for it keep others waiting for far
+    longer than the limit."""
     c = Case(new, lens, heads=heads, kv_heads=kv_heads, dim=dim, dtype=dtype, **opts)
     for r, n in enumerate(lens):
         c.vp[c.tables[r, (n - 2) // 16].item(), :, (n - 2) % 16, 3] = float("inf")
