@@ -98,6 +98,27 @@ def _call(entry, desc, device_index):
         torch._C._cuda_setDevice(was)
 
 
+class _NoBackward(torch.autograd.Function):
+    """Hands results on, and refuses to go back through them."""
+
+    @staticmethod
+    def forward(ctx, out, lse, *inputs):
+        return out, lse
+
+    @staticmethod
+    def backward(ctx, *gradients):
+        raise _invalid("paged_attention has no backward pass: its gradients do not exist (torch.no_grad() or detach() says that none are meant)")
+
+
+def _without_gradient(out, lse, inputs):
+    """The results as they are, or, where an input asks for a gradient, as results whose backward pass raises."""
+    q, key_pages, value_pages, slopes = inputs
+    if (q.requires_grad or key_pages.requires_grad or value_pages.requires_grad or (slopes is not None and slopes.requires_grad)) and (
+            torch.is_grad_enabled()):
+        return _NoBackward.apply(out, lse, *inputs)
+    return out, lse
+
+
 def page_tables(lengths: torch.Tensor, new_lens: torch.Tensor, tables: torch.Tensor, free_pages: torch.Tensor,
                 free_count: torch.Tensor, page_size: int, n_tokens: int, stream=None) -> dict:
     """Gives the new tokens of a step their pages and slots (gorio_page_tables).
@@ -139,7 +160,7 @@ def page_tables(lengths: torch.Tensor, new_lens: torch.Tensor, tables: torch.Ten
 def cache_store(keys: torch.Tensor, values: torch.Tensor, key_pages: torch.Tensor, value_pages: torch.Tensor, slots: torch.Tensor,
                 stream=None) -> None:
     """Stores new keys and values, [tokens, heads, head size], to their slots of the pages in place
-    (gorio_cache_store).  Tokens of a negative slot are skipped."""
+    (gorio_cache_store).  Tokens of a negative slot are skipped.  Numbers are stored, without their autograd history."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return cache_store(keys, values, key_pages, value_pages, slots)
@@ -227,7 +248,8 @@ def paged_attention(q: torch.Tensor, key_pages: torch.Tensor, value_pages: torch
     request.  scale defaults to head size ** -0.5.  Returns dict(out, lse), lse None unless wanted.
     `workspace` (attention_workspace()) defaults to one that this module keeps for each stream, or, in a
     captured call, to one of the graph's own, which costs the graph a fill of 64 KB for each call and which attention_check
-    cannot see; calls that may overlap need one each."""
+    cannot see; calls that may overlap need one each.  There is no backward pass: results of inputs that ask for a
+    gradient raise when one is taken through them."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return paged_attention(q, key_pages, value_pages, tables, lengths, starts, max_new, scale, causal, window, softcap, slopes, want_lse,
@@ -269,4 +291,5 @@ def paged_attention(q: torch.Tensor, key_pages: torch.Tensor, value_pages: torch
     st = _call(lib.gorio_paged_attention, desc, index)
     if st:
         _fail(lib, st)
+    out, lse = _without_gradient(out, lse, (q, key_pages, value_pages, slopes))
     return dict(out=out, lse=lse)
