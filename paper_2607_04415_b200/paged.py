@@ -212,6 +212,12 @@ def attention_workspace(device=None) -> torch.Tensor:
     return ws
 
 
+def _workspace(lib, t, index):
+    if not isinstance(t, torch.Tensor) or t.get_device() != index or t.dtype is not torch.uint8 or not t.is_contiguous() or (
+            t.numel() < lib.gorio_attention_workspace_bytes(index)):
+        raise _invalid("workspace must come from attention_workspace() for this device")
+
+
 def attention_check(workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """Raises GorioError if a paged_attention call with this workspace (default: the current stream's) ran into the time
     limit of a wait inside its kernel (gorio_attention_check).  Waits for the stream."""
@@ -223,7 +229,9 @@ def attention_check(workspace: Optional[torch.Tensor] = None, stream=None) -> No
         workspace = _WORKSPACES.get((torch.cuda.current_device(), _raw_stream(torch.cuda.current_device())))
         if workspace is None:
             return
-    st = _call(lib.gorio_attention_check, workspace.data_ptr(), workspace.device.index)
+    index = _cuda_index("workspace", workspace)
+    _workspace(lib, workspace, index)
+    st = _call(lib.gorio_attention_check, workspace.data_ptr(), index)
     if st:
         _fail(lib, st)
 
@@ -280,9 +288,8 @@ def paged_attention(q: torch.Tensor, key_pages: torch.Tensor, value_pages: torch
     lse = q.new_empty((t, heads), dtype=torch.float32) if want_lse else None
     if workspace is None:
         workspace = _stream_workspace(index)
-    elif workspace.get_device() != index or workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or (
-            workspace.numel() < lib.gorio_attention_workspace_bytes(index)):
-        raise _invalid("workspace must come from attention_workspace() for this device")
+    else:
+        _workspace(lib, workspace, index)
     desc = _ATTENTION.pack(q.data_ptr(), key_pages.data_ptr(), value_pages.data_ptr(), out.data_ptr(), lse.data_ptr() if want_lse else 0,
                            tables.data_ptr(), lengths.data_ptr(), starts.data_ptr(), 0 if slopes is None else slopes.data_ptr(),
                            workspace.data_ptr(), qs[0], qs[1], os[0], os[1], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], row,

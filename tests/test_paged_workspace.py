@@ -74,3 +74,21 @@ def test_calls_on_two_streams_overlap(gorio):
     torch.cuda.synchronize()
     for k, g in got + list(enumerate(held)):
         assert torch.equal(g["out"], want[k]["out"]) and torch.equal(g["lse"], want[k]["lse"])
+
+
+def test_check_refuses_what_is_no_workspace(gorio):
+    for bad in (torch.zeros(1 << 20, dtype=torch.uint8), [0] * 10, 7):
+        with pytest.raises(gorio.GorioError) as e:
+            gorio.attention_check(bad)
+        assert e.value.status == 1 and "workspace" in str(e.value)
+
+
+@pytest.mark.gpu
+def test_check_refuses_tensors_that_are_no_workspace(gorio):
+    """It reads a word 64 KB from the start and, where that is not 0, clears them: of a smaller tensor, its neighbours' memory."""
+    good = gorio.attention_workspace()
+    for bad in (good[:100], good[: 1 << 16], good.view(torch.int32), good[::2], torch.zeros((2, 2), device="cuda")):
+        with pytest.raises(gorio.GorioError) as e:
+            gorio.attention_check(bad)
+        assert e.value.status == 1
+    gorio.attention_check(good)
