@@ -398,7 +398,7 @@ int gorio_page_tables(const gorio_page_tables_desc *d, void *cuda_stream);
  * slot = slots[t], and the same for values.  Negative slots are skipped.  Two tokens of the same slot:
  * either may win.  16-bit elements; the head's elements are contiguous everywhere.
  * Preconditions: dim a multiple of 8, every stride a multiple of 8, pointers 16-byte aligned,
- * n_pages * page_size < 2^31.
+ * n_pages * page_size < 2^31, n_tokens < 2^31.
  */
 typedef struct {
   const void *keys, *values;

@@ -94,6 +94,7 @@ extern "C" int gorio_cache_store(const gorio_cache_store_desc *d, void *cuda_str
   if (strides & 7) return bad("cache store: every stride must be a multiple of 8 elements");
   if (!aligned(d->keys, 16) || !aligned(d->values, 16) || !aligned(d->key_pages, 16) || !aligned(d->value_pages, 16))
     return bad("cache store: keys, values and pages must be 16-byte aligned");
+  if (d->n_tokens >= (1u << 31)) return bad("cache store: at most 2^31 - 1 tokens");        // the kernel counts past them in 32 bits
   if (d->n_heads > 65536 || d->dim > 65536 || (uint64_t)d->n_tokens * d->n_heads * d->dim >= (1ull << 40))
     return bad("cache store: too large");
   return launched(launch_cache_store(*d, (cudaStream_t)cuda_stream), "cache store");
