@@ -161,6 +161,10 @@ extern "C" int gorio_paged_attention(const gorio_paged_attention_desc *d, void *
   a.q_t = d->q_token_stride; a.q_h = d->q_head_stride; a.o_t = d->o_token_stride; a.o_h = d->o_head_stride;
   a.k_p = d->kp_page_stride; a.k_h = d->kp_head_stride; a.k_t = d->kp_token_stride;
   a.v_p = d->vp_page_stride; a.v_h = d->vp_head_stride; a.v_t = d->vp_token_stride;
+  if (d->n_pages == 0) {                                     // nothing is read, but the copies of no bytes name an address
+    a.kp = a.vp = d->workspace;
+    a.k_p = a.k_h = a.k_t = a.v_p = a.v_h = a.v_t = 0;
+  }
   a.tab_r = d->table_stride;
   a.n_req = d->n_requests; a.n_tok = d->n_tokens; a.hq = d->n_heads; a.hkv = d->n_kv_heads; a.group = d->n_heads / d->n_kv_heads;
   a.page = d->page_size; a.n_pages = d->n_pages; a.width = d->table_width;
