@@ -85,6 +85,14 @@ def _cuda_index(name, t):
     return t.get_device()
 
 
+def _on(stream, name, t):
+    """The context of a `stream` argument, which has to be one of the tensors' device: work would go to that device's current stream."""
+    index = _cuda_index(name, t)
+    if getattr(stream, "device_index", None) != index:
+        raise _invalid(f"stream must be a stream of cuda:{index}, where {name} lives")
+    return torch.cuda.stream(stream)
+
+
 def _call(entry, desc, device_index):
     """The C call on the current stream of the tensors' device, which is made current for it."""
     s = _raw_stream(device_index)
@@ -129,7 +137,7 @@ def page_tables(lengths: torch.Tensor, new_lens: torch.Tensor, tables: torch.Ten
     positions, requests of each new token, starts [requests + 1], lengths after the step, served,
     free_count after the step, and tables.  Requests that find no pages are not served: slots -1."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream, "lengths", lengths):
             return page_tables(lengths, new_lens, tables, free_pages, free_count, page_size, n_tokens)
     lib = load_library()
     index = _cuda_index("lengths", lengths)
@@ -162,7 +170,7 @@ def cache_store(keys: torch.Tensor, values: torch.Tensor, key_pages: torch.Tenso
     """Stores new keys and values, [tokens, heads, head size], to their slots of the pages in place
     (gorio_cache_store).  Tokens of a negative slot are skipped.  Numbers are stored, without their autograd history."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream, "key_pages", key_pages):
             return cache_store(keys, values, key_pages, value_pages, slots)
     lib = load_library()
     index = _cuda_index("key_pages", key_pages)
@@ -222,8 +230,11 @@ def attention_check(workspace: Optional[torch.Tensor] = None, stream=None) -> No
     """Raises GorioError if a paged_attention call with this workspace (default: the current stream's) ran into the time
     limit of a wait inside its kernel (gorio_attention_check).  Waits for the stream."""
     if stream is not None:
+        if workspace is not None:
+            with _on(stream, "workspace", workspace):
+                return attention_check(workspace)
         with torch.cuda.stream(stream):
-            return attention_check(workspace)
+            return attention_check()
     lib = load_library()
     if workspace is None:
         workspace = _WORKSPACES.get((torch.cuda.current_device(), _raw_stream(torch.cuda.current_device())))
@@ -259,7 +270,7 @@ def paged_attention(q: torch.Tensor, key_pages: torch.Tensor, value_pages: torch
     cannot see; calls that may overlap need one each.  There is no backward pass: results of inputs that ask for a
     gradient raise when one is taken through them."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream, "q", q):
             return paged_attention(q, key_pages, value_pages, tables, lengths, starts, max_new, scale, causal, window, softcap, slopes, want_lse,
                                    out, workspace)
     lib = load_library()

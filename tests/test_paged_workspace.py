@@ -92,3 +92,23 @@ def test_check_refuses_tensors_that_are_no_workspace(gorio):
             gorio.attention_check(bad)
         assert e.value.status == 1
     gorio.attention_check(good)
+
+
+def test_streams_of_another_device_are_refused(gorio, monkeypatch):
+    """The calls would run on the current stream of the tensors' device instead, ordered after nothing that `stream` holds."""
+    from paper_2607_04415_b200 import paged
+
+    class Stream:                                             # of cuda:1
+        device_index = 1
+    entered = []
+    monkeypatch.setattr(torch.cuda, "Stream", Stream)
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: entered.append(s))
+    monkeypatch.setattr(paged, "_cuda_index", lambda name, t: 0)
+    i, x = torch.zeros(2, dtype=torch.int32), torch.zeros(1)
+    for call in (lambda s: gorio.page_tables(i, i, i, i, i, 16, 0, stream=s), lambda s: gorio.cache_store(x, x, x, x, x, stream=s),
+                 lambda s: gorio.paged_attention(x, x, x, i, i, i, 1, stream=s), lambda s: gorio.attention_check(x, stream=s)):
+        for stream in (Stream(), 12345):
+            with pytest.raises(gorio.GorioError) as e:
+                call(stream)
+            assert e.value.status == 1 and "stream" in str(e.value)
+    assert not entered
