@@ -23,6 +23,8 @@ _COUNTER_BYTES = 1 << 16      # the part of an attention workspace that starts a
 _WORKSPACES = {}              # (device, stream) -> workspace; calls on one stream do not overlap
 
 _raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch._C._cuda_getDevice
+_current_stream_captured = torch._C._cuda_isCurrentStreamCapturing
 
 
 def _fail(lib, status):
@@ -96,7 +98,7 @@ def _on(stream, name, t):
 def _call(entry, desc, device_index):
     """The C call on the current stream of the tensors' device, which is made current for it."""
     s = _raw_stream(device_index)
-    was = torch._C._cuda_getDevice()
+    was = _current_device()
     if was == device_index:
         return entry(desc, s)
     torch._C._cuda_setDevice(device_index)
@@ -120,9 +122,7 @@ class _NoBackward(torch.autograd.Function):
 
 def _without_gradient(out, lse, inputs):
     """The results as they are, or, where an input asks for a gradient, as results whose backward pass raises."""
-    q, key_pages, value_pages, slopes = inputs
-    if (q.requires_grad or key_pages.requires_grad or value_pages.requires_grad or (slopes is not None and slopes.requires_grad)) and (
-            torch.is_grad_enabled()):
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in inputs):
         return _NoBackward.apply(out, lse, *inputs)
     return out, lse
 
@@ -188,18 +188,13 @@ def cache_store(keys: torch.Tensor, values: torch.Tensor, key_pages: torch.Tenso
         _fail(lib, st)
 
 
-def _capturing(index):
-    """Whether the current stream of a device is being captured into a graph."""
-    if torch._C._cuda_getDevice() == index:
-        return torch._C._cuda_isCurrentStreamCapturing()
-    with torch.cuda.device(index):
-        return torch._C._cuda_isCurrentStreamCapturing()
-
-
 def _stream_workspace(index):
     """The workspace that this module keeps for the current stream of a device.  While that stream is captured, always a new one, which
     belongs to the graph (its zeroing is captured too): a replay may run beside calls on the stream, or beside other graphs of it."""
-    if _capturing(index):
+    if _current_device() != index:
+        with torch.cuda.device(index):
+            return _stream_workspace(index)
+    if _current_stream_captured():
         return attention_workspace(torch.device("cuda", index))
     key = (index, _raw_stream(index))
     ws = _WORKSPACES.get(key)
@@ -309,5 +304,6 @@ def paged_attention(q: torch.Tensor, key_pages: torch.Tensor, value_pages: torch
     st = _call(lib.gorio_paged_attention, desc, index)
     if st:
         _fail(lib, st)
-    out, lse = _without_gradient(out, lse, (q, key_pages, value_pages, slopes))
+    if q.requires_grad or key_pages.requires_grad or value_pages.requires_grad or slopes is not None:      # most calls need no more
+        out, lse = _without_gradient(out, lse, (q, key_pages, value_pages, slopes))
     return dict(out=out, lse=lse)

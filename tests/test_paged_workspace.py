@@ -19,9 +19,8 @@ def test_a_captured_call_never_takes_the_streams_workspace(gorio, monkeypatch):
     monkeypatch.setattr(paged, "attention_workspace", lambda device=None: made.append(object()) or made[-1])
     monkeypatch.setattr(paged, "_raw_stream", lambda index: 77)
     monkeypatch.setattr(paged, "_WORKSPACES", {})
-    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
-    monkeypatch.setattr(torch._C, "_cuda_isCurrentStreamCapturing", lambda: state.capturing, raising=False)
-    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: state.capturing)
+    monkeypatch.setattr(paged, "_current_device", lambda: 0)
+    monkeypatch.setattr(paged, "_current_stream_captured", lambda: state.capturing)
     kept = paged._stream_workspace(0)
     assert paged._stream_workspace(0) is kept
     state.capturing = True
