@@ -26,7 +26,7 @@
 // see and others do not, warp 10 puts zeros in their place before the product, and the rows that see them add
 // them at the end (add_odd).
 //
-// 2048 tokens over 18432 keys (32 heads of 128, 8 key heads, bfloat16) take 537 us sustained, 1.09 PFLOP/s, 476 us in a burst.
+// 2048 tokens over 18432 keys (32 heads of 128, 8 key heads, bfloat16) take 545 us sustained, 1.07 PFLOP/s, 484 us in a burst.
 #include "paged/common.cuh"
 #include "paged/tensor.cuh"
 
