@@ -421,7 +421,8 @@ int gorio_cache_store(const gorio_cache_store_desc *d, void *cuda_stream);
  * bits; the weights are rounded to the cache's type for the sum over values, and out once at the end.
  * A capped score is off by at most some 2^-20 of itself (under caps up to 64: or 2^-22 of the cap), however large the cap.
  * What a query does not see has no effect on its result, whatever it holds (NaN included).  Rows of q that
- * belong to no request are not read and their results not written.
+ * belong to no request are not read and their results not written.  An infinite value under a weight that is rounded to 0
+ * gives an infinity or NaN.
  *   q, out        [n_tokens][n_heads][dim]; key_pages, value_pages [n_pages][n_kv_heads][page_size][dim],
  *                 in any order of the outer axes (strides); lse f32 [n_tokens][n_heads] or NULL.
  *   tables        i32 [n_requests] rows of table_width entries, table_stride apart.
