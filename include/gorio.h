@@ -451,6 +451,34 @@ typedef struct {
 int gorio_paged_attention(const gorio_paged_attention_desc *d, void *cuda_stream);
 
 /*
+ * Attention of a batch whose requests share prefixes.  Requests group_starts[g] .. group_starts[g+1]-1 form group g, in front of whose
+ * keys stand the same prefix_lengths[g] keys, in the pages of row g of prefix_tables: each is read once for the whole group.  A
+ * request's own keys (own.tables, own.lengths) follow them on its key axis, so that with P = prefix_lengths[g] its prefix's key j
+ * stands at position j, its own key j at P + j and its i-th of n new tokens at P + lengths[r] - n + i.  Mask, window, cap and bias are
+ * those of gorio_paged_attention with these positions, out and lse those of one softmax over both parts; a prefix is causally before every
+ * new token of its group, whatever lengths[r] says.  P need not be a multiple of the page size.  Requests of no group
+ * (before group_starts[0] or from group_starts[n_groups] on) have no prefix.
+ *   own           as for gorio_paged_attention; key_pages and value_pages hold prefixes and own keys; its lengths count own keys only.
+ *   prefix_tables i32 [n_groups] rows of prefix_width entries, prefix_table_stride apart; prefix_lengths i32 [n_groups], cut to what the
+ *                 tables hold.
+ *   group_starts  i32 [n_groups+1], cut to [0, n_requests]; it must not decrease (where it does, results are not defined).
+ *   scratch       gorio_prefix_scratch_bytes() bytes, 256-byte aligned, of any content; free again when the call's kernels have run.
+ * Two kernels, of which the second may begin before the first has ended.  Preconditions: those of gorio_paged_attention, 1 to 2^20 groups,
+ * (prefix_width + table_width) * page_size + n_tokens < 2^31.
+ */
+typedef struct {
+  gorio_paged_attention_desc own;
+  const int32_t *prefix_tables, *prefix_lengths, *group_starts;
+  void *scratch;
+  int64_t prefix_table_stride;
+  uint32_t n_groups, prefix_width;
+} gorio_prefix_attention_desc;
+int gorio_prefix_attention(const gorio_prefix_attention_desc *d, void *cuda_stream);
+
+/* Bytes of the scratch above on CUDA device `cuda_device`; 0 if there is no such device. */
+uint64_t gorio_prefix_scratch_bytes(int cuda_device, uint32_t n_tokens, uint32_t n_heads, uint32_t dim);
+
+/*
  * Whether every call with this workspace went well so far: OK; TIMEOUT if a wait inside a kernel passed its
  * limit (the kernel then ends, its results are not valid); CAPACITY if a call had 2^31
  * or more tiles of keys, hours of work, and was not computed.  Waits for the stream; makes the workspace

@@ -16,3 +16,4 @@ from .binding import (  # noqa: F401
 from .paged import (  # noqa: F401
     attention_check, attention_wait_limit, attention_workspace, cache_store, page_tables, paged_attention,
 )
+from .prefix import prefix_attention  # noqa: F401

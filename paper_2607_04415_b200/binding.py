@@ -17,6 +17,7 @@ EXPORTED_SYMBOLS = [
     "gorio_search_resident_noalloc", "gorio_link_probe",
     "gorio_page_tables", "gorio_cache_store", "gorio_paged_attention", "gorio_attention_check",
     "gorio_attention_workspace_bytes", "gorio_attention_wait_limit",
+    "gorio_prefix_attention", "gorio_prefix_scratch_bytes",
 ]
 
 STATUS_NAMES = {0: "OK", 1: "INVALID_ARG", 2: "CUDA", 3: "NOMEM", 4: "STATE", 5: "TIMEOUT",
@@ -99,12 +100,14 @@ def load_library():
     for name in EXPORTED_SYMBOLS:
         if name not in ("gorio_status_str", "gorio_last_error"):
             getattr(lib, name).restype = ctypes.c_int
-    for name in ("gorio_page_tables", "gorio_cache_store", "gorio_paged_attention"):
+    for name in ("gorio_page_tables", "gorio_cache_store", "gorio_paged_attention", "gorio_prefix_attention"):
         getattr(lib, name).argtypes = [ctypes.c_char_p, vp]      # a packed descriptor, a stream
     lib.gorio_attention_check.argtypes = [vp, vp]
     lib.gorio_attention_wait_limit.argtypes = [ctypes.c_uint64]
     lib.gorio_attention_workspace_bytes.argtypes = [ctypes.c_int]
     lib.gorio_attention_workspace_bytes.restype = ctypes.c_uint64
+    lib.gorio_prefix_scratch_bytes.argtypes = [ctypes.c_int, u32, u32, u32]
+    lib.gorio_prefix_scratch_bytes.restype = ctypes.c_uint64
     _LIB = lib
     return lib
 

@@ -8,11 +8,12 @@ import sys
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libgorio.so")
-SOURCES = ["gorio_api.cu", "search_kernels.cu", "noalloc_entry.cu", "paged_api.cu", "paged_tables.cu", "paged_rows.cu", "paged_chunk.cu"]
+SOURCES = ["gorio_api.cu", "search_kernels.cu", "noalloc_entry.cu", "paged_api.cu", "paged_tables.cu", "paged_rows.cu", "paged_chunk.cu",
+           "prefix_rows.cu", "prefix_chunk.cu", "prefix_chunk_own.cu"]
 HEADERS = ["gorio_internal.h", os.path.join("..", "..", "include", "gorio.h")] + [
     os.path.join("device", f) for f in ("mem.cuh", "queue.cuh", "page_cache.cuh", "scoring.cuh", "arrival.cuh", "batch.cuh",
                                         "list.cuh", "pq.cuh", "scheduler.cuh", "resident.cuh")] + [
-    os.path.join("paged", f) for f in ("common.cuh", "mma.cuh", "tensor.cuh", "entries.h")]
+    os.path.join("paged", f) for f in ("common.cuh", "mma.cuh", "tensor.cuh", "rows.cuh", "chunk.cuh", "entries.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-pthread"]
 
@@ -62,12 +63,13 @@ def build(force: bool = False, verbose: bool = False) -> str:
             if not force and not _stale():      # another process built it while this one waited
                 return LIB_PATH
             nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-            objs = []
-            for src in SOURCES:
-                obj = os.path.join(CSRC, src.replace(".cu", ".o"))
-                cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-c", os.path.join(CSRC, src), "-o", obj]
-                subprocess.check_call(cmd)
-                objs.append(obj)
+            objs = [os.path.join(CSRC, src.replace(".cu", ".o")) for src in SOURCES]
+
+            def compile_one(src, obj):
+                subprocess.check_call([nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-c", os.path.join(CSRC, src), "-o", obj])
+            from concurrent.futures import ThreadPoolExecutor
+            with ThreadPoolExecutor(max(1, min(len(SOURCES), os.cpu_count() or 1))) as pool:
+                list(pool.map(compile_one, SOURCES, objs))
             tmp = LIB_PATH + ".tmp"
             subprocess.check_call([nvcc, "-shared", "-o", tmp] + objs + ["-lcudart"])
             os.replace(tmp, LIB_PATH)           # readers never see a half-written library

@@ -39,6 +39,36 @@ struct Attn {
   u32 wait_ticks;              // of 1024 ns: a wait inside the chunk kernel gives up when it has lasted as long
 };
 
+// Attention over keys that the requests of a group share takes two kernels.  The first, over the shared keys, sees the groups as its
+// requests (Attn's tables, lengths and n_req are theirs, `starts` are the requests' rows) and leaves each row's weighted sum of
+// values, its maximum and its sum of weights in 32 bits.  The second, over each request's own keys, joins them to its own
+// before it writes a row.  It may begin while the first still runs (and then has its own counters and parts), and waits for its end
+// before it reads what the first has left.
+struct PrefixAttn : Attn {
+  const int *group_starts;     // [n_req + 1]: the requests of each group
+  const int *own_lengths;      // [n_members]
+  u32 n_members, own_places;   // requests; the most keys of its own that one can have
+  float *mid_o;                // [n_tok][hq][dim]
+  float2 *mid_ml;              // [n_tok][hq]: maximum in units of log2, sum
+};
+struct OwnAttn : Attn {
+  const int *group_starts;
+  u32 n_groups;
+  const float *mid_o;
+  const float2 *mid_ml;
+};
+constexpr u32 kOwnCounters = (u32)(kCounterBytes / 8);     // the second kernel's counters: the other half
+
+__device__ __forceinline__ u32 *error_word(const Attn &a) { return a.arrived + kErrorWord; }
+__device__ __forceinline__ u32 *error_word(const OwnAttn &a) { return a.arrived + (kErrorWord - kOwnCounters); }
+
+// The kernel that was launched before this one with leave to overlap has ended, and what it wrote is visible.
+__device__ __forceinline__ void wait_for_first(const Attn &) {}
+__device__ __forceinline__ void wait_for_first(const OwnAttn &) { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// The next kernel of the stream may begin where this one leaves room.
+__device__ __forceinline__ void let_second_begin(const Attn &) {}
+__device__ __forceinline__ void let_second_begin(const PrefixAttn &) { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // One request as the kernels see it: keys it can have at most, its new tokens and where their rows
 // start.  Bad lengths or starts are cut to what the tables and the query tensor hold, so that no
 // access leaves them.
@@ -55,6 +85,50 @@ __device__ __forceinline__ Request request_at(const Attn &a, u32 r) {
   const int e = s1 > (int)a.n_tok ? (int)a.n_tok : s1;
   x.n = e > x.q0 ? e - x.q0 : 0;
   return x;
+}
+
+// First row of the g-th group's requests, cut like the rest.
+__device__ __forceinline__ int group_row(const int *group_starts, const int *starts, u32 members, u32 n_tok, u32 g) {
+  const int r = group_starts[g], s = starts[r < 0 ? 0 : r > (int)members ? (int)members : r];
+  return s < 0 ? 0 : s > (int)n_tok ? (int)n_tok : s;
+}
+
+__device__ __forceinline__ Request request_at(const PrefixAttn &a, u32 g) {
+  Request x;
+  const i64 cap = (i64)a.width * a.page;
+  const int l = a.lengths[g];
+  x.len = l < 0 ? 0 : (i64)l > cap ? (int)cap : l;
+  x.q0 = group_row(a.group_starts, a.starts, a.n_members, a.n_tok, g);
+  const int e = group_row(a.group_starts, a.starts, a.n_members, a.n_tok, g + 1);
+  x.n = e > x.q0 ? e - x.q0 : 0;
+  return x;
+}
+
+// The rows that belong to a group: the others have no shared keys, and the first kernel leaves nothing for them.
+struct NoRows {};
+struct CoveredRows {
+  int from, to;
+};
+__device__ __forceinline__ NoRows covered_rows(const Attn &) { return NoRows{}; }
+__device__ __forceinline__ CoveredRows covered_rows(const OwnAttn &a) {
+  return CoveredRows{group_row(a.group_starts, a.starts, a.n_req, a.n_tok, 0), group_row(a.group_starts, a.starts, a.n_req, a.n_tok, a.n_groups)};
+}
+
+// Where the tok-th new token of a request stands on its key axis.
+__device__ __forceinline__ int position_of(const Attn &, const Request &x, int tok) { return x.len - x.n + tok; }
+// Of a group, whose tokens are of several requests: behind all shared keys and those that its own request holds before it.  Only
+// windows and biases ask for it, so that a search for the request is made for those calls alone.
+__device__ __forceinline__ int position_of(const PrefixAttn &a, const Request &x, int tok) {
+  if (!a.window && !a.slopes) return x.len;
+  const int row = x.q0 + tok;
+  u32 lo = 0, hi = a.n_members;                          // the last request that starts at or before the row
+  while (hi - lo > 1) {
+    const u32 mid = (lo + hi) / 2;
+    if (a.starts[mid] <= row) lo = mid; else hi = mid;
+  }
+  const int s0 = a.starts[lo], s1 = a.starts[lo + 1], own = a.own_lengths[lo];
+  const int n = (s1 > (int)a.n_tok ? (int)a.n_tok : s1) - (s0 < 0 ? 0 : s0);
+  return x.len + (own < 0 ? 0 : (u32)own > a.own_places ? (int)a.own_places : own) - n + (row - (s0 < 0 ? 0 : s0));
 }
 
 // A unit is up to ROWS rows -- (token, query head of the group) pairs, token outer -- of one request
@@ -126,8 +200,8 @@ __device__ __forceinline__ u32 unit_places(u32 tiles, u32 fill) { return fill ? 
 struct Places {
   u32 sum, units, longest;
 };
-template <int ROWS, int TK, int OVER>
-__device__ __forceinline__ Places request_places(const Attn &a, u32 r, bool have, u32 fill) {
+template <int ROWS, int TK, int OVER, typename A>
+__device__ __forceinline__ Places request_places(const A &a, u32 r, bool have, u32 fill) {
   const u32 lane = threadIdx.x & 31;
   Request q{0, 0, 0};
   if (have) q = request_at(a, r);
@@ -170,8 +244,8 @@ __device__ __forceinline__ u32 warp_scan(u32 x) {
 
 // Sets the cursor to the place `offset` places after the first of request r.  Warp-collective, the same
 // for all warps.
-template <int ROWS, int TK, int OVER>
-__device__ __forceinline__ Cursor cursor_in(const Attn &a, u32 r, u32 offset, u32 fill) {
+template <int ROWS, int TK, int OVER, typename A>
+__device__ __forceinline__ Cursor cursor_in(const A &a, u32 r, u32 offset, u32 fill) {
   const u32 lane = threadIdx.x & 31;
   Cursor c;
   c.r = r;
@@ -202,8 +276,8 @@ __device__ __forceinline__ Cursor cursor_in(const Attn &a, u32 r, u32 offset, u3
 }
 
 // The next unit after the cursor's; false at the end of the line.
-template <int ROWS, int TK>
-__device__ __forceinline__ bool next_unit(const Attn &a, Cursor &c) {
+template <int ROWS, int TK, typename A>
+__device__ __forceinline__ bool next_unit(const A &a, Cursor &c) {
   c.at = 0;
   if (c.m + 1 < unit_count<ROWS>(a, c.req.n)) {
     ++c.m;
@@ -224,8 +298,8 @@ __device__ __forceinline__ bool next_unit(const Attn &a, Cursor &c) {
 
 // Moves the cursor from a place without work, or past the unit's last tile, to the next tile; `left`: places of the block's
 // share from the cursor on, 0 at its end.
-template <int ROWS, int TK, int OVER>
-__device__ __forceinline__ void settle(const Attn &a, Cursor &c, u32 &left, u32 fill) {
+template <int ROWS, int TK, int OVER, typename A>
+__device__ __forceinline__ void settle(const A &a, Cursor &c, u32 &left, u32 fill) {
   while (left && c.at >= c.span.tiles) {
     const u32 skip = unit_places<OVER>((u32)c.span.tiles, fill) - (u32)c.at;
     if (skip >= left) { left = 0; return; }
@@ -243,8 +317,8 @@ struct Plan {
 
 // By a block of NT threads.  `spread` times the square root of the longest unit: the least share of filled-up units.
 // Requests are dealt out to all warps, each a run of consecutive ones, since a warp takes those of many units one by one.
-template <int ROWS, int TK, int OVER, int NT>
-__device__ __forceinline__ Plan block_plan(const Attn &a, PlanShared &sh, float spread) {
+template <int ROWS, int TK, int OVER, int NT, typename A>
+__device__ __forceinline__ Plan block_plan(const A &a, PlanShared &sh, float spread) {
   constexpr u32 kWarpsHere = NT / 32;
   const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const u32 run = min(32u, (a.n_req + kWarpsHere - 1) / kWarpsHere), round = run * kWarpsHere;
@@ -277,7 +351,7 @@ __device__ __forceinline__ Plan block_plan(const Attn &a, PlanShared &sh, float 
   all_units *= a.hkv;
   const u64 line = tiles + all_units * OVER;
   if (line >= (1ull << 31)) {                            // a call of hours
-    if (tid == 0) a.arrived[kErrorWord] = 2;
+    if (tid == 0) *error_word(a) = 2;
     return p;
   }
   if (tiles == 0) return p;
@@ -329,10 +403,34 @@ constexpr u32 kMaxDim = 128;
 inline u64 part_ml_bytes(u32 sms) { return (u64)sms * kPartRowsPerSm * 2 * sizeof(float); }
 inline u64 part_bytes(u32 sms) { return part_ml_bytes(sms) + (u64)sms * kPartRowsPerSm * kMaxDim * sizeof(float); }
 
-// launchers
+// launchers, of each kernel for each of its places
 // False where no tensor map of the pages can be made (strides or addresses that it does not hold): nothing ran.
 bool launch_chunk(const Attn &a, int dtype, int dim, u32 sms, cudaStream_t s, cudaError_t *e);
 cudaError_t launch_rows(const Attn &a, int dtype, int dim, u32 sms, cudaStream_t s);
+bool launch_chunk(const PrefixAttn &a, int dtype, int dim, u32 sms, cudaStream_t s, cudaError_t *e);
+cudaError_t launch_rows(const PrefixAttn &a, int dtype, int dim, u32 sms, cudaStream_t s);
+bool launch_chunk(const OwnAttn &a, int dtype, int dim, u32 sms, cudaStream_t s, cudaError_t *e);
+cudaError_t launch_rows(const OwnAttn &a, int dtype, int dim, u32 sms, cudaStream_t s);
+
+// A kernel that reads what a first one leaves is launched with leave to begin before that one has ended.
+template <typename A>
+struct Overlaps { static constexpr bool value = false; };
+template <>
+struct Overlaps<OwnAttn> { static constexpr bool value = true; };
+template <typename A, typename... Args>
+cudaError_t launch_kernel(void (*kernel)(Args...), u32 blocks, u32 threads, size_t shared, cudaStream_t s, Args... args) {
+  cudaLaunchAttribute overlap{};
+  overlap.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  overlap.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t c{};
+  c.gridDim = blocks;
+  c.blockDim = threads;
+  c.dynamicSmemBytes = shared;
+  c.stream = s;
+  c.attrs = &overlap;
+  c.numAttrs = Overlaps<A>::value ? 1 : 0;
+  return cudaLaunchKernelEx(&c, kernel, args...);
+}
 
 }  // namespace paged
 }  // namespace gorio

@@ -115,22 +115,104 @@ __device__ __forceinline__ float capped_log2(float dot, float in, float out, flo
   return fabsf(w) < kCapSeries ? small : large;
 }
 
-// Writes four columns of a finished row: acc / sum, rounded once.  A row that sees no key has sum 0 and gives 0 and
+// How a row ends.  `m` (in units of log2) and `l` are its maximum and sum: weights count from 2^m.  Alone a row is divided by its sum; of
+// the shared keys it is left as it is; of a request's own keys it is first joined to what was left of the shared ones.
+struct RowEnd {
+  float f;
+  __device__ __forceinline__ RowEnd(const Attn &a, const NoRows &, i64 tok, int head, int, float m, float l, bool first) {
+    f = l == 0.0f ? 0.0f : 1.0f / l;
+    if (first && a.lse) a.lse[tok * a.hq + head] = l == 0.0f ? -INFINITY : m * kLn2 + logf(l);
+  }
+  template <typename T>
+  __device__ __forceinline__ void write4(const Attn &a, i64 tok, int head, int col, float4 o) const {
+    *(uint2 *)((u16 *)a.out + tok * a.o_t + (i64)head * a.o_h + col) = make_uint2(pack2<T>(o.x * f, o.y * f), pack2<T>(o.z * f, o.w * f));
+  }
+  template <typename T>
+  __device__ __forceinline__ void write32(const Attn &a, i64 tok, int head, int col, const float *o) const {
+    uint4 *to = (uint4 *)((u16 *)a.out + tok * a.o_t + (i64)head * a.o_h + col);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      to[k] = make_uint4(pack2<T>(o[8 * k] * f, o[8 * k + 1] * f), pack2<T>(o[8 * k + 2] * f, o[8 * k + 3] * f), pack2<T>(o[8 * k + 4] * f, o[8 * k + 5] * f),
+                         pack2<T>(o[8 * k + 6] * f, o[8 * k + 7] * f));
+  }
+};
+
+struct PrefixRowEnd {
+  float *to;
+  __device__ __forceinline__ PrefixRowEnd(const PrefixAttn &a, const NoRows &, i64 tok, int head, int dim, float m, float l, bool first) {
+    to = a.mid_o + (tok * a.hq + head) * dim;
+    if (first) a.mid_ml[tok * a.hq + head] = make_float2(m, l);
+  }
+  template <typename T>
+  __device__ __forceinline__ void write4(const PrefixAttn &, i64, int, int col, float4 o) const { *(float4 *)(to + col) = o; }
+  template <typename T>
+  __device__ __forceinline__ void write32(const PrefixAttn &, i64, int, int col, const float *o) const {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) *(float4 *)(to + col + 4 * k) = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+  }
+};
+
+struct OwnRowEnd {
+  float f, g;                  // of its own sums, and of those over the shared keys
+  const float *from;           // NULL: none
+  __device__ __forceinline__ OwnRowEnd(const OwnAttn &a, const CoveredRows &rows, i64 tok, int head, int dim, float m, float l, bool first) {
+    wait_for_first(a);
+    from = nullptr;
+    float2 mid = make_float2(-INFINITY, 0.0f);
+    if (tok >= rows.from && tok < rows.to) {
+      mid = __ldcg(a.mid_ml + tok * a.hq + head);
+      from = a.mid_o + (tok * a.hq + head) * dim;
+    }
+    const float top = fmaxf(m, mid.x), base = top == -INFINITY ? 0.0f : top;
+    f = exp2_approx(m - base);
+    g = exp2_approx(mid.x - base);
+    const float sum = f * l + g * mid.y, inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
+    if (first && a.lse) a.lse[tok * a.hq + head] = sum == 0.0f ? -INFINITY : top * kLn2 + logf(sum);
+    f *= inverse;
+    g *= inverse;
+  }
+  __device__ __forceinline__ float4 joined(float4 o, int col) const {
+    const float4 x = from ? __ldcg((const float4 *)(from + col)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    return make_float4(o.x * f + x.x * g, o.y * f + x.y * g, o.z * f + x.z * g, o.w * f + x.w * g);
+  }
+  template <typename T>
+  __device__ __forceinline__ void write4(const OwnAttn &a, i64 tok, int head, int col, float4 o) const {
+    o = joined(o, col);
+    *(uint2 *)((u16 *)a.out + tok * a.o_t + (i64)head * a.o_h + col) = make_uint2(pack2<T>(o.x, o.y), pack2<T>(o.z, o.w));
+  }
+  template <typename T>
+  __device__ __forceinline__ void write32(const OwnAttn &a, i64 tok, int head, int col, const float *o) const {
+    uint4 *to = (uint4 *)((u16 *)a.out + tok * a.o_t + (i64)head * a.o_h + col);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float4 x = joined(make_float4(o[8 * k], o[8 * k + 1], o[8 * k + 2], o[8 * k + 3]), col + 8 * k);
+      const float4 y = joined(make_float4(o[8 * k + 4], o[8 * k + 5], o[8 * k + 6], o[8 * k + 7]), col + 8 * k + 4);
+      to[k] = make_uint4(pack2<T>(x.x, x.y), pack2<T>(x.z, x.w), pack2<T>(y.x, y.y), pack2<T>(y.z, y.w));
+    }
+  }
+};
+
+template <typename A>
+struct EndOf { typedef RowEnd type; };
+template <>
+struct EndOf<PrefixAttn> { typedef PrefixRowEnd type; };
+template <>
+struct EndOf<OwnAttn> { typedef OwnRowEnd type; };
+
+// Writes four columns of a finished row, rounded once.  A row that sees no key has sum 0 and gives 0 and
 // -inf.  `row` counts (token, head of the group) pairs of the request, `top` is in units of log2.
-template <typename T>
-__device__ __forceinline__ void finish_row(const Attn &a, int q0, i64 row, u32 h, int col, float4 acc, float top, float sum) {
+template <typename T, int D, typename A, typename Rows>
+__device__ __forceinline__ void finish_row(const A &a, const Rows &rows, int q0, i64 row, u32 h, int col, float4 acc, float top, float sum) {
   const int tok = (int)(row / a.group), head = (int)(row - (i64)tok * a.group) + (int)(h * a.group);
-  const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
-  uint2 v = make_uint2(pack2<T>(acc.x * f, acc.y * f), pack2<T>(acc.z * f, acc.w * f));
-  *(uint2 *)((u16 *)a.out + (i64)(q0 + tok) * a.o_t + (i64)head * a.o_h + col) = v;
-  if (col == 0 && a.lse) a.lse[(i64)(q0 + tok) * a.hq + head] = sum == 0.0f ? -INFINITY : top * kLn2 + logf(sum);
+  const typename EndOf<A>::type end(a, rows, q0 + tok, head, D, top, sum, col == 0);
+  end.template write4<T>(a, q0 + tok, head, col, acc);
 }
 
 // Joins the parts of a unit that blocks i0..i1 left, in the order of the key axis.  Block-collective.  What it costs
 // is waiting for loads, 0.7 us a time, so a thread keeps those of AHEAD parts in flight: the 33 parts of one token over
 // 4097 keys take 22 us in all with 2, 16 with 4, 14 with 8, no less with 16.
-template <typename T, int D, int ROWS, int NT, int ITEMS, int AHEAD>
-__device__ __forceinline__ void join_parts(const Attn &a, const Cursor &c, i64 row0, int rows, u32 i0, u32 i1) {
+template <typename T, int D, int ROWS, int NT, int ITEMS, int AHEAD, typename A, typename Rows>
+__device__ __forceinline__ void join_parts(const A &a, const Rows &covered, const Cursor &c, i64 row0, int rows, u32 i0, u32 i1) {
   const int items = rows * (D / 4);
   for (int x0 = (int)threadIdx.x; x0 < items; x0 += NT * ITEMS) {
     float top[ITEMS], sum[ITEMS];
@@ -173,7 +255,7 @@ __device__ __forceinline__ void join_parts(const Attn &a, const Cursor &c, i64 r
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k) {
       const int x = x0 + k * NT, row = x / (D / 4);
-      if (x < items) finish_row<T>(a, c.req.q0, row0 + row, c.h, (x - row * (D / 4)) * 4, acc[k], top[k], sum[k]);
+      if (x < items) finish_row<T, D>(a, covered, c.req.q0, row0 + row, c.h, (x - row * (D / 4)) * 4, acc[k], top[k], sum[k]);
     }
   }
 }

@@ -127,9 +127,10 @@ extern "C" int gorio_attention_check(void *workspace, void *cuda_stream) {
   return GORIO_ERR_TIMEOUT;
 }
 
-extern "C" int gorio_paged_attention(const gorio_paged_attention_desc *d, void *cuda_stream) {
-  if (!d) return bad("paged attention: null argument");
-  if (d->n_requests == 0 || d->n_tokens == 0) return GORIO_OK;
+namespace {
+
+// Checks of the numbers and addresses of an attention call; its workspace's among them.
+int check_attention(const gorio_paged_attention_desc *d) {
   if (!d->q || !d->out || !d->tables || !d->lengths || !d->starts || !d->workspace) return bad("paged attention: null argument");
   if (d->n_pages && (!d->key_pages || !d->value_pages)) return bad("paged attention: null argument");
   if (d->dtype > GORIO_KV_FP16) return bad("paged attention: unknown dtype");
@@ -149,13 +150,19 @@ extern "C" int gorio_paged_attention(const gorio_paged_attention_desc *d, void *
   if (!aligned(d->q, 16) || !aligned(d->out, 16) || !aligned(d->key_pages, 16) || !aligned(d->value_pages, 16))
     return bad("paged attention: q, out and pages must be 16-byte aligned");
   if (!aligned(d->workspace, 256)) return bad("paged attention: the workspace must be 256-byte aligned");
+  return GORIO_OK;
+}
+
+// SMs of the current device
+int current_sms(int *sms, const char *what) {
   int dev = 0;
   const cudaError_t found = cudaGetDevice(&dev);
-  if (found != cudaSuccess) return launched(found, "paged attention");
-  const int sms = sm_count(dev);
-  if (sms < 1) return launched(cudaErrorInvalidDevice, "paged attention");
+  if (found != cudaSuccess) return launched(found, what);
+  *sms = sm_count(dev);
+  return *sms < 1 ? launched(cudaErrorInvalidDevice, what) : GORIO_OK;
+}
 
-  Attn a{};
+void fill_attention(Attn &a, const gorio_paged_attention_desc *d, int sms) {
   a.q = d->q; a.kp = d->key_pages; a.vp = d->value_pages; a.out = d->out; a.lse = d->lse;
   a.tables = d->tables; a.lengths = d->lengths; a.starts = d->starts; a.slopes = d->slopes;
   a.q_t = d->q_token_stride; a.q_h = d->q_head_stride; a.o_t = d->o_token_stride; a.o_h = d->o_head_stride;
@@ -175,9 +182,81 @@ extern "C" int gorio_paged_attention(const gorio_paged_attention_desc *d, void *
   a.arrived = (u32 *)d->workspace;
   a.part_ml = (float *)((char *)d->workspace + kCounterBytes);
   a.part_o = (float *)((char *)a.part_ml + part_ml_bytes((u32)sms));
-  if (!takes_rows(*d)) {
+}
+
+// One of the two kernels, by the bounds of rows and keys in `d`.
+template <typename A>
+cudaError_t launch_attention(const A &a, const gorio_paged_attention_desc &d, int sms, cudaStream_t s) {
+  if (!takes_rows(d)) {
     cudaError_t e = cudaSuccess;
-    if (launch_chunk(a, (int)d->dtype, (int)d->dim, (u32)sms, (cudaStream_t)cuda_stream, &e)) return launched(e, "paged attention");
+    if (launch_chunk(a, (int)d.dtype, (int)d.dim, (u32)sms, s, &e)) return e;
   }
-  return launched(launch_rows(a, (int)d->dtype, (int)d->dim, (u32)sms, (cudaStream_t)cuda_stream), "paged attention");
+  return launch_rows(a, (int)d.dtype, (int)d.dim, (u32)sms, s);
+}
+
+}  // namespace
+
+extern "C" int gorio_paged_attention(const gorio_paged_attention_desc *d, void *cuda_stream) {
+  if (!d) return bad("paged attention: null argument");
+  if (d->n_requests == 0 || d->n_tokens == 0) return GORIO_OK;
+  int sms = 0, st = check_attention(d);
+  if (st == GORIO_OK) st = current_sms(&sms, "paged attention");
+  if (st != GORIO_OK) return st;
+  Attn a{};
+  fill_attention(a, d, sms);
+  return launched(launch_attention(a, *d, sms, (cudaStream_t)cuda_stream), "paged attention");
+}
+
+namespace {
+
+// What a call on shared keys needs besides the workspace: the second kernel's parts, then the first kernel's results.
+uint64_t mid_ml_bytes(uint64_t rows) { return (rows * sizeof(float2) + 255) / 256 * 256; }
+uint64_t scratch_bytes(int sms, uint64_t rows, uint64_t dim) { return part_bytes((u32)sms) + mid_ml_bytes(rows) + rows * dim * sizeof(float); }
+
+}  // namespace
+
+extern "C" uint64_t gorio_prefix_scratch_bytes(int cuda_device, uint32_t n_tokens, uint32_t n_heads, uint32_t dim) {
+  const int sms = sm_count(cuda_device);
+  return sms ? scratch_bytes(sms, (uint64_t)n_tokens * n_heads, dim) : 0;
+}
+
+extern "C" int gorio_prefix_attention(const gorio_prefix_attention_desc *d, void *cuda_stream) {
+  if (!d) return bad("prefix attention: null argument");
+  const gorio_paged_attention_desc &own = d->own;
+  if (own.n_requests == 0 || own.n_tokens == 0) return GORIO_OK;
+  int sms = 0, st = check_attention(&own);
+  if (st != GORIO_OK) return st;
+  if (!d->prefix_tables || !d->prefix_lengths || !d->group_starts || !d->scratch) return bad("prefix attention: null argument");
+  if (d->n_groups < 1 || d->n_groups > (1u << 20) || d->prefix_width < 1 || (uint64_t)own.page_size * d->prefix_width >= (1ull << 31))
+    return bad("prefix attention: need 1 to 2^20 groups and fewer than 2^31 places in a row of their tables");
+  if (((uint64_t)d->prefix_width + own.table_width) * own.page_size + own.n_tokens >= (1ull << 31))
+    return bad("prefix attention: positions must stay below 2^31");
+  if (!aligned(d->scratch, 256)) return bad("prefix attention: the scratch must be 256-byte aligned");
+  st = current_sms(&sms, "prefix attention");
+  if (st != GORIO_OK) return st;
+
+  const uint64_t rows = (uint64_t)own.n_tokens * own.n_heads;
+  float2 *const mid_ml = (float2 *)((char *)d->scratch + part_bytes((u32)sms));
+  float *const mid_o = (float *)((char *)mid_ml + mid_ml_bytes(rows));
+  PrefixAttn p{};
+  fill_attention(p, &own, sms);
+  p.tables = d->prefix_tables; p.lengths = d->prefix_lengths; p.tab_r = d->prefix_table_stride;
+  p.n_req = d->n_groups; p.width = d->prefix_width;
+  p.causal = 0;                                              // shared keys stand before all new tokens
+  p.group_starts = d->group_starts; p.own_lengths = own.lengths;
+  p.n_members = own.n_requests; p.own_places = own.table_width * own.page_size;
+  p.mid_o = mid_o; p.mid_ml = mid_ml;
+  gorio_paged_attention_desc shared = own;                   // bounds of the first kernel's rows and keys
+  shared.n_requests = d->n_groups; shared.table_width = d->prefix_width; shared.max_new = own.n_tokens;
+  cudaError_t e = launch_attention(p, shared, sms, (cudaStream_t)cuda_stream);
+  if (e != cudaSuccess) return launched(e, "prefix attention");
+
+  OwnAttn o{};
+  fill_attention(o, &own, sms);
+  o.arrived += kOwnCounters;
+  o.part_ml = (float *)d->scratch;
+  o.part_o = (float *)((char *)d->scratch + part_ml_bytes((u32)sms));
+  o.group_starts = d->group_starts; o.n_groups = d->n_groups;
+  o.mid_o = mid_o; o.mid_ml = mid_ml;
+  return launched(launch_attention(o, own, sms, (cudaStream_t)cuda_stream), "prefix attention");
 }
