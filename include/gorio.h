@@ -451,6 +451,54 @@ typedef struct {
 int gorio_paged_attention(const gorio_paged_attention_desc *d, void *cuda_stream);
 
 /*
+ * A quantised cache holds keys and values in 8 bits: each row (a token's numbers of one key head) as codes and a scale,
+ * number = code * scale.  Codes are e4m3 (L = 448; sign, 4 bits of exponent, 3 of mantissa, no infinities) or whole numbers of
+ * 8 bits (L = 127).  The store takes a row's largest magnitude M and writes, all in 32-bit arithmetic,
+ *   scale = M / L,   inverse = L / M,   code = x * inverse rounded to the nearest code, ties to even.
+ * A row with M below 2^-100 is stored as zeros with scale 0; a row with a number that is not finite gets codes 0 and the scale NaN, so
+ * that all of it reads as NaN.  The codes 0x7F and 0xFF of e4m3, which the store does not write, read as 480 and -480.
+ */
+enum { GORIO_CODES_E4M3 = 0, GORIO_CODES_INT8 = 1 };
+
+/*
+ * Rows of a quantised cache and their 16-bit form.  gorio_cache_store_quantized: keys[t][h][:] and values[t][h][:] to slot
+ * slots[t] of the pages, as gorio_cache_store does (negative slots and such outside the cache are skipped; two
+ * tokens of the same slot: either may win, a row's codes and scale may then be of different ones).
+ * gorio_cache_load_quantized: the other way round, keys and values are written: code * scale, rounded to 32 bits and to the type;
+ * zeros for a slot outside the cache.
+ *   keys, values       16-bit [n_tokens][n_heads][dim]; key_pages, value_pages 8-bit [n_pages][n_heads][page_size][dim];
+ *   key_scales, value_scales  f32 [n_pages][n_heads][page_size]; strides count elements.
+ * Preconditions: dim a multiple of 16, at most 256; strides of keys and values multiples of 8, of the pages multiples of 16; pointers to
+ * them 16-byte aligned, to scales 4-byte aligned; n_pages * page_size < 2^31; n_tokens * n_heads < 2^31.
+ */
+typedef struct {
+  void *keys, *values, *key_pages, *value_pages;
+  float *key_scales, *value_scales;
+  const int64_t *slots;
+  int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+  int64_t kp_page_stride, kp_head_stride, kp_token_stride, vp_page_stride, vp_head_stride, vp_token_stride;
+  int64_t ks_page_stride, ks_head_stride, ks_token_stride, vs_page_stride, vs_head_stride, vs_token_stride;
+  uint32_t n_tokens, n_heads, dim, n_pages, page_size, dtype, format, reserved;
+} gorio_quantized_rows_desc;
+int gorio_cache_store_quantized(const gorio_quantized_rows_desc *d, void *cuda_stream);
+int gorio_cache_load_quantized(const gorio_quantized_rows_desc *d, void *cuda_stream);
+
+/*
+ * Attention over a quantised cache: gorio_paged_attention where key_pages and value_pages hold codes, with code * scale for each
+ * number.  attention.dtype is that of q and out; strides of its pages count codes and must be multiples of 16.  Scores
+ * are products of exact codes and of q in 32-bit sums.  A weight is multiplied by its value's scale before it is rounded, once, to
+ * 16 bits, or the value by its scale, rounded once to 11 bits (many rows); a scale counts fully between 2^-80 and 2^80.
+ * A scale that is not a number reaches the queries that see its key, and no others.  Preconditions otherwise as there.
+ */
+typedef struct {
+  gorio_paged_attention_desc attention;
+  const float *key_scales, *value_scales;
+  int64_t ks_page_stride, ks_head_stride, ks_token_stride, vs_page_stride, vs_head_stride, vs_token_stride;
+  uint32_t format, reserved;
+} gorio_quantized_attention_desc;
+int gorio_paged_attention_quantized(const gorio_quantized_attention_desc *d, void *cuda_stream);
+
+/*
  * Attention of a batch whose requests share prefixes.  Requests group_starts[g] .. group_starts[g+1]-1 form group g, in front of whose
  * keys stand the same prefix_lengths[g] keys, in the pages of row g of prefix_tables: each is read once for the whole group.  A
  * request's own keys (own.tables, own.lengths) follow them on its key axis, so that with P = prefix_lengths[g] its prefix's key j

@@ -17,3 +17,4 @@ from .paged import (  # noqa: F401
     attention_check, attention_wait_limit, attention_workspace, cache_store, page_tables, paged_attention,
 )
 from .prefix import prefix_attention  # noqa: F401
+from .quantized import cache_load_quantized, cache_store_quantized, paged_attention_quantized  # noqa: F401

@@ -18,6 +18,7 @@ EXPORTED_SYMBOLS = [
     "gorio_page_tables", "gorio_cache_store", "gorio_paged_attention", "gorio_attention_check",
     "gorio_attention_workspace_bytes", "gorio_attention_wait_limit",
     "gorio_prefix_attention", "gorio_prefix_scratch_bytes",
+    "gorio_cache_store_quantized", "gorio_cache_load_quantized", "gorio_paged_attention_quantized",
 ]
 
 STATUS_NAMES = {0: "OK", 1: "INVALID_ARG", 2: "CUDA", 3: "NOMEM", 4: "STATE", 5: "TIMEOUT",
@@ -100,7 +101,8 @@ def load_library():
     for name in EXPORTED_SYMBOLS:
         if name not in ("gorio_status_str", "gorio_last_error"):
             getattr(lib, name).restype = ctypes.c_int
-    for name in ("gorio_page_tables", "gorio_cache_store", "gorio_paged_attention", "gorio_prefix_attention"):
+    for name in ("gorio_page_tables", "gorio_cache_store", "gorio_paged_attention", "gorio_prefix_attention",
+                 "gorio_cache_store_quantized", "gorio_cache_load_quantized", "gorio_paged_attention_quantized"):
         getattr(lib, name).argtypes = [ctypes.c_char_p, vp]      # a packed descriptor, a stream
     lib.gorio_attention_check.argtypes = [vp, vp]
     lib.gorio_attention_wait_limit.argtypes = [ctypes.c_uint64]

@@ -1,0 +1,10 @@
+// Attention of few rows over a cache of int8 codes.
+#include "paged/coded_rows.cuh"
+
+namespace gorio {
+namespace paged {
+
+cudaError_t launch_coded_rows_int8(const CodedAttn &a, int dtype, int dim, u32 sms, cudaStream_t s) { return launch_coded_rows_of<kInt8>(a, dtype, dim, sms, s); }
+
+}  // namespace paged
+}  // namespace gorio

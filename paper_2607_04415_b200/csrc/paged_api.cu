@@ -5,7 +5,7 @@
 #include <mutex>
 
 #include "../../include/gorio.h"
-#include "paged/common.cuh"
+#include "paged/coded.cuh"
 #include "paged/entries.h"
 
 namespace gorio { void set_global_error(const char *msg); }
@@ -259,4 +259,60 @@ extern "C" int gorio_prefix_attention(const gorio_prefix_attention_desc *d, void
   o.group_starts = d->group_starts; o.n_groups = d->n_groups;
   o.mid_o = mid_o; o.mid_ml = mid_ml;
   return launched(launch_attention(o, own, sms, (cudaStream_t)cuda_stream), "prefix attention");
+}
+
+namespace {
+
+// Both calls on rows of a quantised cache.
+int quantized_rows(const gorio_quantized_rows_desc *d, bool store, void *cuda_stream) {
+  const char *const what = store ? "quantized store" : "quantized load";
+  if (!d) return bad("quantized rows: null argument");
+  if (d->n_tokens == 0 || d->n_heads == 0 || (store && d->n_pages == 0)) return GORIO_OK;
+  if (!d->keys || !d->values || !d->slots) return bad("quantized rows: null argument");
+  if (d->n_pages && (!d->key_pages || !d->value_pages || !d->key_scales || !d->value_scales)) return bad("quantized rows: null argument");
+  if (d->dtype > GORIO_KV_FP16 || d->format > GORIO_CODES_INT8) return bad("quantized rows: unknown dtype or format");
+  if (d->dim == 0 || d->dim % 16 != 0 || d->dim > 256 || d->page_size < 1 || (uint64_t)d->n_pages * d->page_size >= (1ull << 31))
+    return bad("quantized rows: need dim a multiple of 16 and at most 256, page_size >= 1 and n_pages * page_size < 2^31");
+  const int64_t wide = d->k_token_stride | d->k_head_stride | d->v_token_stride | d->v_head_stride;
+  const int64_t codes = d->kp_page_stride | d->kp_head_stride | d->kp_token_stride | d->vp_page_stride | d->vp_head_stride | d->vp_token_stride;
+  if ((wide & 7) || (codes & 15)) return bad("quantized rows: strides must be multiples of 8 elements, of the pages of 16");
+  if (!aligned(d->keys, 16) || !aligned(d->values, 16) || !aligned(d->key_pages, 16) || !aligned(d->value_pages, 16))
+    return bad("quantized rows: keys, values and pages must be 16-byte aligned");
+  if (!aligned(d->key_scales, 4) || !aligned(d->value_scales, 4)) return bad("quantized rows: scales must be 4-byte aligned");
+  if (d->n_tokens >= (1u << 31) || d->n_heads > 65536 || (uint64_t)d->n_tokens * d->n_heads >= (1ull << 31))
+    return bad("quantized rows: n_tokens * n_heads must be below 2^31");
+  return launched(launch_quantized_rows(*d, store, (cudaStream_t)cuda_stream), what);
+}
+
+}  // namespace
+
+extern "C" int gorio_cache_store_quantized(const gorio_quantized_rows_desc *d, void *cuda_stream) { return quantized_rows(d, true, cuda_stream); }
+extern "C" int gorio_cache_load_quantized(const gorio_quantized_rows_desc *d, void *cuda_stream) { return quantized_rows(d, false, cuda_stream); }
+
+extern "C" int gorio_paged_attention_quantized(const gorio_quantized_attention_desc *d, void *cuda_stream) {
+  if (!d) return bad("quantized attention: null argument");
+  const gorio_paged_attention_desc &p = d->attention;
+  if (p.n_requests == 0 || p.n_tokens == 0) return GORIO_OK;
+  int sms = 0, st = check_attention(&p);
+  if (st != GORIO_OK) return st;
+  if (d->format > GORIO_CODES_INT8) return bad("quantized attention: unknown format");
+  if (p.n_pages && (!d->key_scales || !d->value_scales)) return bad("quantized attention: null argument");
+  if (!aligned(d->key_scales, 4) || !aligned(d->value_scales, 4)) return bad("quantized attention: scales must be 4-byte aligned");
+  if ((p.kp_page_stride | p.kp_head_stride | p.kp_token_stride | p.vp_page_stride | p.vp_head_stride | p.vp_token_stride) & 15)
+    return bad("quantized attention: strides of the pages must be multiples of 16");
+  st = current_sms(&sms, "quantized attention");
+  if (st != GORIO_OK) return st;
+  CodedAttn a{};
+  fill_attention(a, &p, sms);
+  a.ks = d->key_scales; a.vs = d->value_scales;
+  a.ks_p = d->ks_page_stride; a.ks_h = d->ks_head_stride; a.ks_t = d->ks_token_stride;
+  a.vs_p = d->vs_page_stride; a.vs_h = d->vs_head_stride; a.vs_t = d->vs_token_stride;
+  if (p.n_pages == 0) {                                      // as for the pages
+    a.ks = a.vs = (const float *)p.workspace;
+    a.ks_p = a.ks_h = a.ks_t = a.vs_p = a.vs_h = a.vs_t = 0;
+  }
+  const cudaStream_t s = (cudaStream_t)cuda_stream;
+  const cudaError_t e = d->format == GORIO_CODES_E4M3 ? launch_coded_rows_e4m3(a, (int)p.dtype, (int)p.dim, (u32)sms, s)
+                                                      : launch_coded_rows_int8(a, (int)p.dtype, (int)p.dim, (u32)sms, s);
+  return launched(e, "quantized attention");
 }
