@@ -163,10 +163,169 @@ __device__ __forceinline__ void weights64(const float *s, f32x2 mul, f32x2 minus
   }
 }
 
+// The end of a part, by the eight warps of the softmax: its rows written, or left for or joined with the unit's other parts.  `output` gives
+// COLS columns of this thread's row, `output32` 32, as weighted sums that count from 2^m, like l.  `mine`: the thread's warpgroup writes the row.
+// Returns false once a wait has run out.
+template <typename T, int D, int COLS, typename A, typename Rows, typename Shared, typename Meet, typename Output, typename Output32>
+__device__ __forceinline__ bool write_part(const A &a, const Rows &covered, Shared &sh, const PartInfo &p, const Row &r, bool valid, bool mine, bool fine,
+                                           int unit_row, float m, float l, const Meet &meet, const Output &output, const Output32 &output32) {
+  typedef typename EndOf<A>::type End;
+  constexpr int kCols = COLS;
+  constexpr int kAhead = 2;                                  // parts of a cut unit that are fetched at a time, 32 columns of each
+  if (p.whole) {
+    if (mine && fine) {
+      const End end(a, covered, r.tok, r.head, D, m, l, valid);
+#pragma unroll 1
+      for (int col = 0; col < D; col += kCols) {
+        float o[kCols];
+        output(o, col);
+#pragma unroll
+        for (int k = 0; k < kCols; k += 32)
+          if (valid) end.template write32<T>(a, r.tok, r.head, col + k, o + k);
+      }
+    }
+  } else if (fine) {
+    // A cut unit.  The last block to get here joins the parts, its own out of tensor memory; the others leave theirs in
+    // the workspace: [part][column / 4][row][4], so that neighbouring threads' rows lie side by side.
+    const u32 own = blockIdx.x, others = p.i1 - p.i0;
+    if (threadIdx.x == 0) sh.last = load_acquire(a.arrived + p.i0) == others;
+    fine = meet();
+    bool join = fine && sh.last != 0;
+    if (fine && !join) {
+      const i64 slot = 2 * own + (own == p.i0 ? 1 : 0);
+      if (mine) {
+        *(float2 *)(a.part_ml + (slot * kRows + unit_row) * 2) = make_float2(m, l);
+#pragma unroll 1
+        for (int col = 0; col < D; col += kCols) {
+          float o[kCols];
+          output(o, col);
+#pragma unroll
+          for (int k = 0; k < kCols / 4; ++k)
+            __stcg((float4 *)a.part_o + (slot * (D / 4) + col / 4 + k) * kRows + unit_row, make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]));
+        }
+      }
+      __threadfence();
+      fine = meet();
+      if (threadIdx.x == 0 && fine) { sh.last = atomicAdd(a.arrived + p.i0, 1u) == others; __threadfence(); }
+      fine = fine && meet();
+      join = fine && sh.last != 0;
+    }
+    if (join) {
+      if (threadIdx.x == 0) a.arrived[p.i0] = 0;                 // ready for the next call
+      if (mine) {
+        auto place = [&](u32 i) { return (i64)(2 * i + (i == p.i0 ? 1 : 0)); };
+        float top = -INFINITY, sum = 0.0f;
+#pragma unroll 4
+        for (u32 i = p.i0; i <= p.i1; ++i) {
+          const float x = __ldcg(a.part_ml + (place(i) * kRows + unit_row) * 2);
+          top = fmaxf(top, i == own ? m : x);
+        }
+        const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll 4
+        for (u32 i = p.i0; i <= p.i1; ++i) {
+          const float2 x = __ldcg((const float2 *)(a.part_ml + (place(i) * kRows + unit_row) * 2));
+          sum += i == own ? exp2_approx(m - base) * l : exp2_approx(x.x - base) * x.y;
+        }
+        const End end(a, covered, r.tok, r.head, D, top, sum, valid);
+#pragma unroll 1
+        for (int col = 0; col < D; col += 32) {
+          float acc[32];
+#pragma unroll
+          for (int k = 0; k < 32; ++k) acc[k] = 0.0f;
+#pragma unroll 1
+          for (u32 i = p.i0; i <= p.i1; i += kAhead) {
+            float o[kAhead][32], g[kAhead];
+#pragma unroll
+            for (u32 j = 0; j < kAhead; ++j) {
+              const bool there = i + j <= p.i1 && i + j != own;
+              const i64 at = place(i + j);
+              const float4 *from = (const float4 *)a.part_o + (at * (D / 4) + col / 4) * kRows + unit_row;
+              g[j] = there ? __ldcg(a.part_ml + (at * kRows + unit_row) * 2) : -INFINITY;
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                const float4 x = there ? __ldcg(from + k * kRows) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                o[j][4 * k] = x.x; o[j][4 * k + 1] = x.y; o[j][4 * k + 2] = x.z; o[j][4 * k + 3] = x.w;
+              }
+            }
+#pragma unroll
+            for (u32 j = 0; j < kAhead; ++j) {
+              if (i + j == own) {
+                g[j] = m;
+                output32(o[j], col);
+              }
+              g[j] = exp2_approx(g[j] - base);
+#pragma unroll
+              for (int k = 0; k < 32; ++k) acc[k] += g[j] * o[j][k];
+            }
+          }
+          if (valid) end.template write32<T>(a, r.tok, r.head, col, acc);
+        }
+      }
+    }
+  }
+  return fine;
+}
+
 // What becomes of q.k: nothing but the scale; a cap of up to 64 or a bias; a cap of any size.  Without its series capped_log2 is off by
 // some 2^-22 of the cap, which up to 64 is less than the weights' rounding, and a call of such layers takes 103 us where it
 // takes 111 with the series.
 enum Scores { kPlain, kSmallCap, kLargeCap };
+
+// A row's 128 products to units of log2, with cap and bias.  `in` and `linear`: the cap's exponent and the score of a product of 1; `far`: the
+// first key's bias.
+template <Scores SCORES>
+__device__ __forceinline__ void scores128(const Attn &a, float *s, float in, float linear, float slope, float far) {
+  const float cap = a.softcap * kLog2e;
+  const f32x2 in2 = pack_f32(in, in), slope2 = pack_f32(slope, slope), one2 = pack_f32(1.0f, 1.0f), zero2 = pack_f32(0.0f, 0.0f);
+  const f32x2 twice2 = pack_f32(-2.0f * cap, -2.0f * cap), far2 = pack_f32(far, far);
+  const f32x2 cap2 = SCORES == kLargeCap ? pack_f32(cap, cap) : pack_f32(cap + far, cap + far);
+  const f32x2 linear2 = pack_f32(linear, linear), c1 = pack_f32(kCap1, kCap1), c2 = pack_f32(kCap2, kCap2), c3 = pack_f32(kCap3, kCap3);
+#pragma unroll
+  for (int i = 0; i < 128; i += 2) {
+    const f32x2 dot = pack_f32(s[i], s[i + 1]);
+    f32x2 x;
+    if (SCORES == kLargeCap || a.softcap > 0.0f) {  // cap * tanh(x / cap), see capped_log2
+      float e0, e1;
+      const f32x2 w = fma_f32x2(dot, in2, zero2);
+      unpack_f32(w, e0, e1);
+      unpack_f32(add_f32x2(pack_f32(exp2_approx(e0), exp2_approx(e1)), one2), e0, e1);
+      x = fma_f32x2(twice2, pack_f32(rcp_approx(e0), rcp_approx(e1)), cap2);
+      if (SCORES == kLargeCap) {
+        const f32x2 q = fma_f32x2(w, w, zero2);
+        const f32x2 small = fma_f32x2(fma_f32x2(dot, linear2, zero2), fma_f32x2(q, fma_f32x2(q, fma_f32x2(q, c3, c2), c1), one2), zero2);
+        float w0, w1, s0, s1;
+        unpack_f32(w, w0, w1);
+        unpack_f32(small, s0, s1);
+        unpack_f32(x, e0, e1);
+        x = add_f32x2(pack_f32(fabsf(w0) < kCapSeries ? s0 : e0, fabsf(w1) < kCapSeries ? s1 : e1), far2);
+      }
+    } else {
+      x = fma_f32x2(dot, in2, far2);
+    }
+    unpack_f32(fma_f32x2(slope2, pack_f32((float)i, (float)(i + 1)), x), s[i], s[i + 1]);
+  }
+}
+
+// Masks all but the keys [lo, hi) of 128.
+__device__ __forceinline__ void mask128(float *s, int lo, int hi) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {                              // a bit for each of 32 keys
+    const u32 seen = bits_below(hi - 32 * w) & ~bits_below(lo - 32 * w);
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (!(seen & (1u << i))) s[32 * w + i] = -INFINITY;
+  }
+}
+
+// The largest of 128: four chains of three-way maxima.
+__device__ __forceinline__ float largest128(const float *s) {
+  float tops[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+  for (int i = 4; i < 124; i += 8)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) tops[k] = fmaxf(fmaxf(tops[k], s[i + k]), s[i + 4 + k]);
+  return fmaxf(fmaxf(fmaxf(tops[0], s[124]), fmaxf(tops[1], s[125])), fmaxf(fmaxf(tops[2], s[126]), fmaxf(tops[3], s[127])));
+}
 
 template <typename T, int D, Scores SCORES, typename A>
 __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __grid_constant__ A a, const __grid_constant__ CUtensorMap keys,
@@ -215,8 +374,6 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
     const int t = warp >> 2, row = tid & (kTileRows - 1);
     constexpr int kCols = D % 64 == 0 ? 64 : 32;             // columns of the output that are worked on at a time
     constexpr float kLift = WeightLift<T, 8>::value;
-    typedef typename EndOf<A>::type End;
-    constexpr int kAhead = 2;                                // parts of a cut unit that are fetched at a time, 32 columns of each
     const u32 lanes = (u32)(warp & 3) << 21;                 // this warp's 32 lanes of tensor memory
     const u32 scores = tmem + kScores + t * 128 + lanes, outputs = tmem + kOutputs + t * D + lanes;
     u32 s_phase = 0, o_phase = 0, meet_phase = 0;            // o_phase: a bit for each row tile's output
@@ -252,53 +409,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
           for (int i = 0; i < 4; ++i) keep(s + 32 * i);
           const int key0 = (p.tile + at) * kTileKeys;
           if (SCORES != kPlain) {                            // to units of log2, with cap and bias
-            const float far = slope * (float)(key0 - r.pos), linear = a.scale * kLog2e, cap = a.softcap * kLog2e;
-            const float in = a.softcap > 0.0f ? cap_in(a) : linear;
-            const f32x2 in2 = pack_f32(in, in), slope2 = pack_f32(slope, slope), one2 = pack_f32(1.0f, 1.0f), zero2 = pack_f32(0.0f, 0.0f);
-            const f32x2 twice2 = pack_f32(-2.0f * cap, -2.0f * cap), far2 = pack_f32(far, far);
-            const f32x2 cap2 = SCORES == kLargeCap ? pack_f32(cap, cap) : pack_f32(cap + far, cap + far);
-            const f32x2 linear2 = pack_f32(linear, linear), c1 = pack_f32(kCap1, kCap1), c2 = pack_f32(kCap2, kCap2), c3 = pack_f32(kCap3, kCap3);
-#pragma unroll
-            for (int i = 0; i < 128; i += 2) {
-              const f32x2 dot = pack_f32(s[i], s[i + 1]);
-              f32x2 x;
-              if (SCORES == kLargeCap || a.softcap > 0.0f) {  // cap * tanh(x / cap), see capped_log2
-                float e0, e1;
-                const f32x2 w = fma_f32x2(dot, in2, zero2);
-                unpack_f32(w, e0, e1);
-                unpack_f32(add_f32x2(pack_f32(exp2_approx(e0), exp2_approx(e1)), one2), e0, e1);
-                x = fma_f32x2(twice2, pack_f32(rcp_approx(e0), rcp_approx(e1)), cap2);
-                if (SCORES == kLargeCap) {
-                  const f32x2 q = fma_f32x2(w, w, zero2);
-                  const f32x2 small = fma_f32x2(fma_f32x2(dot, linear2, zero2), fma_f32x2(q, fma_f32x2(q, fma_f32x2(q, c3, c2), c1), one2), zero2);
-                  float w0, w1, s0, s1;
-                  unpack_f32(w, w0, w1);
-                  unpack_f32(small, s0, s1);
-                  unpack_f32(x, e0, e1);
-                  x = add_f32x2(pack_f32(fabsf(w0) < kCapSeries ? s0 : e0, fabsf(w1) < kCapSeries ? s1 : e1), far2);
-                }
-              } else {
-                x = fma_f32x2(dot, in2, far2);
-              }
-              unpack_f32(fma_f32x2(slope2, pack_f32((float)i, (float)(i + 1)), x), s[i], s[i + 1]);
-            }
+            const float linear = a.scale * kLog2e;
+            scores128<SCORES>(a, s, a.softcap > 0.0f ? cap_in(a) : linear, linear, slope, slope * (float)(key0 - r.pos));
           }
-          if (__any_sync(0xffffffffu, key0 < r.lo || key0 + kTileKeys > r.hi)) {
-            const int lo = r.lo - key0, hi = r.hi - key0;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {                    // a bit for each of 32 keys
-              const u32 seen = bits_below(hi - 32 * w) & ~bits_below(lo - 32 * w);
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (!(seen & (1u << i))) s[32 * w + i] = -INFINITY;
-            }
-          }
-          float tops[4] = {s[0], s[1], s[2], s[3]};          // four chains of three-way maxima
-#pragma unroll
-          for (int i = 4; i < 124; i += 8)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) tops[k] = fmaxf(fmaxf(tops[k], s[i + k]), s[i + 4 + k]);
-          float top = fmaxf(fmaxf(fmaxf(tops[0], s[124]), fmaxf(tops[1], s[125])), fmaxf(fmaxf(tops[2], s[126]), fmaxf(tops[3], s[127])));
+          if (__any_sync(0xffffffffu, key0 < r.lo || key0 + kTileKeys > r.hi)) mask128(s, r.lo - key0, r.hi - key0);
+          float top = largest128(s);
           top *= mul;
           const bool moves = top > m + 8.0f || (m == -INFINITY && top > -INFINITY);
           if (__any_sync(0xffffffffu, moves)) {
@@ -395,97 +510,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
 #pragma unroll
         for (int k = 0; k < kCols; k += 32) keep(o + k);
       };
-      if (p.whole) {
-        if (mine && fine) {
-          const End end(a, covered, r.tok, r.head, D, m, l, valid);
-#pragma unroll 1
-          for (int col = 0; col < D; col += kCols) {
-            float o[kCols];
-            output(o, col);
-#pragma unroll
-            for (int k = 0; k < kCols; k += 32)
-              if (valid) end.template write32<T>(a, r.tok, r.head, col + k, o + k);
-          }
-        }
-      } else if (fine) {
-        // A cut unit.  The last block to get here joins the parts, its own out of tensor memory; the others leave theirs in
-        // the workspace: [part][column / 4][row][4], so that neighbouring threads' rows lie side by side.
-        const u32 own = blockIdx.x, others = p.i1 - p.i0;
-        if (tid == 0) sh.last = load_acquire(a.arrived + p.i0) == others;
-        fine = meet();
-        bool join = fine && sh.last != 0;
-        if (fine && !join) {
-          const i64 slot = 2 * own + (own == p.i0 ? 1 : 0);
-          if (mine) {
-            *(float2 *)(a.part_ml + (slot * kRows + unit_row) * 2) = make_float2(m, l);
-#pragma unroll 1
-            for (int col = 0; col < D; col += kCols) {
-              float o[kCols];
-              output(o, col);
-#pragma unroll
-              for (int k = 0; k < kCols / 4; ++k)
-                __stcg((float4 *)a.part_o + (slot * (D / 4) + col / 4 + k) * kRows + unit_row, make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]));
-            }
-          }
-          __threadfence();
-          fine = meet();
-          if (tid == 0 && fine) { sh.last = atomicAdd(a.arrived + p.i0, 1u) == others; __threadfence(); }
-          fine = fine && meet();
-          join = fine && sh.last != 0;
-        }
-        if (join) {
-          if (tid == 0) a.arrived[p.i0] = 0;                 // ready for the next call
-          if (mine) {
-            auto place = [&](u32 i) { return (i64)(2 * i + (i == p.i0 ? 1 : 0)); };
-            float top = -INFINITY, sum = 0.0f;
-#pragma unroll 4
-            for (u32 i = p.i0; i <= p.i1; ++i) {
-              const float x = __ldcg(a.part_ml + (place(i) * kRows + unit_row) * 2);
-              top = fmaxf(top, i == own ? m : x);
-            }
-            const float base = top == -INFINITY ? 0.0f : top;
-#pragma unroll 4
-            for (u32 i = p.i0; i <= p.i1; ++i) {
-              const float2 x = __ldcg((const float2 *)(a.part_ml + (place(i) * kRows + unit_row) * 2));
-              sum += i == own ? exp2_approx(m - base) * l : exp2_approx(x.x - base) * x.y;
-            }
-            const End end(a, covered, r.tok, r.head, D, top, sum, valid);
-#pragma unroll 1
-            for (int col = 0; col < D; col += 32) {
-              float acc[32];
-#pragma unroll
-              for (int k = 0; k < 32; ++k) acc[k] = 0.0f;
-#pragma unroll 1
-              for (u32 i = p.i0; i <= p.i1; i += kAhead) {
-                float o[kAhead][32], g[kAhead];
-#pragma unroll
-                for (u32 j = 0; j < kAhead; ++j) {
-                  const bool there = i + j <= p.i1 && i + j != own;
-                  const i64 at = place(i + j);
-                  const float4 *from = (const float4 *)a.part_o + (at * (D / 4) + col / 4) * kRows + unit_row;
-                  g[j] = there ? __ldcg(a.part_ml + (at * kRows + unit_row) * 2) : -INFINITY;
-#pragma unroll
-                  for (int k = 0; k < 8; ++k) {
-                    const float4 x = there ? __ldcg(from + k * kRows) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    o[j][4 * k] = x.x; o[j][4 * k + 1] = x.y; o[j][4 * k + 2] = x.z; o[j][4 * k + 3] = x.w;
-                  }
-                }
-#pragma unroll
-                for (u32 j = 0; j < kAhead; ++j) {
-                  if (i + j == own) {
-                    g[j] = m;
-                    output32(o[j], col);
-                  }
-                  g[j] = exp2_approx(g[j] - base);
-#pragma unroll
-                  for (int k = 0; k < 32; ++k) acc[k] += g[j] * o[j][k];
-                }
-              }
-              if (valid) end.template write32<T>(a, r.tok, r.head, col, acc);
-            }
-          }
-        }
-      }
+      fine = write_part<T, D, kCols>(a, covered, sh, p, r, valid, mine, fine, unit_row, m, l, meet, output, output32);
       mma_fence_before();
       if (two || !p.whole) fine = fine && meet();            // sh.last and the other's output are free again
       part_done(no);

@@ -59,6 +59,11 @@ __device__ __forceinline__ void decode_along(u32 w, u32 &lo, u32 &hi) {
   }
 }
 
+// 4 bytes, or zeros
+__device__ __forceinline__ void cp_async4(void *to, const void *from, u32 bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_addr(to)), "l"(from), "r"(bytes) : "memory");
+}
+
 // Queries become float16 too, each row times a power of two that brings its largest number to 2^14 or more: nothing is lost but
 // what lies below 2^-38 of that.  `largest` is a magnitude's bits; returns the factor.
 __device__ __forceinline__ float query_factor(float largest) {
@@ -69,6 +74,8 @@ __device__ __forceinline__ float query_factor(float largest) {
 // launchers, one for each format
 cudaError_t launch_coded_rows_e4m3(const CodedAttn &a, int dtype, int dim, u32 sms, cudaStream_t s);
 cudaError_t launch_coded_rows_int8(const CodedAttn &a, int dtype, int dim, u32 sms, cudaStream_t s);
+bool launch_coded_chunk_e4m3(const CodedAttn &a, int dtype, int dim, u32 sms, cudaStream_t s, cudaError_t *e);
+bool launch_coded_chunk_int8(const CodedAttn &a, int dtype, int dim, u32 sms, cudaStream_t s, cudaError_t *e);
 
 }  // namespace paged
 }  // namespace gorio

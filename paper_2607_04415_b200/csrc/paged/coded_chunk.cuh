@@ -1,0 +1,684 @@
+// Attention of many rows over a quantised paged cache: the chunk form, on the fifth-generation tensor cores.
+//
+// Units, parts, products, softmax and joins are those of the 16-bit cache's kernel (chunk.cuh); what is new stands between the copies and
+// the products.  Sixteen warps:
+//   0-3, 4-7  the softmax of row tile 0 and 1: a thread a row.  At a part's start each thread brings its own row of queries, as float16 times a
+//             power of two.
+//   8         issues both products (one thread).
+//   9         copies codes of keys and values, 64 keys at a time, into a ring of their own (tensor copies).
+//   10        fetches the scales of a tile's keys and values.
+//   11        walks the block's share of the work and tells the others its parts.
+//   12-15     take codes apart into the 16-bit tiles that the products read.
+// Keys become their codes, exactly; a score is multiplied by its key's scale in 32 bits.  Values are multiplied by their scales as they
+// become float16, one rounding to 11 bits; so that neither side of that leaves float16's range, a tile has a power of two of its own, taken out of
+// its values and put into its weights: 2^(x + shift - m) with m the running maximum of x + shift, whose sum is taken back by 2^-shift once a tile.
+// The factor itself is kept as two float16 numbers, so that its rounding is not added to the product's.
+//
+// A value's scale that is not finite would reach rows that do not see its key as 0 * inf in the product.  It is left out there, and stands in the
+// key's place instead: scores of rows that see the key are then not a number.  With it all operands are finite, so that tiles that some rows
+// see and others do not need no care beyond the mask.
+#pragma once
+#include "chunk.cuh"
+#include "coded.cuh"
+
+namespace gorio {
+namespace paged {
+
+namespace {
+
+constexpr int kCodedThreads = 512;
+constexpr int kCodedSoftmaxRegs = 208, kCodedOtherRegs = 48;     // a thread, of 128 * 4 = 208 * 2 + 48 * 2 at launch
+constexpr int kHalfKeys = 64;                                    // of a copy
+constexpr int kScaleSlots = 4;                                   // tiles whose scales are there
+constexpr int kScalesAhead = 2;                                  // tiles whose scales are on their way
+
+template <int D>
+struct CodedShape {
+  static constexpr int chunks = (D + 63) / 64;                   // of 64 elements, 128 bytes
+  static constexpr int tile_bytes = chunks * kTileKeys * 128;
+  static constexpr int stages = chunks == 1 ? 8 : 4;
+  static constexpr int half_bytes = kHalfKeys * D;
+  static constexpr int halves = D == 128 ? 3 : D == 96 ? 4 : 6;  // 24 KB, which is what is left
+};
+
+template <int D>
+struct CodedChunkShared {
+  unsigned char q[2][CodedShape<D>::tile_bytes];
+  unsigned char kv[CodedShape<D>::stages][CodedShape<D>::tile_bytes];
+  unsigned char codes[CodedShape<D>::halves][CodedShape<D>::half_bytes];
+  float k_scale[kScaleSlots][kTileKeys];
+  u32 v_factor[kScaleSlots][kTileKeys];          // two float16: the factor and what it lacks; until they are there, the scale
+  int shift[kScaleSlots];
+  float q_to_dot[kTileRows];                     // of the rows of a unit of one row tile
+  PartInfo part[kParts];
+  u64 kv_full[CodedShape<D>::stages], kv_empty[CodedShape<D>::stages], codes_full[CodedShape<D>::halves], codes_empty[CodedShape<D>::halves];
+  u64 scales_full[kScaleSlots], scales_empty[kScaleSlots];
+  u64 part_full[kParts], part_empty[kParts];
+  u64 q_full[2], q_empty[2], s_full[2], p_full[2][2], o_full[2], meet, drained;
+  u32 tmem, failed, last;
+  union {
+    PlanShared plan;                 // until the parts begin
+    float2 half_ml[kTileRows];
+  };
+};
+
+__device__ __forceinline__ f32x2 mul_f32x2(f32x2 a, f32x2 b) {
+  f32x2 v;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+  return v;
+}
+__device__ __forceinline__ u32 mul_f16x2(u32 a, u32 b) {
+  u32 v;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(v) : "r"(a), "r"(b));
+  return v;
+}
+__device__ __forceinline__ u32 fma_f16x2(u32 a, u32 b, u32 c) {
+  u32 v;
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(v) : "r"(a), "r"(b), "r"(c));
+  return v;
+}
+__device__ __forceinline__ void bar_arrive_n(u64 *bar, u32 n) {
+  asm volatile("mbarrier.arrive.shared.b64 _, [%0], %1;" ::"r"(smem_addr(bar)), "r"(n) : "memory");
+}
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((u32)(127 + e) << 23); }
+
+template <typename T, Format F, int D, Scores SCORES>
+__global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __grid_constant__ CodedAttn a, const __grid_constant__ CUtensorMap keys,
+                                                                       const __grid_constant__ CUtensorMap values, const u32 box_rows) {
+  extern __shared__ unsigned char raw[];
+  typedef CodedChunkShared<D> Shared;
+  Shared &sh = *(Shared *)(raw + ((1024 - (smem_addr(raw) & 1023)) & 1023));
+  typedef CodedShape<D> S;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (warp == 8) {
+    if (lane < S::stages) { bar_init(&sh.kv_full[lane], 4); bar_init(&sh.kv_empty[lane], 1); }
+    if (lane < S::halves) { bar_init(&sh.codes_full[lane], 1); bar_init(&sh.codes_empty[lane], 4); }
+    if (lane < kScaleSlots) { bar_init(&sh.scales_full[lane], 1); bar_init(&sh.scales_empty[lane], 12); }
+    if (lane < kParts) { bar_init(&sh.part_full[lane], 1); bar_init(&sh.part_empty[lane], 15); }
+    if (lane < 2) {
+      bar_init(&sh.q_full[lane], 4); bar_init(&sh.q_empty[lane], 1); bar_init(&sh.s_full[lane], 1); bar_init(&sh.o_full[lane], 1);
+      bar_init(&sh.p_full[lane][0], 4); bar_init(&sh.p_full[lane][1], 4);
+    }
+    if (lane == 0) { bar_init(&sh.meet, 8); bar_init(&sh.drained, 1); sh.failed = 0; }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async();
+    __syncwarp();
+    tmem_alloc(&sh.tmem, 512);
+  }
+  const Plan plan = block_plan<kRows, kTileKeys, kOver, kCodedThreads>(a, sh.plan, kSpread);
+  mma_fence_before();
+  __syncthreads();
+  mma_fence_after();
+  const u32 tmem = sh.tmem;
+  const WaitLimit limit{a.wait_ticks, &sh.failed};
+  auto wait = [&](u64 *bar, u32 parity) { return warp_wait(bar, parity, limit); };
+  // the part that is told `no`-th; false at the end
+  auto take_part = [&](u32 no, PartInfo &p) {
+    if (!wait(&sh.part_full[no % kParts], (no / kParts) & 1)) return false;
+    p = sh.part[no % kParts];
+    return p.tiles != 0;
+  };
+  auto part_done = [&](u32 no) {
+    __syncwarp();
+    if (lane == 0) bar_arrive(&sh.part_empty[no % kParts]);
+  };
+
+  if (warp < 8) {
+    // ------------------------------------------------------------------ softmax of row tile t
+    more_registers<kCodedSoftmaxRegs>();
+    const int t = warp >> 2, row = tid & (kTileRows - 1);
+    constexpr int kCols = D % 64 == 0 ? 64 : 32;             // columns of the output that are worked on at a time
+    constexpr float kLift = WeightLift<__half, 8>::value;
+    const u32 lanes = (u32)(warp & 3) << 21;                 // this warp's 32 lanes of tensor memory
+    const u32 scores = tmem + kScores + t * 128 + lanes, outputs = tmem + kOutputs + t * D + lanes;
+    u32 s_phase = 0, o_phase = 0, meet_phase = 0, q_phase = 1;   // o_phase: a bit for each row tile's output
+    u32 tile_no = 0;                                         // tiles of the parts before
+    auto meet = [&]() {                                      // all eight warps, with the limit of every other wait
+      __syncwarp();
+      if (lane == 0) bar_arrive(&sh.meet);
+      const bool ok = wait(&sh.meet, meet_phase);
+      meet_phase ^= 1;
+      return ok;
+    };
+    PartInfo p;
+    bool fine = true;                                        // no wait of this warp has run out
+    for (u32 no = 0; fine && take_part(no, p); ++no) {
+      const bool split = p.rows <= kTileRows;                // one row tile: key tiles by turns
+      const bool mine = t == 0 || !split;                    // whose rows this warpgroup writes
+      const int unit_row = (split ? 0 : t * kTileRows) + row, first = split ? t : 0;
+      const bool valid = unit_row < p.rows;
+      const Row r = row_of(a, p, (u32)p.row0 + (valid ? unit_row : 0));
+      float to_dot = 1.0f;
+      if (mine) {
+        // this thread's row of queries: float16, times a power of two
+        fine = wait(&sh.q_empty[t], q_phase);
+        q_phase ^= 1;
+        const u16 *src = (const u16 *)a.q + r.tok * a.q_t + (i64)r.head * a.q_h;
+        uint4 x[D / 8];
+        float top = 0.0f;
+#pragma unroll
+        for (int k = 0; k < D / 8; ++k) x[k] = valid ? *(const uint4 *)(src + 8 * k) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int k = 0; k < D / 8; ++k) {
+          const u32 w[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float2 v = unpack2<T>(w[i]);
+            top = fmaxf(top, fmaxf(fabsf(v.x), fabsf(v.y)));
+          }
+        }
+        const float f = query_factor(top);
+        to_dot = kUnit<F> / f;                               // powers of two
+#pragma unroll
+        for (int k = 0; k < D / 8; ++k) {
+          u32 w[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float2 v = unpack2<T>(w[i]);
+            w[i] = pack2<__half>(v.x * f, v.y * f);
+          }
+          if (fine) *(uint4 *)(sh.q[t] + (k >> 3) * (kTileRows * 128) + row * 128 + (((k & 7) ^ (row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        if (split && fine) sh.q_to_dot[row] = to_dot;
+        fence_async();
+        __syncwarp();
+        if (lane == 0 && fine) bar_arrive(&sh.q_full[t]);
+      }
+      float m = -INFINITY, l = 0.0f;
+      {
+        const float slope = SCORES != kPlain && a.slopes ? a.slopes[r.head] * kLog2e : 0.0f;
+        for (int at = first; at < p.tiles && fine; at += split ? 2 : 1) {
+          const u32 slot = (tile_no + (u32)at) % kScaleSlots;
+          fine = wait(&sh.scales_full[slot], ((tile_no + (u32)at) / kScaleSlots) & 1) && wait(&sh.s_full[t], s_phase);
+          if (!fine) break;
+          s_phase ^= 1;
+          mma_fence_after();
+          if (split && t == 1 && at == 1) to_dot = sh.q_to_dot[row];     // the queries came before the scores
+          const float mul = SCORES != kPlain ? 1.0f : a.scale * kLog2e * to_dot;
+          float s[128];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) tmem_ld32(s + 32 * i, scores + 32 * i);
+          tmem_wait_ld();
+#pragma unroll
+          for (int i = 0; i < 4; ++i) keep(s + 32 * i);
+#pragma unroll
+          for (int i = 0; i < 128; i += 4) {
+            const float4 k = *(const float4 *)&sh.k_scale[slot][i];
+            unpack_f32(mul_f32x2(pack_f32(s[i], s[i + 1]), pack_f32(k.x, k.y)), s[i], s[i + 1]);
+            unpack_f32(mul_f32x2(pack_f32(s[i + 2], s[i + 3]), pack_f32(k.z, k.w)), s[i + 2], s[i + 3]);
+          }
+          const int shift = sh.shift[slot];
+          __syncwarp();
+          if (lane == 0) bar_arrive_n(&sh.scales_empty[slot], split ? 2 : 1);
+          const int key0 = (p.tile + at) * kTileKeys;
+          if (SCORES != kPlain) {                            // to units of log2, with cap and bias
+            const float linear = a.scale * kLog2e * to_dot;
+            scores128<SCORES>(a, s, a.softcap > 0.0f ? cap_in(a) * to_dot : linear, linear, slope, slope * (float)(key0 - r.pos));
+          }
+          if (__any_sync(0xffffffffu, key0 < r.lo || key0 + kTileKeys > r.hi)) mask128(s, r.lo - key0, r.hi - key0);
+          const float top = largest128(s) * mul + (float)shift;
+          const bool moves = top > m + 8.0f || (m == -INFINITY && top > -INFINITY);
+          if (__any_sync(0xffffffffu, moves)) {
+            const float to = moves ? top : m;
+            const float f = m == -INFINITY ? 0.0f : exp2_approx(m - to);
+            m = to;
+            l *= f;
+            if (at > first) {                                // the scores' arrival says that the product before is done
+#pragma unroll 2
+              for (int i = 0; i < D / 32; ++i) {
+                float o[32];
+                tmem_ld32(o, outputs + 32 * i);
+                tmem_wait_ld();
+                keep(o);
+                u32 w[32];
+#pragma unroll
+                for (int k = 0; k < 32; ++k) w[k] = __float_as_uint(o[k] * f);
+                tmem_st32(outputs + 32 * i, w);
+              }
+            }
+          }
+          const float minus_base = m == -INFINITY ? 0.0f : kLift - m + (float)shift;
+          const f32x2 mul2 = pack_f32(mul, mul), base2 = pack_f32(minus_base, minus_base);
+          f32x2 sum[2] = {pack_f32(0.0f, 0.0f), pack_f32(0.0f, 0.0f)};
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {                      // the product starts on the first half of the weights
+            u32 w[32];
+            weights64<__half>(s + 64 * i, mul2, base2, sum, w);
+            tmem_st32(scores + 32 * i, w);
+            tmem_wait_st();
+            mma_fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(&sh.p_full[t][i]);
+          }
+          float l0, l1;
+          unpack_f32(add_f32x2(sum[0], sum[1]), l0, l1);
+          l = fmaf(l0 + l1, power_of_two(-shift), l);
+        }
+      }
+      tile_no += (u32)p.tiles;
+      m -= kLift;                                            // what the weights and their sum count from
+      const bool two = split && p.tiles > 1;                 // both warpgroups have a part of the same rows
+      if (two && t == 1) sh.half_ml[row] = make_float2(m, l);
+      for (int u = 0; u < 2; ++u) {                          // each keeps count of both outputs' phases
+        if (u == 1 && split && !two) continue;
+        if (u == t || two) fine = fine && wait(&sh.o_full[u], (o_phase >> u) & 1);
+        o_phase ^= 1u << u;
+      }
+      mma_fence_after();
+      float f0 = 1.0f, f1 = 0.0f;
+      if (two) {
+        fine = fine && meet();
+        if (t == 0) {
+          const float2 other = sh.half_ml[row];
+          const float top = fmaxf(m, other.x), base = top == -INFINITY ? 0.0f : top;
+          f0 = exp2_approx(m - base);
+          f1 = exp2_approx(other.x - base);
+          l = l * f0 + other.y * f1;
+          m = top;
+        }
+      }
+      auto output32 = [&](float *o, int col) {               // 32 columns of the row's output, not yet divided by l
+        tmem_ld32(o, outputs + col);
+        tmem_wait_ld();
+        keep(o);
+        if (two) {
+          float x[32];
+          tmem_ld32(x, outputs + D + col);
+          tmem_wait_ld();
+          keep(x);
+#pragma unroll
+          for (int k = 0; k < 32; ++k) o[k] = f0 * o[k] + f1 * x[k];
+        }
+      };
+      auto output = [&](float *o, int col) {                 // the same for kCols columns, with one wait where it can be
+        if (two) {
+#pragma unroll
+          for (int k = 0; k < kCols; k += 32) output32(o + k, col + k);
+          return;
+        }
+#pragma unroll
+        for (int k = 0; k < kCols; k += 32) tmem_ld32(o + k, outputs + col + k);
+        tmem_wait_ld();
+#pragma unroll
+        for (int k = 0; k < kCols; k += 32) keep(o + k);
+      };
+      fine = write_part<T, D, kCols>((const Attn &)a, NoRows{}, sh, p, r, valid, mine, fine, unit_row, m, l, meet, output, output32);
+      mma_fence_before();
+      if (two || !p.whole) fine = fine && meet();            // sh.last and the other's output are free again
+      part_done(no);
+    }
+  } else {
+    fewer_registers<kCodedOtherRegs>();
+    if (warp == 8) {
+      // ---------------------------------------------------------------- the products, as in the 16-bit cache's kernel
+      constexpr u32 kScoreShape = mma_shape<__half>(kTileKeys, false), kOutShape = mma_shape<__half>(D, true);
+      constexpr u32 kChunk = (kTileKeys * 128) >> 4, kTile = S::tile_bytes >> 4;
+      const u32 tm = uniform(tmem), q_at = uniform(operand(sh.q[0], 16)), k_at = uniform(operand(sh.kv[0], 16)), v_at = uniform(operand(sh.kv[0], kTileKeys * 128));
+      u32 stage = 0, kv_phase = 0, q_phase = 0, p_phase = 0;          // bit t of the last two
+      bool fine = true;
+      auto scores_of = [&](u32 t, u32 q_tile, u32 k_stage, bool last, bool frees, u32 v_stage) {
+        if (one_lane()) {
+#pragma unroll
+          for (u32 i = 0; i < D / 16; ++i)
+            mma_ss(tm + kScores + t * 128, q_at + q_tile * kTile + (i >> 2) * kChunk + (i & 3) * 2, k_at + k_stage * kTile + (i >> 2) * kChunk + (i & 3) * 2, kScoreShape, i > 0);
+          mma_commit(&sh.s_full[t]);
+          if (frees) {
+            if (v_stage != k_stage) mma_commit(&sh.kv_empty[v_stage]);
+            mma_commit(&sh.kv_empty[k_stage]);
+          }
+          if (last) mma_commit(&sh.q_empty[q_tile]);
+        }
+        __syncwarp();
+      };
+      auto outputs_of = [&](u32 t, u32 v_stage, u32 half, bool add, bool last, bool frees) {
+        if (one_lane()) {
+#pragma unroll
+          for (u32 k = 0; k < kTileKeys / 32; ++k)
+            mma_ts(tm + kOutputs + t * D, tm + kScores + t * 128 + (half * 4 + k) * 8, v_at + v_stage * kTile + (half * 4 + k) * (2048 >> 4), kOutShape, add || k > 0);
+          if (last) mma_commit(&sh.o_full[t]);
+          if (frees) mma_commit(&sh.kv_empty[v_stage]);
+        }
+        __syncwarp();
+      };
+      auto step = [&]() { if (++stage == (u32)S::stages) { stage = 0; kv_phase ^= 1; } };
+      for (u32 no = 0; fine; ++no) {
+        PartInfo p;
+        if (!__all_sync(0xffffffffu, take_part(no, p))) break;
+        const u32 n_tiles = uniform((u32)p.tiles);
+        fine = wait(&sh.q_full[0], q_phase & 1);
+        q_phase ^= 1;
+        if (uniform(p.rows <= kTileRows)) {
+          // one row tile: key tile i goes to place i & 1; the ring holds key, value, key, value ...
+          auto ahead = [&](u32 by, u32 &ph) {                         // the stage `by` fills after this one
+            const u32 i = stage + by;
+            ph = i >= (u32)S::stages ? kv_phase ^ 1 : kv_phase;
+            return i >= (u32)S::stages ? i - S::stages : i;
+          };
+          for (u32 i = 0; i < 2 && i < n_tiles && fine; ++i) {
+            u32 ph;
+            const u32 k_stage = ahead(2 * i, ph);
+            fine = wait(&sh.kv_full[k_stage], ph);
+            if (!fine) break;
+            mma_fence_after();
+            scores_of(i, 0, k_stage, i + 1 == n_tiles, true, k_stage);
+          }
+          for (u32 at = 0; at < n_tiles && fine; ++at) {
+            u32 v_ph, k_ph;
+            const u32 t = at & 1, v_stage = ahead(1, v_ph), k_stage = ahead(4, k_ph);
+            const bool more = at + 2 < n_tiles;
+            // with four stages the keys of the next but one tile come to the stage of this tile's, whose scores are done
+            fine = wait(&sh.kv_full[v_stage], v_ph) && (!more || wait(&sh.kv_full[k_stage], k_ph));
+            for (u32 half = 0; half < 2 && fine; ++half) {
+              fine = wait(&sh.p_full[t][half], (p_phase >> t) & 1);
+              if (!fine) break;
+              mma_fence_after();
+              outputs_of(t, v_stage, half, at > 1 || half > 0, half == 1 && !more, half == 1);
+            }
+            p_phase ^= 1u << t;
+            if (more && fine) scores_of(t, 0, k_stage, at + 3 == n_tiles, true, k_stage);
+            step();
+            step();
+          }
+          part_done(no);
+          continue;
+        }
+        fine = fine && wait(&sh.q_full[1], q_phase >> 1) && wait(&sh.kv_full[stage], kv_phase);
+        q_phase ^= 2;
+        if (!fine) break;
+        mma_fence_after();
+        for (u32 t = 0; t < 2; ++t) scores_of(t, t, stage, n_tiles == 1, t == 1, stage);
+        step();
+        fine = wait(&sh.kv_full[stage], kv_phase);
+        for (u32 at = 0; at < n_tiles && fine; ++at) {
+          // here stage holds the tile's values, and they have arrived
+          const u32 v_stage = stage;
+          const bool more = at + 1 < n_tiles;
+          step();
+          const u32 k_stage = stage;
+          if (more && at == 0) fine = wait(&sh.kv_full[k_stage], kv_phase);
+          if (more) step();                                           // to the next tile's values
+#pragma unroll
+          for (u32 t = 0; t < 2; ++t) {
+            const bool final_t = t == 1;
+            for (u32 half = 0; half < 2; ++half) {
+              fine = fine && wait(&sh.p_full[t][half], (p_phase >> t) & 1);
+              if (!fine) break;
+              mma_fence_after();
+              outputs_of(t, v_stage, half, at > 0 || half > 0, half == 1 && !more, half == 1 && !more && final_t);
+            }
+            p_phase ^= 1u << t;
+            if (!fine) break;
+            if (more) {
+              scores_of(t, t, k_stage, at + 2 == n_tiles, final_t, v_stage);
+              // what the next tile needs, looked at while these products run: its values, then the keys after it
+              if (t == 0) fine = wait(&sh.kv_full[stage], kv_phase);
+              if (fine && final_t && at + 2 < n_tiles) {
+                const u32 after = stage + 1 == (u32)S::stages ? 0 : stage + 1;
+                fine = wait(&sh.kv_full[after], after ? kv_phase : kv_phase ^ 1);
+              }
+            }
+          }
+        }
+        part_done(no);
+      }
+      // tensor memory is given back, and shared memory left, only when no product uses them any more
+      if (one_lane()) mma_commit(&sh.drained);
+      __syncwarp();
+      drain(&sh.drained, 0);
+    } else if (warp == 9) {
+      // ---------------------------------------------------------------- the copies of codes
+      const int boxes = kHalfKeys / (int)box_rows;                    // at most 8: a lane each
+      int stage = 0;
+      u32 phase = 1;                                                  // the first round finds the stages free
+      bool fine = true;
+      PartInfo p;
+      for (u32 no = 0; fine && take_part(no, p); ++no) {
+        for (int at = 0; at < p.tiles && fine; ++at) {
+          int page[2], in[2];
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const int key = (p.tile + at) * kTileKeys + half * kHalfKeys + lane * (int)box_rows;
+            page[half] = (int)a.n_pages;                              // past the last page: zeros
+            in[half] = 0;
+            if (lane < boxes && key < p.hi && key + (int)box_rows > p.lo) {
+              const u32 pi = (u32)key / a.page;
+              const int pg = __ldg(a.tables + (i64)p.r * a.tab_r + pi);
+              if ((u32)pg < a.n_pages) { page[half] = pg; in[half] = (int)((u32)key - pi * a.page); }
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {                               // keys, then values
+            const int half = i & 1;
+            fine = fine && wait(&sh.codes_empty[stage], phase);
+            if (!fine) break;
+            if (lane == 0) bar_expect(&sh.codes_full[stage], (u32)S::half_bytes);
+            __syncwarp();
+            if (lane < boxes) copy_box(sh.codes[stage] + lane * (int)box_rows * D, i < 2 ? &keys : &values, 0, in[half], p.h, page[half], &sh.codes_full[stage]);
+            if (++stage == S::halves) { stage = 0; phase ^= 1; }
+          }
+        }
+        part_done(no);
+      }
+      // No copy is left in flight, even where the warps that wait for it have given up: each stage's last one.
+      for (int i = 0; i < S::halves; ++i) drain(&sh.codes_full[i], i < stage ? phase ^ 1 : phase);
+    } else if (warp == 10) {
+      // ---------------------------------------------------------------- the scales
+      // A lane has keys lane, lane + 32 ... of a tile.  Of the finite scales of a tile's values the largest one's power of two becomes the
+      // tile's: factors are then below 2^14 (e4m3; its decoded codes are below 2) or 2^8 (whole numbers, below 2^7).
+      constexpr int kTop = F == kE4m3 ? 13 : 7, kUnitLog = F == kE4m3 ? 8 : 0, kRange = 100;
+      u32 tile_no = 0;
+      bool fine = true;
+      PartInfo p;
+      for (u32 no = 0; fine && take_part(no, p); ++no) {
+        for (int at = 0; at < p.tiles + kScalesAhead && fine; ++at) {
+          if (at < p.tiles) {
+            const u32 x = tile_no + (u32)at, slot = x % kScaleSlots;
+            fine = wait(&sh.scales_empty[slot], ((x / kScaleSlots) & 1) ^ 1);
+            if (!fine) break;
+#pragma unroll
+            for (int j = 0; j < kTileKeys / 32; ++j) {
+              const int key = (p.tile + at) * kTileKeys + j * 32 + lane;
+              i64 page = 0, in = 0;
+              u32 bytes = 0;                                          // zeros
+              if (key >= p.lo && key < p.hi) {
+                const u32 pi = (u32)key / a.page;
+                const int pg = __ldg(a.tables + (i64)p.r * a.tab_r + pi);
+                if ((u32)pg < a.n_pages) { page = pg; in = (i64)((u32)key - pi * a.page); bytes = 4; }
+              }
+              cp_async4(&sh.k_scale[slot][j * 32 + lane], a.ks + (i64)p.h * a.ks_h + page * a.ks_p + in * a.ks_t, bytes);
+              cp_async4(&sh.v_factor[slot][j * 32 + lane], a.vs + (i64)p.h * a.vs_h + page * a.vs_p + in * a.vs_t, bytes);
+            }
+          }
+          cp_async_commit();
+          if (at < kScalesAhead) continue;
+          cp_async_wait<kScalesAhead>();
+          const u32 slot = (tile_no + (u32)(at - kScalesAhead)) % kScaleSlots;
+          float v[kTileKeys / 32];
+          u32 most = 0;
+#pragma unroll
+          for (int j = 0; j < kTileKeys / 32; ++j) {
+            v[j] = __uint_as_float(sh.v_factor[slot][j * 32 + lane]);
+            if (!isfinite(v[j])) {
+              sh.k_scale[slot][j * 32 + lane] = __int_as_float(0x7fffffff);
+              v[j] = 0.0f;
+            }
+            most = max(most, __float_as_uint(fabsf(v[j])));
+          }
+          most = __reduce_max_sync(0xffffffffu, most);
+          const int e = min(kRange, max(-kRange, (int)(most >> 23) - 127)) - kTop;
+          const float down = power_of_two(-e);
+#pragma unroll
+          for (int j = 0; j < kTileKeys / 32; ++j) {
+            const float f = fminf(fmaxf(v[j] * down, -power_of_two(kTop + 1)), power_of_two(kTop + 1));   // scales past 2^100 too are finite here
+            const __half hi = __float2half_rn(f), lo = __float2half_rn(f - __half2float(hi));
+            sh.v_factor[slot][j * 32 + lane] = (u32)__half_as_ushort(hi) | ((u32)__half_as_ushort(lo) << 16);
+          }
+          if (lane == 0) sh.shift[slot] = e + kUnitLog;
+          __syncwarp();
+          if (lane == 0) bar_arrive(&sh.scales_full[slot]);
+        }
+        tile_no += (u32)p.tiles;
+        part_done(no);
+      }
+      cp_async_wait<0>();
+    } else if (warp >= 12) {
+      // ---------------------------------------------------------------- codes to float16
+      constexpr int P = D / 16, kEach = kHalfKeys * P / 128;          // pieces of 16 codes: of a row, of a thread and half
+      const int me = tid - 12 * 32;
+      int stage = 0, from = 0;
+      u32 phase = 1, from_phase = 0, tile_no = 0;
+      bool fine = true;
+      PartInfo p;
+      for (u32 no = 0; fine && take_part(no, p); ++no) {
+        for (int at = 0; at < p.tiles && fine; ++at, ++tile_no) {
+          const u32 slot = tile_no % kScaleSlots;
+#pragma unroll
+          for (int kv = 0; kv < 2; ++kv) {
+            fine = fine && wait(&sh.kv_empty[stage], phase);
+            if (kv) fine = fine && wait(&sh.scales_full[slot], (tile_no / kScaleSlots) & 1);
+            if (!fine) break;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              fine = fine && wait(&sh.codes_full[from], from_phase);
+              if (!fine) break;
+              uint4 w[kEach];
+#pragma unroll
+              for (int i = 0; i < kEach; ++i) w[i] = *(const uint4 *)(sh.codes[from] + (i * 128 + me) * 16);
+              __syncwarp();
+              if (lane == 0) bar_arrive(&sh.codes_empty[from]);
+              if (++from == S::halves) { from = 0; from_phase ^= 1; }
+#pragma unroll
+              for (int i = 0; i < kEach; ++i) {
+                const int x = i * 128 + me, row = x / P + half * kHalfKeys, piece = (x % P) * 2;
+                u32 h[8];
+                decode_along<F>(w[i].x, h[0], h[1]);
+                decode_along<F>(w[i].y, h[2], h[3]);
+                decode_along<F>(w[i].z, h[4], h[5]);
+                decode_along<F>(w[i].w, h[6], h[7]);
+                if (kv) {
+                  const u32 f = sh.v_factor[slot][row], hi = __byte_perm(f, 0, 0x1010), lo = __byte_perm(f, 0, 0x3232);
+#pragma unroll
+                  for (int k = 0; k < 8; ++k) h[k] = fma_f16x2(h[k], hi, mul_f16x2(h[k], lo));
+                }
+                // the second chunk's lanes write their second half first, so that eight lanes' pieces lie in different banks
+                const bool swap = (piece >> 3) != 0;
+                unsigned char *const to = sh.kv[stage] + (piece >> 3) * (kTileKeys * 128) + row * 128;
+                const int at0 = ((piece & 7) ^ (row & 7)) << 4, at1 = (((piece + 1) & 7) ^ (row & 7)) << 4;
+                *(uint4 *)(to + (swap ? at1 : at0)) = swap ? make_uint4(h[4], h[5], h[6], h[7]) : make_uint4(h[0], h[1], h[2], h[3]);
+                *(uint4 *)(to + (swap ? at0 : at1)) = swap ? make_uint4(h[0], h[1], h[2], h[3]) : make_uint4(h[4], h[5], h[6], h[7]);
+              }
+            }
+            if (!fine) break;
+            fence_async();
+            __syncwarp();
+            if (lane == 0) {
+              bar_arrive(&sh.kv_full[stage]);
+              if (kv) bar_arrive(&sh.scales_empty[slot]);
+            }
+            if (++stage == S::stages) { stage = 0; phase ^= 1; }
+          }
+        }
+        part_done(no);
+      }
+    } else {
+      // ---------------------------------------------------------------- the parts
+      Cursor c = plan.first;
+      u32 left = plan.end - plan.begin;
+      bool more = true;
+      for (u32 told = 0; more; ++told) {
+        settle<kRows, kTileKeys, kOver>(a, c, left, plan.fill);
+        const u32 slot = told % kParts;
+        PartInfo p{};
+        more = left != 0;
+        if (more) {
+          p.r = (int)c.r; p.h = (int)c.h; p.len = c.req.len; p.n = c.req.n; p.q0 = c.req.q0;
+          p.row0 = c.m * kRows;
+          p.rows = (int)min((i64)kRows, (i64)c.req.n * a.group - p.row0);
+          const int to = (int)min((u32)c.span.tiles, (u32)c.at + left);
+          p.tile = c.span.first + c.at;
+          p.tiles = to - c.at;
+          p.lo = c.span.lo; p.hi = c.span.hi;
+          p.whole = c.at == 0 && to == c.span.tiles;
+          if (!p.whole) {
+            const u32 unit0 = plan.end - left - (u32)c.at;
+            p.i0 = plan.shares.owner(unit0);
+            p.i1 = plan.shares.owner(unit0 + (u32)c.span.tiles - 1);
+          }
+          left -= (u32)p.tiles;
+          c.at = to;
+        }
+        if (!wait(&sh.part_empty[slot], ((told / kParts) & 1) ^ 1)) break;
+        if (lane == 0) {
+          sh.part[slot] = p;
+          bar_arrive(&sh.part_full[slot]);
+        }
+        __syncwarp();
+      }
+    }
+  }
+  mma_fence_before();
+  __syncthreads();
+  mma_fence_after();
+  if (warp == 8) tmem_free(tmem, 512);
+  if (tid == 0 && sh.failed) *error_word(a) = 1;
+}
+
+bool codes_map(CUtensorMap *map, const CodedAttn &a, const void *base, i64 st, i64 sh, i64 sp, int dim, u32 box_rows) {
+  const cuuint64_t dims[4] = {(cuuint64_t)dim, a.page, a.hkv, a.n_pages};
+  const cuuint64_t strides[3] = {(cuuint64_t)st, (cuuint64_t)sh, (cuuint64_t)sp};
+  const cuuint32_t box[4] = {(cuuint32_t)dim, box_rows, 1, 1}, step[4] = {1, 1, 1, 1};
+  return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void *>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                   CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, Format F, int D, Scores SCORES>
+cudaError_t launch_coded_chunk(const CodedAttn &a, const CUtensorMap &k, const CUtensorMap &v, u32 box_rows, u32 sms, cudaStream_t s) {
+  static bool ready[64] = {};
+  constexpr size_t bytes = sizeof(CodedChunkShared<D>) + 1024;
+  static_assert(bytes <= 227 * 1024, "shared memory of one block");
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= 64) return cudaErrorInvalidDevice;
+  if (!ready[dev]) {
+    e = cudaFuncSetAttribute(coded_chunk_kernel<T, F, D, SCORES>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e != cudaSuccess) return e;
+    // the warps' register shares come out of what the block is launched with: with fewer they would wait for ever
+    cudaFuncAttributes f;
+    e = cudaFuncGetAttributes(&f, coded_chunk_kernel<T, F, D, SCORES>);
+    if (e != cudaSuccess) return e;
+    if (f.numRegs * kCodedThreads < kCodedSoftmaxRegs * 256 + kCodedOtherRegs * 256) return cudaErrorInvalidKernelImage;
+    ready[dev] = true;
+  }
+  return launch_kernel<Attn>(coded_chunk_kernel<T, F, D, SCORES>, sms, kCodedThreads, bytes, s, a, k, v, box_rows);
+}
+
+template <typename T, Format F, int D>
+cudaError_t pick_coded_scores(const CodedAttn &a, const CUtensorMap &k, const CUtensorMap &v, u32 box_rows, u32 sms, cudaStream_t s) {
+  if (a.softcap > 64.0f) return launch_coded_chunk<T, F, D, kLargeCap>(a, k, v, box_rows, sms, s);
+  return a.softcap > 0.0f || a.slopes ? launch_coded_chunk<T, F, D, kSmallCap>(a, k, v, box_rows, sms, s)
+                                      : launch_coded_chunk<T, F, D, kPlain>(a, k, v, box_rows, sms, s);
+}
+
+template <typename T, Format F>
+cudaError_t pick_coded_chunk_dim(const CodedAttn &a, const CUtensorMap &k, const CUtensorMap &v, u32 box_rows, int dim, u32 sms, cudaStream_t s) {
+  if (dim == 64) return pick_coded_scores<T, F, 64>(a, k, v, box_rows, sms, s);
+  if (dim == 96) return pick_coded_scores<T, F, 96>(a, k, v, box_rows, sms, s);
+  return pick_coded_scores<T, F, 128>(a, k, v, box_rows, sms, s);
+}
+
+// False where no tensor map of the pages can be made: nothing ran.
+template <Format F>
+bool launch_coded_chunk_of(const CodedAttn &a, int dtype, int dim, u32 sms, cudaStream_t s, cudaError_t *e) {
+  if (!encoder() || a.n_pages == 0) return false;
+  u32 box_rows = a.page & (0u - a.page);               // the largest power of two in the page size, so that a box stays in its page
+  if (box_rows > (u32)kHalfKeys) box_rows = kHalfKeys;
+  CUtensorMap k, v;
+  if (!codes_map(&k, a, a.kp, a.k_t, a.k_h, a.k_p, dim, box_rows) || !codes_map(&v, a, a.vp, a.v_t, a.v_h, a.v_p, dim, box_rows)) return false;
+  *e = dtype == 0 ? pick_coded_chunk_dim<__nv_bfloat16, F>(a, k, v, box_rows, dim, sms, s) : pick_coded_chunk_dim<__half, F>(a, k, v, box_rows, dim, sms, s);
+  return true;
+}
+
+}  // namespace
+}  // namespace paged
+}  // namespace gorio

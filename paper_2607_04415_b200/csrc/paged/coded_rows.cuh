@@ -45,10 +45,6 @@ __device__ __forceinline__ int code_piece(int row, int piece) {
   return row * P + (piece ^ ((row >> 2) & 1));   // 96 bytes: four rows lie apart by themselves, the next four one piece on
 }
 
-__device__ __forceinline__ void cp_async4(void *to, const void *from, u32 bytes) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_addr(to)), "l"(from), "r"(bytes) : "memory");
-}
-
 // log2 of a value's scale, cut to what the running maximum counts
 __device__ __forceinline__ float scale_log2(float scale) {
   float e;

@@ -312,7 +312,13 @@ extern "C" int gorio_paged_attention_quantized(const gorio_quantized_attention_d
     a.ks_p = a.ks_h = a.ks_t = a.vs_p = a.vs_h = a.vs_t = 0;
   }
   const cudaStream_t s = (cudaStream_t)cuda_stream;
-  const cudaError_t e = d->format == GORIO_CODES_E4M3 ? launch_coded_rows_e4m3(a, (int)p.dtype, (int)p.dim, (u32)sms, s)
-                                                      : launch_coded_rows_int8(a, (int)p.dtype, (int)p.dim, (u32)sms, s);
+  cudaError_t e = cudaSuccess;
+  if (!takes_rows(p)) {
+    const bool ran = d->format == GORIO_CODES_E4M3 ? launch_coded_chunk_e4m3(a, (int)p.dtype, (int)p.dim, (u32)sms, s, &e)
+                                                   : launch_coded_chunk_int8(a, (int)p.dtype, (int)p.dim, (u32)sms, s, &e);
+    if (ran) return launched(e, "quantized attention");
+  }
+  e = d->format == GORIO_CODES_E4M3 ? launch_coded_rows_e4m3(a, (int)p.dtype, (int)p.dim, (u32)sms, s)
+                                    : launch_coded_rows_int8(a, (int)p.dtype, (int)p.dim, (u32)sms, s);
   return launched(e, "quantized attention");
 }
