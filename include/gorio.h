@@ -456,7 +456,8 @@ int gorio_paged_attention(const gorio_paged_attention_desc *d, void *cuda_stream
  * 8 bits (L = 127).  The store takes a row's largest magnitude M and writes, all in 32-bit arithmetic,
  *   scale = M / L,   inverse = L / M,   code = x * inverse rounded to the nearest code, ties to even.
  * A row with M below 2^-100 is stored as zeros with scale 0; a row with a number that is not finite gets codes 0 and the scale NaN, so
- * that all of it reads as NaN.  The codes 0x7F and 0xFF of e4m3, which the store does not write, read as 480 and -480.
+ * that all of it reads as NaN.  e4m3's two codes that are no numbers (0x7F, 0xFF) are never written; in attention they reach the queries that see their
+ * key, as NaN or as 480, and no others.
  */
 enum { GORIO_CODES_E4M3 = 0, GORIO_CODES_INT8 = 1 };
 

@@ -134,8 +134,7 @@ __global__ void __launch_bounds__(kThreads) load_kernel(const RowsArgs a) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const float2 v = unpack2<__half>(h[k]);
-      // an empty slot's zeros stay zeros; the factor of the decoded code is a power of two
-      h[k] = pack2<T>(v.x * kUnit<F> * scale[i], v.y * kUnit<F> * scale[i]);
+      h[k] = pack2<T>(v.x * scale[i], v.y * scale[i]);
     }
     __stcs((uint4 *)(s.wide + (first + i) * s.wide_t + lane * 8), make_uint4(h[0], h[1], h[2], h[3]));
   }

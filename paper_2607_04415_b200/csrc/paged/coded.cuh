@@ -1,10 +1,9 @@
 // Keys and values held in 8 bits: what the kernels of a quantised cache share.
 //
 // A row (a token's numbers of one key head) is 8-bit codes and a scale of 32 bits; code times scale is the value.  Codes are
-// e4m3 (4 bits of exponent, 3 of mantissa) or whole numbers.  Both become 16-bit floating-point numbers exactly: an e4m3 code, with
-// its 7 low bits 7 places up, is the number times 2^-8 in float16, below its normal numbers too; a whole number's byte under
-// the exponent of 1024 is 1024 more than itself.  That is 2 to 4 operations for two codes, where the conversion instruction would also make
-// numbers that are not finite of e4m3's two codes for them.  The store never writes those; here they read as +-480.
+// e4m3 (4 bits of exponent, 3 of mantissa) or whole numbers.  Both become 16-bit floating-point numbers exactly: e4m3 by the conversion
+// instruction, two codes in one cycle (by shifts and masks, 14 cycles for four codes where this takes 2); a whole number's byte
+// under the exponent of 1024 is 1024 more than itself (4 cycles).
 #pragma once
 #include "common.cuh"
 #include "mma.cuh"
@@ -18,14 +17,13 @@ struct CodedAttn : Attn {
 };
 
 enum Format { kE4m3 = 0, kInt8 = 1 };
-// what a decoded code has to be multiplied by
-template <Format F>
-constexpr float kUnit = F == kE4m3 ? 256.0f : 1.0f;
 template <Format F>
 constexpr float kLargest = F == kE4m3 ? 448.0f : 127.0f;
 
-// two e4m3 codes in the high bytes of the halves of t
-__device__ __forceinline__ u32 decode_e4m3(u32 t) { return (t & 0x80008000u) | ((t >> 1) & 0x3f803f80u); }
+// the two e4m3 codes in a half of w
+__device__ __forceinline__ void decode_e4m3(u32 w, u32 &lo, u32 &hi) {
+  asm("{ .reg .b16 x, y; mov.b32 {x, y}, %2; cvt.rn.f16x2.e4m3x2 %0, x; cvt.rn.f16x2.e4m3x2 %1, y; }" : "=r"(lo), "=r"(hi) : "r"(w));
+}
 // two bytes of w ^ 0x80.., chosen by `which`
 __device__ __forceinline__ u32 decode_int8(u32 w, u32 which) {
   const u32 x = __byte_perm(w, 0x64646464u, which);
@@ -34,29 +32,32 @@ __device__ __forceinline__ u32 decode_int8(u32 w, u32 which) {
   return r;
 }
 
-// Four codes: bytes 0 and 2, bytes 1 and 3.
+// Four codes in their order; bytes 0 and 2, bytes 1 and 3.
+template <Format F>
+__device__ __forceinline__ void decode_along(u32 w, u32 &lo, u32 &hi) {
+  if (F == kE4m3) {
+    decode_e4m3(w, lo, hi);
+  } else {
+    w ^= 0x80808080u;
+    lo = decode_int8(w, 0x4140);
+    hi = decode_int8(w, 0x4342);
+  }
+}
 template <Format F>
 __device__ __forceinline__ void decode_across(u32 w, u32 &even, u32 &odd) {
   if (F == kE4m3) {
-    even = decode_e4m3(w << 8);
-    odd = decode_e4m3(w);
+    decode_e4m3(__byte_perm(w, 0, 0x3120), even, odd);
   } else {
     w ^= 0x80808080u;
     even = decode_int8(w, 0x4240);
     odd = decode_int8(w, 0x4341);
   }
 }
-// Four codes in their order.
+// 480 in the place of e4m3 codes that are no numbers: the store writes none, but what no query sees may hold any
 template <Format F>
-__device__ __forceinline__ void decode_along(u32 w, u32 &lo, u32 &hi) {
-  if (F == kE4m3) {
-    lo = decode_e4m3(__byte_perm(w, 0, 0x1404));
-    hi = decode_e4m3(__byte_perm(w, 0, 0x3424));
-  } else {
-    w ^= 0x80808080u;
-    lo = decode_int8(w, 0x4140);
-    hi = decode_int8(w, 0x4342);
-  }
+__device__ __forceinline__ u32 finite_codes(u32 h) {
+  if (F == kE4m3) asm("min.f16x2 %0, %0, %1;" : "+r"(h) : "r"(0x5f805f80u));
+  return h;
 }
 
 // 4 bytes, or zeros

@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
           }
         }
         const float f = query_factor(top);
-        to_dot = kUnit<F> / f;                               // powers of two
+        to_dot = 1.0f / f;                                   // powers of two
 #pragma unroll
         for (int k = 0; k < D / 8; ++k) {
           u32 w[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
@@ -464,8 +464,8 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
     } else if (warp == 10) {
       // ---------------------------------------------------------------- the scales
       // A lane has keys lane, lane + 32 ... of a tile.  Of the finite scales of a tile's values the largest one's power of two becomes the
-      // tile's: factors are then below 2^14 (e4m3; its decoded codes are below 2) or 2^8 (whole numbers, below 2^7).
-      constexpr int kTop = F == kE4m3 ? 13 : 7, kUnitLog = F == kE4m3 ? 8 : 0, kRange = 100;
+      // tile's: factors are then below 2^7 (e4m3, whose codes are at most 448) or 2^8 (whole numbers, at most 128).
+      constexpr int kTop = F == kE4m3 ? 6 : 7, kRange = 100;
       u32 tile_no = 0;
       bool fine = true;
       PartInfo p;
@@ -513,7 +513,7 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
             const __half hi = __float2half_rn(f), lo = __float2half_rn(f - __half2float(hi));
             sh.v_factor[slot][j * 32 + lane] = (u32)__half_as_ushort(hi) | ((u32)__half_as_ushort(lo) << 16);
           }
-          if (lane == 0) sh.shift[slot] = e + kUnitLog;
+          if (lane == 0) sh.shift[slot] = e;
           __syncwarp();
           if (lane == 0) bar_arrive(&sh.scales_full[slot]);
         }
@@ -524,7 +524,11 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
     } else if (warp >= 12) {
       // ---------------------------------------------------------------- codes to float16
       constexpr int P = D / 16, kEach = kHalfKeys * P / 128;          // pieces of 16 codes: of a row, of a thread and half
+      // Which piece: four of a row and 64-byte chunk to four neighbouring lanes.  Eight lanes then write even places of one row and odd ones of
+      // the next, or the other way round, which lie in different banks.
       const int me = tid - 12 * 32;
+      auto row_at = [&](int i) { return P == 6 ? (i * 128 + me) / 6 : (i / (P / 4)) * 32 + (me >> 2); };
+      auto piece_at = [&](int i) { return P == 6 ? (i * 128 + me) % 6 : (i % (P / 4)) * 4 + (me & 3); };
       int stage = 0, from = 0;
       u32 phase = 1, from_phase = 0, tile_no = 0;
       bool fine = true;
@@ -532,6 +536,8 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
       for (u32 no = 0; fine && take_part(no, p); ++no) {
         for (int at = 0; at < p.tiles && fine; ++at, ++tile_no) {
           const u32 slot = tile_no % kScaleSlots;
+          const int key0 = (p.tile + at) * kTileKeys;
+          const bool every = key0 >= p.every0 && key0 + kTileKeys <= p.every1;      // all rows see all keys of the tile
 #pragma unroll
           for (int kv = 0; kv < 2; ++kv) {
             fine = fine && wait(&sh.kv_empty[stage], phase);
@@ -543,13 +549,13 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
               if (!fine) break;
               uint4 w[kEach];
 #pragma unroll
-              for (int i = 0; i < kEach; ++i) w[i] = *(const uint4 *)(sh.codes[from] + (i * 128 + me) * 16);
+              for (int i = 0; i < kEach; ++i) w[i] = *(const uint4 *)(sh.codes[from] + row_at(i) * D + piece_at(i) * 16);
               __syncwarp();
               if (lane == 0) bar_arrive(&sh.codes_empty[from]);
               if (++from == S::halves) { from = 0; from_phase ^= 1; }
 #pragma unroll
               for (int i = 0; i < kEach; ++i) {
-                const int x = i * 128 + me, row = x / P + half * kHalfKeys, piece = (x % P) * 2;
+                const int row = row_at(i) + half * kHalfKeys, piece = piece_at(i) * 2;
                 u32 h[8];
                 decode_along<F>(w[i].x, h[0], h[1]);
                 decode_along<F>(w[i].y, h[2], h[3]);
@@ -557,15 +563,16 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
                 decode_along<F>(w[i].w, h[6], h[7]);
                 if (kv) {
                   const u32 f = sh.v_factor[slot][row], hi = __byte_perm(f, 0, 0x1010), lo = __byte_perm(f, 0, 0x3232);
+                  if (F == kE4m3 && !every) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) h[k] = finite_codes<F>(h[k]);
+                  }
 #pragma unroll
                   for (int k = 0; k < 8; ++k) h[k] = fma_f16x2(h[k], hi, mul_f16x2(h[k], lo));
                 }
-                // the second chunk's lanes write their second half first, so that eight lanes' pieces lie in different banks
-                const bool swap = (piece >> 3) != 0;
                 unsigned char *const to = sh.kv[stage] + (piece >> 3) * (kTileKeys * 128) + row * 128;
-                const int at0 = ((piece & 7) ^ (row & 7)) << 4, at1 = (((piece + 1) & 7) ^ (row & 7)) << 4;
-                *(uint4 *)(to + (swap ? at1 : at0)) = swap ? make_uint4(h[4], h[5], h[6], h[7]) : make_uint4(h[0], h[1], h[2], h[3]);
-                *(uint4 *)(to + (swap ? at0 : at1)) = swap ? make_uint4(h[0], h[1], h[2], h[3]) : make_uint4(h[4], h[5], h[6], h[7]);
+                *(uint4 *)(to + (((piece & 7) ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+                *(uint4 *)(to + (((piece + 1) & 7 ^ (row & 7)) << 4)) = make_uint4(h[4], h[5], h[6], h[7]);
               }
             }
             if (!fine) break;
@@ -598,6 +605,7 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
           p.tile = c.span.first + c.at;
           p.tiles = to - c.at;
           p.lo = c.span.lo; p.hi = c.span.hi;
+          all_see(a, p);
           p.whole = c.at == 0 && to == c.span.tiles;
           if (!p.whole) {
             const u32 unit0 = plan.end - left - (u32)c.at;

@@ -4,7 +4,7 @@
 // different comes from the 8 bits.  The same bytes in flight are twice as many keys, so a warp's tile is 32 keys.  Codes
 // become float16 in registers, exactly, in the lanes and the order in which the matrix instructions want them:
 //   keys     a 16-byte piece of a row is what one product over 16 elements takes.  A lane gets four neighbouring codes of a
-//            key, and its queries are loaded in the order in which the codes come apart (0, 2 | 1, 3), so that nothing is moved.
+//            key, and its queries are loaded in the same order, so that nothing is moved.
 //   values   read transposed by pairs of codes, a lane gets two neighbouring columns of two neighbouring keys; taken apart they are
 //            the operand of one product for the even columns and of one for the odd ones.
 // Products of queries (float16, a power of two a row) and codes are summed in 32 bits; the key's scale comes after.  The value's scale
@@ -171,12 +171,12 @@ __global__ void __launch_bounds__(kThreads, kCodedBlocks<D>) coded_rows_kernel(c
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
       const float f = query_factor(top);
-      to_dot[i] = kUnit<F> / f;                   // powers of two
+      to_dot[i] = 1.0f / f;                       // powers of two
 #pragma unroll
       for (int k = 0; k < P; ++k) {
         const float2 lo = unpack2<T>(x[k].x), hi = unpack2<T>(x[k].y);
-        qf[k][i] = pack2<__half>(lo.x * f, hi.x * f);
-        qf[k][2 + i] = pack2<__half>(lo.y * f, hi.y * f);
+        qf[k][i] = pack2<__half>(lo.x * f, lo.y * f);
+        qf[k][2 + i] = pack2<__half>(hi.x * f, hi.y * f);
       }
     }
     float o[P][2][4];                             // even and odd columns of 16
@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(kThreads, kCodedBlocks<D>) coded_rows_kernel(c
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
           u32 b0, b1;
-          decode_across<F>(w[n], b0, b1);
+          decode_along<F>(w[n], b0, b1);
           mma_half(s[n], qf[k], b0, b1);
         }
       }
@@ -264,6 +264,10 @@ __global__ void __launch_bounds__(kThreads, kCodedBlocks<D>) coded_rows_kernel(c
         ldmatrix4t(w, vs + code_piece<D>(lane, n) * 16);
 #pragma unroll
         for (int j = 0; j < 4; ++j) decode_across<F>(w[j], even[j], odd[j]);
+        if (F == kE4m3 && !all_seen) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) { even[j] = finite_codes<F>(even[j]); odd[j] = finite_codes<F>(odd[j]); }
+        }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const u32 pf[4] = {pack2<__half>(s[2 * j][0], s[2 * j][1]), pack2<__half>(s[2 * j][2], s[2 * j][3]), pack2<__half>(s[2 * j + 1][0], s[2 * j + 1][1]),
@@ -289,8 +293,7 @@ __global__ void __launch_bounds__(kThreads, kCodedBlocks<D>) coded_rows_kernel(c
       if (row < rows) {
 #pragma unroll
         for (int n = 0; n < P; ++n)
-          *(float4 *)(mine + row * D + (n ^ (row & 1)) * 16 + t4 * 4) = make_float4(o[n][0][2 * i] * kUnit<F>, o[n][1][2 * i] * kUnit<F>, o[n][0][2 * i + 1] * kUnit<F>,
-                                                                                  o[n][1][2 * i + 1] * kUnit<F>);
+          *(float4 *)(mine + row * D + (n ^ (row & 1)) * 16 + t4 * 4) = make_float4(o[n][0][2 * i], o[n][1][2 * i], o[n][0][2 * i + 1], o[n][1][2 * i + 1]);
       }
     }
     __syncthreads();
