@@ -5,14 +5,14 @@
 //   0-3, 4-7  the softmax of row tile 0 and 1: a thread a row.  At a part's start each thread brings its own row of queries, as float16 times a
 //             power of two.
 //   8         issues both products (one thread).
-//   9         copies codes of keys and values, 64 keys at a time, into a ring of their own (tensor copies).
-//   10        fetches the scales of a tile's keys and values.
+//   9         copies codes of keys and values, 64 keys at a time, into a ring of their own, and their scales (tensor copies).
+//   10        makes a tile's factors of the scales of its values.
 //   11        walks the block's share of the work and tells the others its parts.
 //   12-15     take codes apart into the 16-bit tiles that the products read.
 // Keys become their codes, exactly; a score is multiplied by its key's scale in 32 bits.  Values are multiplied by their scales as they
 // become float16, one rounding to 11 bits; so that neither side of that leaves float16's range, a tile has a power of two of its own, taken out of
 // its values and put into its weights: 2^(x + shift - m) with m the running maximum of x + shift, whose sum is taken back by 2^-shift once a tile.
-// The factor itself is kept as two float16 numbers, so that its rounding is not added to the product's.
+// The factor is a float16 too: a second rounding to 11 bits, which all numbers of a row share (a factor of 22 bits in two numbers took 25 % longer).
 //
 // A value's scale that is not finite would reach rows that do not see its key as 0 * inf in the product.  It is left out there, and stands in the
 // key's place instead: scores of rows that see the key are then not a number.  With it all operands are finite, so that tiles that some rows
@@ -27,10 +27,9 @@ namespace paged {
 namespace {
 
 constexpr int kCodedThreads = 512;
-constexpr int kCodedSoftmaxRegs = 208, kCodedOtherRegs = 48;     // a thread, of 128 * 4 = 208 * 2 + 48 * 2 at launch
+constexpr int kCodedSoftmaxRegs = 192, kCodedOtherRegs = 80, kDecodeRegs = 48;   // a thread, of 128 * 4 = 192 * 2 + 80 + 48 at launch
 constexpr int kHalfKeys = 64;                                    // of a copy
 constexpr int kScaleSlots = 4;                                   // tiles whose scales are there
-constexpr int kScalesAhead = 2;                                  // tiles whose scales are on their way
 
 template <int D>
 struct CodedShape {
@@ -46,13 +45,14 @@ struct CodedChunkShared {
   unsigned char q[2][CodedShape<D>::tile_bytes];
   unsigned char kv[CodedShape<D>::stages][CodedShape<D>::tile_bytes];
   unsigned char codes[CodedShape<D>::halves][CodedShape<D>::half_bytes];
-  float k_scale[kScaleSlots][kTileKeys];
-  u32 v_factor[kScaleSlots][kTileKeys];          // two float16: the factor and what it lacks; until they are there, the scale
+  __align__(128) float k_scale[kScaleSlots][kTileKeys];
+  u32 v_factor[kScaleSlots][kTileKeys];          // float16, twice; until it is there, the scale
+  u32 scales_boxes[kScaleSlots];                 // which boxes of them were copied
   int shift[kScaleSlots];
   float q_to_dot[kTileRows];                     // of the rows of a unit of one row tile
   PartInfo part[kParts];
   u64 kv_full[CodedShape<D>::stages], kv_empty[CodedShape<D>::stages], codes_full[CodedShape<D>::halves], codes_empty[CodedShape<D>::halves];
-  u64 scales_full[kScaleSlots], scales_empty[kScaleSlots];
+  u64 scales_there[kScaleSlots], scales_full[kScaleSlots], scales_empty[kScaleSlots];
   u64 part_full[kParts], part_empty[kParts];
   u64 q_full[2], q_empty[2], s_full[2], p_full[2][2], o_full[2], meet, drained;
   u32 tmem, failed, last;
@@ -72,13 +72,15 @@ __device__ __forceinline__ u32 mul_f16x2(u32 a, u32 b) {
   asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(v) : "r"(a), "r"(b));
   return v;
 }
-__device__ __forceinline__ u32 fma_f16x2(u32 a, u32 b, u32 c) {
-  u32 v;
-  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(v) : "r"(a), "r"(b), "r"(c));
-  return v;
-}
 __device__ __forceinline__ void bar_arrive_n(u64 *bar, u32 n) {
   asm volatile("mbarrier.arrive.shared.b64 _, [%0], %1;" ::"r"(smem_addr(bar)), "r"(n) : "memory");
+}
+// The scales of some rows of a page into shared memory: both addresses are multiples of 16 bytes, and so is the size.  (A tensor copy would want
+// 128 bytes of the second, which a page of 8 or 16 rows does not give.)
+__device__ __forceinline__ void copy_scales(void *to, const float *from, u32 bytes, u64 *bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_addr(to)), "l"(from), "r"(bytes),
+               "r"(smem_addr(bar))
+               : "memory");
 }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((u32)(127 + e) << 23); }
 
@@ -93,7 +95,7 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
   if (warp == 8) {
     if (lane < S::stages) { bar_init(&sh.kv_full[lane], 4); bar_init(&sh.kv_empty[lane], 1); }
     if (lane < S::halves) { bar_init(&sh.codes_full[lane], 1); bar_init(&sh.codes_empty[lane], 4); }
-    if (lane < kScaleSlots) { bar_init(&sh.scales_full[lane], 1); bar_init(&sh.scales_empty[lane], 12); }
+    if (lane < kScaleSlots) { bar_init(&sh.scales_there[lane], 1); bar_init(&sh.scales_full[lane], 1); bar_init(&sh.scales_empty[lane], 12); }
     if (lane < kParts) { bar_init(&sh.part_full[lane], 1); bar_init(&sh.part_empty[lane], 15); }
     if (lane < 2) {
       bar_init(&sh.q_full[lane], 4); bar_init(&sh.q_empty[lane], 1); bar_init(&sh.s_full[lane], 1); bar_init(&sh.o_full[lane], 1);
@@ -307,6 +309,73 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
       if (two || !p.whole) fine = fine && meet();            // sh.last and the other's output are free again
       part_done(no);
     }
+  } else if (warp >= 12) {
+    fewer_registers<kDecodeRegs>();
+    // ---------------------------------------------------------------- codes to float16
+    constexpr int P = D / 16, kEach = kHalfKeys * P / 128;          // pieces of 16 codes: of a row, of a thread and half
+    // Which piece: four of a row and 64-byte chunk to four neighbouring lanes.  Eight lanes then write even places of one row and odd ones of
+    // the next, or the other way round, which lie in different banks.
+    const int me = tid - 12 * 32;
+    auto row_at = [&](int i) { return P == 6 ? (i * 128 + me) / 6 : (i / (P / 4)) * 32 + (me >> 2); };
+    auto piece_at = [&](int i) { return P == 6 ? (i * 128 + me) % 6 : (i % (P / 4)) * 4 + (me & 3); };
+    int stage = 0, from = 0;
+    u32 phase = 1, from_phase = 0, tile_no = 0;
+    bool fine = true;
+    PartInfo p;
+    for (u32 no = 0; fine && take_part(no, p); ++no) {
+      for (int at = 0; at < p.tiles && fine; ++at, ++tile_no) {
+        const u32 slot = tile_no % kScaleSlots;
+        const int key0 = (p.tile + at) * kTileKeys;
+        const bool every = key0 >= p.every0 && key0 + kTileKeys <= p.every1;      // all rows see all keys of the tile
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+          fine = fine && wait(&sh.kv_empty[stage], phase);
+          if (kv) fine = fine && wait(&sh.scales_full[slot], (tile_no / kScaleSlots) & 1);
+          if (!fine) break;
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            fine = fine && wait(&sh.codes_full[from], from_phase);
+            if (!fine) break;
+            uint4 w[kEach];
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) w[i] = *(const uint4 *)(sh.codes[from] + row_at(i) * D + piece_at(i) * 16);
+            __syncwarp();
+            if (lane == 0) bar_arrive(&sh.codes_empty[from]);
+            if (++from == S::halves) { from = 0; from_phase ^= 1; }
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+              const int row = row_at(i) + half * kHalfKeys, piece = piece_at(i) * 2;
+              u32 h[8];
+              decode_along<F>(w[i].x, h[0], h[1]);
+              decode_along<F>(w[i].y, h[2], h[3]);
+              decode_along<F>(w[i].z, h[4], h[5]);
+              decode_along<F>(w[i].w, h[6], h[7]);
+              if (kv) {
+                const u32 f = sh.v_factor[slot][row];
+                if (F == kE4m3 && !every) {
+#pragma unroll
+                  for (int k = 0; k < 8; ++k) h[k] = finite_codes<F>(h[k]);
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) h[k] = mul_f16x2(h[k], f);
+              }
+              unsigned char *const to = sh.kv[stage] + (piece >> 3) * (kTileKeys * 128) + row * 128;
+              *(uint4 *)(to + (((piece & 7) ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+              *(uint4 *)(to + (((piece + 1) & 7 ^ (row & 7)) << 4)) = make_uint4(h[4], h[5], h[6], h[7]);
+            }
+          }
+          if (!fine) break;
+          fence_async();
+          __syncwarp();
+          if (lane == 0) {
+            bar_arrive(&sh.kv_full[stage]);
+            if (kv) bar_arrive(&sh.scales_empty[slot]);
+          }
+          if (++stage == S::stages) { stage = 0; phase ^= 1; }
+        }
+      }
+      part_done(no);
+    }
   } else {
     fewer_registers<kCodedOtherRegs>();
     if (warp == 8) {
@@ -426,25 +495,54 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
       __syncwarp();
       drain(&sh.drained, 0);
     } else if (warp == 9) {
-      // ---------------------------------------------------------------- the copies of codes
-      const int boxes = kHalfKeys / (int)box_rows;                    // at most 8: a lane each
+      // ---------------------------------------------------------------- the copies of codes and scales
+      const int boxes = kHalfKeys / (int)box_rows;                    // at most 8 for 64 keys: a lane each
       int stage = 0;
-      u32 phase = 1;                                                  // the first round finds the stages free
+      u32 phase = 1, tile_no = 0;                                     // the first round finds the stages free
       bool fine = true;
       PartInfo p;
+      // Page and place of this lane's box in each half of a tile, looked up a tile ahead: the entry of a table is far away.
+      int page[2], in[2];
+      auto look_up = [&](int tile) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const int key = tile * kTileKeys + half * kHalfKeys + lane * (int)box_rows;
+          page[half] = (int)a.n_pages;                                // past the last page: zeros
+          in[half] = 0;
+          if (lane < boxes && key < p.hi && key + (int)box_rows > p.lo) {
+            const u32 pi = (u32)key / a.page;
+            const int pg = __ldg(a.tables + (i64)p.r * a.tab_r + pi);
+            if ((u32)pg < a.n_pages) { page[half] = pg; in[half] = (int)((u32)key - pi * a.page); }
+          }
+        }
+      };
       for (u32 no = 0; fine && take_part(no, p); ++no) {
-        for (int at = 0; at < p.tiles && fine; ++at) {
-          int page[2], in[2];
+        look_up(p.tile);
+        for (int at = 0; at < p.tiles && fine; ++at, ++tile_no) {
+          const int page_now[2] = {page[0], page[1]}, in_now[2] = {in[0], in[1]};
+          if (at + 1 < p.tiles) look_up(p.tile + at + 1);
+          const u32 slot = tile_no % kScaleSlots;
+          fine = wait(&sh.scales_empty[slot], ((tile_no / kScaleSlots) & 1) ^ 1);
+          if (!fine) break;
+          bool there[2];
+          u32 all = 0;                                                // a bit for each box
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
-            const int key = (p.tile + at) * kTileKeys + half * kHalfKeys + lane * (int)box_rows;
-            page[half] = (int)a.n_pages;                              // past the last page: zeros
-            in[half] = 0;
-            if (lane < boxes && key < p.hi && key + (int)box_rows > p.lo) {
-              const u32 pi = (u32)key / a.page;
-              const int pg = __ldg(a.tables + (i64)p.r * a.tab_r + pi);
-              if ((u32)pg < a.n_pages) { page[half] = pg; in[half] = (int)((u32)key - pi * a.page); }
-            }
+            there[half] = lane < boxes && page_now[half] < (int)a.n_pages;
+            all |= __ballot_sync(0xffffffffu, there[half]) << (half * boxes);
+          }
+          if (lane == 0) {
+            sh.scales_boxes[slot] = all;
+            bar_expect(&sh.scales_there[slot], (u32)__popc(all) * 2 * box_rows * 4);
+          }
+          __syncwarp();
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            if (!there[half]) continue;
+            const int to = half * kHalfKeys + lane * (int)box_rows;
+            const i64 page = page_now[half], row = in_now[half];
+            copy_scales(&sh.k_scale[slot][to], a.ks + (i64)p.h * a.ks_h + page * a.ks_p + row, box_rows * 4, &sh.scales_there[slot]);
+            copy_scales(&sh.v_factor[slot][to], a.vs + (i64)p.h * a.vs_h + page * a.vs_p + row, box_rows * 4, &sh.scales_there[slot]);
           }
 #pragma unroll
           for (int i = 0; i < 4; ++i) {                               // keys, then values
@@ -453,7 +551,8 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
             if (!fine) break;
             if (lane == 0) bar_expect(&sh.codes_full[stage], (u32)S::half_bytes);
             __syncwarp();
-            if (lane < boxes) copy_box(sh.codes[stage] + lane * (int)box_rows * D, i < 2 ? &keys : &values, 0, in[half], p.h, page[half], &sh.codes_full[stage]);
+            if (lane < boxes)
+              copy_box(sh.codes[stage] + lane * (int)box_rows * D, i < 2 ? &keys : &values, 0, in_now[half], p.h, page_now[half], &sh.codes_full[stage]);
             if (++stage == S::halves) { stage = 0; phase ^= 1; }
           }
         }
@@ -461,43 +560,33 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
       }
       // No copy is left in flight, even where the warps that wait for it have given up: each stage's last one.
       for (int i = 0; i < S::halves; ++i) drain(&sh.codes_full[i], i < stage ? phase ^ 1 : phase);
+      for (u32 i = 0; i < kScaleSlots; ++i) drain(&sh.scales_there[i], i < tile_no % kScaleSlots ? (tile_no / kScaleSlots) & 1 : ((tile_no / kScaleSlots) & 1) ^ 1);
     } else if (warp == 10) {
       // ---------------------------------------------------------------- the scales
       // A lane has keys lane, lane + 32 ... of a tile.  Of the finite scales of a tile's values the largest one's power of two becomes the
-      // tile's: factors are then below 2^7 (e4m3, whose codes are at most 448) or 2^8 (whole numbers, at most 128).
+      // tile's: factors are then below 2^7 (e4m3, whose codes are at most 448) or 2^8 (whole numbers, at most 128).  Keys outside the unit's have
+      // factor 0, whatever is there.
       constexpr int kTop = F == kE4m3 ? 6 : 7, kRange = 100;
       u32 tile_no = 0;
       bool fine = true;
       PartInfo p;
       for (u32 no = 0; fine && take_part(no, p); ++no) {
-        for (int at = 0; at < p.tiles + kScalesAhead && fine; ++at) {
-          if (at < p.tiles) {
-            const u32 x = tile_no + (u32)at, slot = x % kScaleSlots;
-            fine = wait(&sh.scales_empty[slot], ((x / kScaleSlots) & 1) ^ 1);
-            if (!fine) break;
-#pragma unroll
-            for (int j = 0; j < kTileKeys / 32; ++j) {
-              const int key = (p.tile + at) * kTileKeys + j * 32 + lane;
-              i64 page = 0, in = 0;
-              u32 bytes = 0;                                          // zeros
-              if (key >= p.lo && key < p.hi) {
-                const u32 pi = (u32)key / a.page;
-                const int pg = __ldg(a.tables + (i64)p.r * a.tab_r + pi);
-                if ((u32)pg < a.n_pages) { page = pg; in = (i64)((u32)key - pi * a.page); bytes = 4; }
-              }
-              cp_async4(&sh.k_scale[slot][j * 32 + lane], a.ks + (i64)p.h * a.ks_h + page * a.ks_p + in * a.ks_t, bytes);
-              cp_async4(&sh.v_factor[slot][j * 32 + lane], a.vs + (i64)p.h * a.vs_h + page * a.vs_p + in * a.vs_t, bytes);
-            }
-          }
-          cp_async_commit();
-          if (at < kScalesAhead) continue;
-          cp_async_wait<kScalesAhead>();
-          const u32 slot = (tile_no + (u32)(at - kScalesAhead)) % kScaleSlots;
+        for (int at = 0; at < p.tiles && fine; ++at, ++tile_no) {
+          const u32 slot = tile_no % kScaleSlots;
+          fine = wait(&sh.scales_there[slot], (tile_no / kScaleSlots) & 1);
+          if (!fine) break;
+          const u32 all = sh.scales_boxes[slot];
           float v[kTileKeys / 32];
           u32 most = 0;
 #pragma unroll
           for (int j = 0; j < kTileKeys / 32; ++j) {
+            const int key = (p.tile + at) * kTileKeys + j * 32 + lane;
             v[j] = __uint_as_float(sh.v_factor[slot][j * 32 + lane]);
+            if (!(all >> ((u32)(j * 32 + lane) / box_rows) & 1)) {    // outside the cache: zeros
+              v[j] = 0.0f;
+              sh.k_scale[slot][j * 32 + lane] = 0.0f;
+            }
+            if (key < p.lo || key >= p.hi) v[j] = 0.0f;
             if (!isfinite(v[j])) {
               sh.k_scale[slot][j * 32 + lane] = __int_as_float(0x7fffffff);
               v[j] = 0.0f;
@@ -510,80 +599,12 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
 #pragma unroll
           for (int j = 0; j < kTileKeys / 32; ++j) {
             const float f = fminf(fmaxf(v[j] * down, -power_of_two(kTop + 1)), power_of_two(kTop + 1));   // scales past 2^100 too are finite here
-            const __half hi = __float2half_rn(f), lo = __float2half_rn(f - __half2float(hi));
-            sh.v_factor[slot][j * 32 + lane] = (u32)__half_as_ushort(hi) | ((u32)__half_as_ushort(lo) << 16);
+            sh.v_factor[slot][j * 32 + lane] = pack2<__half>(f, f);
           }
           if (lane == 0) sh.shift[slot] = e;
+          fence_async();                                              // the next copy to this slot comes after these accesses
           __syncwarp();
           if (lane == 0) bar_arrive(&sh.scales_full[slot]);
-        }
-        tile_no += (u32)p.tiles;
-        part_done(no);
-      }
-      cp_async_wait<0>();
-    } else if (warp >= 12) {
-      // ---------------------------------------------------------------- codes to float16
-      constexpr int P = D / 16, kEach = kHalfKeys * P / 128;          // pieces of 16 codes: of a row, of a thread and half
-      // Which piece: four of a row and 64-byte chunk to four neighbouring lanes.  Eight lanes then write even places of one row and odd ones of
-      // the next, or the other way round, which lie in different banks.
-      const int me = tid - 12 * 32;
-      auto row_at = [&](int i) { return P == 6 ? (i * 128 + me) / 6 : (i / (P / 4)) * 32 + (me >> 2); };
-      auto piece_at = [&](int i) { return P == 6 ? (i * 128 + me) % 6 : (i % (P / 4)) * 4 + (me & 3); };
-      int stage = 0, from = 0;
-      u32 phase = 1, from_phase = 0, tile_no = 0;
-      bool fine = true;
-      PartInfo p;
-      for (u32 no = 0; fine && take_part(no, p); ++no) {
-        for (int at = 0; at < p.tiles && fine; ++at, ++tile_no) {
-          const u32 slot = tile_no % kScaleSlots;
-          const int key0 = (p.tile + at) * kTileKeys;
-          const bool every = key0 >= p.every0 && key0 + kTileKeys <= p.every1;      // all rows see all keys of the tile
-#pragma unroll
-          for (int kv = 0; kv < 2; ++kv) {
-            fine = fine && wait(&sh.kv_empty[stage], phase);
-            if (kv) fine = fine && wait(&sh.scales_full[slot], (tile_no / kScaleSlots) & 1);
-            if (!fine) break;
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              fine = fine && wait(&sh.codes_full[from], from_phase);
-              if (!fine) break;
-              uint4 w[kEach];
-#pragma unroll
-              for (int i = 0; i < kEach; ++i) w[i] = *(const uint4 *)(sh.codes[from] + row_at(i) * D + piece_at(i) * 16);
-              __syncwarp();
-              if (lane == 0) bar_arrive(&sh.codes_empty[from]);
-              if (++from == S::halves) { from = 0; from_phase ^= 1; }
-#pragma unroll
-              for (int i = 0; i < kEach; ++i) {
-                const int row = row_at(i) + half * kHalfKeys, piece = piece_at(i) * 2;
-                u32 h[8];
-                decode_along<F>(w[i].x, h[0], h[1]);
-                decode_along<F>(w[i].y, h[2], h[3]);
-                decode_along<F>(w[i].z, h[4], h[5]);
-                decode_along<F>(w[i].w, h[6], h[7]);
-                if (kv) {
-                  const u32 f = sh.v_factor[slot][row], hi = __byte_perm(f, 0, 0x1010), lo = __byte_perm(f, 0, 0x3232);
-                  if (F == kE4m3 && !every) {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) h[k] = finite_codes<F>(h[k]);
-                  }
-#pragma unroll
-                  for (int k = 0; k < 8; ++k) h[k] = fma_f16x2(h[k], hi, mul_f16x2(h[k], lo));
-                }
-                unsigned char *const to = sh.kv[stage] + (piece >> 3) * (kTileKeys * 128) + row * 128;
-                *(uint4 *)(to + (((piece & 7) ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
-                *(uint4 *)(to + (((piece + 1) & 7 ^ (row & 7)) << 4)) = make_uint4(h[4], h[5], h[6], h[7]);
-              }
-            }
-            if (!fine) break;
-            fence_async();
-            __syncwarp();
-            if (lane == 0) {
-              bar_arrive(&sh.kv_full[stage]);
-              if (kv) bar_arrive(&sh.scales_empty[slot]);
-            }
-            if (++stage == S::stages) { stage = 0; phase ^= 1; }
-          }
         }
         part_done(no);
       }
@@ -639,8 +660,16 @@ bool codes_map(CUtensorMap *map, const CodedAttn &a, const void *base, i64 st, i
                    CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// What copy_scales wants of a tensor of scales.
+bool scales_in_line(const float *base, i64 st, i64 sh, i64 sp) { return st == 1 && sh % 4 == 0 && sp % 4 == 0 && ((uintptr_t)base & 15) == 0; }
+
+struct CodedMaps {
+  CUtensorMap k, v;
+  u32 box_rows;
+};
+
 template <typename T, Format F, int D, Scores SCORES>
-cudaError_t launch_coded_chunk(const CodedAttn &a, const CUtensorMap &k, const CUtensorMap &v, u32 box_rows, u32 sms, cudaStream_t s) {
+cudaError_t launch_coded_chunk(const CodedAttn &a, const CodedMaps &m, u32 sms, cudaStream_t s) {
   static bool ready[64] = {};
   constexpr size_t bytes = sizeof(CodedChunkShared<D>) + 1024;
   static_assert(bytes <= 227 * 1024, "shared memory of one block");
@@ -655,35 +684,35 @@ cudaError_t launch_coded_chunk(const CodedAttn &a, const CUtensorMap &k, const C
     cudaFuncAttributes f;
     e = cudaFuncGetAttributes(&f, coded_chunk_kernel<T, F, D, SCORES>);
     if (e != cudaSuccess) return e;
-    if (f.numRegs * kCodedThreads < kCodedSoftmaxRegs * 256 + kCodedOtherRegs * 256) return cudaErrorInvalidKernelImage;
+    if (f.numRegs * kCodedThreads < kCodedSoftmaxRegs * 256 + (kCodedOtherRegs + kDecodeRegs) * 128) return cudaErrorInvalidKernelImage;
     ready[dev] = true;
   }
-  return launch_kernel<Attn>(coded_chunk_kernel<T, F, D, SCORES>, sms, kCodedThreads, bytes, s, a, k, v, box_rows);
+  return launch_kernel<Attn>(coded_chunk_kernel<T, F, D, SCORES>, sms, kCodedThreads, bytes, s, a, m.k, m.v, m.box_rows);
 }
 
 template <typename T, Format F, int D>
-cudaError_t pick_coded_scores(const CodedAttn &a, const CUtensorMap &k, const CUtensorMap &v, u32 box_rows, u32 sms, cudaStream_t s) {
-  if (a.softcap > 64.0f) return launch_coded_chunk<T, F, D, kLargeCap>(a, k, v, box_rows, sms, s);
-  return a.softcap > 0.0f || a.slopes ? launch_coded_chunk<T, F, D, kSmallCap>(a, k, v, box_rows, sms, s)
-                                      : launch_coded_chunk<T, F, D, kPlain>(a, k, v, box_rows, sms, s);
+cudaError_t pick_coded_scores(const CodedAttn &a, const CodedMaps &m, u32 sms, cudaStream_t s) {
+  if (a.softcap > 64.0f) return launch_coded_chunk<T, F, D, kLargeCap>(a, m, sms, s);
+  return a.softcap > 0.0f || a.slopes ? launch_coded_chunk<T, F, D, kSmallCap>(a, m, sms, s)
+                                      : launch_coded_chunk<T, F, D, kPlain>(a, m, sms, s);
 }
 
 template <typename T, Format F>
-cudaError_t pick_coded_chunk_dim(const CodedAttn &a, const CUtensorMap &k, const CUtensorMap &v, u32 box_rows, int dim, u32 sms, cudaStream_t s) {
-  if (dim == 64) return pick_coded_scores<T, F, 64>(a, k, v, box_rows, sms, s);
-  if (dim == 96) return pick_coded_scores<T, F, 96>(a, k, v, box_rows, sms, s);
-  return pick_coded_scores<T, F, 128>(a, k, v, box_rows, sms, s);
+cudaError_t pick_coded_chunk_dim(const CodedAttn &a, const CodedMaps &m, int dim, u32 sms, cudaStream_t s) {
+  if (dim == 64) return pick_coded_scores<T, F, 64>(a, m, sms, s);
+  if (dim == 96) return pick_coded_scores<T, F, 96>(a, m, sms, s);
+  return pick_coded_scores<T, F, 128>(a, m, sms, s);
 }
 
-// False where no tensor map of the pages can be made: nothing ran.
+// False where no tensor map of the pages can be made, or where scales do not follow each other along a page: nothing ran.
 template <Format F>
 bool launch_coded_chunk_of(const CodedAttn &a, int dtype, int dim, u32 sms, cudaStream_t s, cudaError_t *e) {
-  if (!encoder() || a.n_pages == 0) return false;
-  u32 box_rows = a.page & (0u - a.page);               // the largest power of two in the page size, so that a box stays in its page
-  if (box_rows > (u32)kHalfKeys) box_rows = kHalfKeys;
-  CUtensorMap k, v;
-  if (!codes_map(&k, a, a.kp, a.k_t, a.k_h, a.k_p, dim, box_rows) || !codes_map(&v, a, a.vp, a.v_t, a.v_h, a.v_p, dim, box_rows)) return false;
-  *e = dtype == 0 ? pick_coded_chunk_dim<__nv_bfloat16, F>(a, k, v, box_rows, dim, sms, s) : pick_coded_chunk_dim<__half, F>(a, k, v, box_rows, dim, sms, s);
+  if (!encoder() || a.n_pages == 0 || !scales_in_line(a.ks, a.ks_t, a.ks_h, a.ks_p) || !scales_in_line(a.vs, a.vs_t, a.vs_h, a.vs_p)) return false;
+  CodedMaps m;
+  m.box_rows = a.page & (0u - a.page);                 // the largest power of two in the page size, so that a box stays in its page
+  if (m.box_rows > (u32)kHalfKeys) m.box_rows = kHalfKeys;
+  if (!codes_map(&m.k, a, a.kp, a.k_t, a.k_h, a.k_p, dim, m.box_rows) || !codes_map(&m.v, a, a.vp, a.v_t, a.v_h, a.v_p, dim, m.box_rows)) return false;
+  *e = dtype == 0 ? pick_coded_chunk_dim<__nv_bfloat16, F>(a, m, dim, sms, s) : pick_coded_chunk_dim<__half, F>(a, m, dim, sms, s);
   return true;
 }
 
