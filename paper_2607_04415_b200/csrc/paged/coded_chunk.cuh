@@ -5,10 +5,11 @@
 //   0-3, 4-7  the softmax of row tile 0 and 1: a thread a row.  At a part's start each thread brings its own row of queries, as float16 times a
 //             power of two.
 //   8         issues both products (one thread).
-//   9         copies codes of keys and values, 64 keys at a time, into a ring of their own, and their scales (tensor copies).
+//   9         copies codes of keys and values, and their scales, into the stages that they are taken apart in.
 //   10        makes a tile's factors of the scales of its values.
 //   11        walks the block's share of the work and tells the others its parts.
-//   12-15     take codes apart into the 16-bit tiles that the products read.
+//   12-15     take codes apart, in place, into the 16-bit tiles that the products read.  (With a ring of their own for codes three pieces of 64 keys
+//             were all that shared memory held beside them, too few on their way: 972 us where this takes 698 for 2048 tokens over 18432 keys.)
 // Keys become their codes, exactly; a score is multiplied by its key's scale in 32 bits.  Values are multiplied by their scales as they
 // become float16, one rounding to 11 bits; so that neither side of that leaves float16's range, a tile has a power of two of its own, taken out of
 // its values and put into its weights: 2^(x + shift - m) with m the running maximum of x + shift, whose sum is taken back by 2^-shift once a tile.
@@ -27,31 +28,26 @@ namespace paged {
 namespace {
 
 constexpr int kCodedThreads = 512;
-constexpr int kCodedSoftmaxRegs = 192, kCodedOtherRegs = 80, kDecodeRegs = 48;   // a thread, of 128 * 4 = 192 * 2 + 80 + 48 at launch
-constexpr int kHalfKeys = 64;                                    // of a copy
+constexpr int kCodedSoftmaxRegs = 200, kCodedOtherRegs = 64, kDecodeRegs = 48;   // a thread, of 128 * 4 = 200 * 2 + 64 + 48 at launch
 constexpr int kScaleSlots = 4;                                   // tiles whose scales are there
 
 template <int D>
 struct CodedShape {
-  static constexpr int chunks = (D + 63) / 64;                   // of 64 elements, 128 bytes
-  static constexpr int tile_bytes = chunks * kTileKeys * 128;
+  static constexpr int chunks = Shape<D>::chunks, tile_bytes = Shape<D>::tile_bytes;
   static constexpr int stages = chunks == 1 ? 8 : 4;
-  static constexpr int half_bytes = kHalfKeys * D;
-  static constexpr int halves = D == 128 ? 3 : D == 96 ? 4 : 6;  // 24 KB, which is what is left
 };
 
 template <int D>
 struct CodedChunkShared {
   unsigned char q[2][CodedShape<D>::tile_bytes];
   unsigned char kv[CodedShape<D>::stages][CodedShape<D>::tile_bytes];
-  unsigned char codes[CodedShape<D>::halves][CodedShape<D>::half_bytes];
   __align__(128) float k_scale[kScaleSlots][kTileKeys];
   u32 v_factor[kScaleSlots][kTileKeys];          // float16, twice; until it is there, the scale
   u32 scales_boxes[kScaleSlots];                 // which boxes of them were copied
   int shift[kScaleSlots];
   float q_to_dot[kTileRows];                     // of the rows of a unit of one row tile
   PartInfo part[kParts];
-  u64 kv_full[CodedShape<D>::stages], kv_empty[CodedShape<D>::stages], codes_full[CodedShape<D>::halves], codes_empty[CodedShape<D>::halves];
+  u64 codes_full[CodedShape<D>::stages], kv_full[CodedShape<D>::stages], kv_empty[CodedShape<D>::stages];
   u64 scales_there[kScaleSlots], scales_full[kScaleSlots], scales_empty[kScaleSlots];
   u64 part_full[kParts], part_empty[kParts];
   u64 q_full[2], q_empty[2], s_full[2], p_full[2][2], o_full[2], meet, drained;
@@ -93,8 +89,7 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
   typedef CodedShape<D> S;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (warp == 8) {
-    if (lane < S::stages) { bar_init(&sh.kv_full[lane], 4); bar_init(&sh.kv_empty[lane], 1); }
-    if (lane < S::halves) { bar_init(&sh.codes_full[lane], 1); bar_init(&sh.codes_empty[lane], 4); }
+    if (lane < S::stages) { bar_init(&sh.codes_full[lane], 1); bar_init(&sh.kv_full[lane], 4); bar_init(&sh.kv_empty[lane], 1); }
     if (lane < kScaleSlots) { bar_init(&sh.scales_there[lane], 1); bar_init(&sh.scales_full[lane], 1); bar_init(&sh.scales_empty[lane], 12); }
     if (lane < kParts) { bar_init(&sh.part_full[lane], 1); bar_init(&sh.part_empty[lane], 15); }
     if (lane < 2) {
@@ -312,14 +307,14 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
   } else if (warp >= 12) {
     fewer_registers<kDecodeRegs>();
     // ---------------------------------------------------------------- codes to float16
-    constexpr int P = D / 16, kEach = kHalfKeys * P / 128;          // pieces of 16 codes: of a row, of a thread and half
-    // Which piece: four of a row and 64-byte chunk to four neighbouring lanes.  Eight lanes then write even places of one row and odd ones of
-    // the next, or the other way round, which lie in different banks.
-    const int me = tid - 12 * 32;
-    auto row_at = [&](int i) { return P == 6 ? (i * 128 + me) / 6 : (i / (P / 4)) * 32 + (me >> 2); };
-    auto piece_at = [&](int i) { return P == 6 ? (i * 128 + me) % 6 : (i % (P / 4)) * 4 + (me & 3); };
-    int stage = 0, from = 0;
-    u32 phase = 1, from_phase = 0, tile_no = 0;
+    // A row's codes lie 128 bytes apart where its first 64 numbers will stand: a warp that has read some rows may write them.  Pieces of 16 codes go
+    // to lanes so that eight lanes write even places of one row and odd ones of the next, or the other way round, which lie in different banks:
+    // four neighbouring lanes have four pieces of a row, the rest of the row comes in another step (of 96 numbers: two pieces of twice as many rows).
+    constexpr int kGroup = D == 64 ? 32 : 16, kEach = D == 96 ? 3 : 4;      // rows that are read before they are written; a lane's pieces of them
+    auto row_at = [&](int i) { return D == 128 ? (i >> 1) * 8 + (lane >> 2) : D == 96 && i == 2 ? lane >> 1 : i * 8 + (lane >> 2); };
+    auto piece_at = [&](int i) { return D == 128 ? (i & 1) * 4 + (lane & 3) : D == 96 && i == 2 ? 4 + (lane & 1) : lane & 3; };
+    int stage = 0;
+    u32 phase = 0, tile_no = 0;
     bool fine = true;
     PartInfo p;
     for (u32 no = 0; fine && take_part(no, p); ++no) {
@@ -329,42 +324,41 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
         const bool every = key0 >= p.every0 && key0 + kTileKeys <= p.every1;      // all rows see all keys of the tile
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
-          fine = fine && wait(&sh.kv_empty[stage], phase);
           if (kv) fine = fine && wait(&sh.scales_full[slot], (tile_no / kScaleSlots) & 1);
+          fine = fine && wait(&sh.codes_full[stage], phase);
           if (!fine) break;
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            fine = fine && wait(&sh.codes_full[from], from_phase);
-            if (!fine) break;
+          unsigned char *const tile = sh.kv[stage];
+#pragma unroll 1
+          for (int row0 = (warp - 12) * 32; row0 < (warp - 11) * 32; row0 += kGroup) {
             uint4 w[kEach];
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) w[i] = *(const uint4 *)(sh.codes[from] + row_at(i) * D + piece_at(i) * 16);
-            __syncwarp();
-            if (lane == 0) bar_arrive(&sh.codes_empty[from]);
-            if (++from == S::halves) { from = 0; from_phase ^= 1; }
+            u32 f[kEach];
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
-              const int row = row_at(i) + half * kHalfKeys, piece = piece_at(i) * 2;
+              w[i] = *(const uint4 *)(tile + (row0 + row_at(i)) * 128 + piece_at(i) * 16);
+              if (kv) f[i] = sh.v_factor[slot][row0 + row_at(i)];
+            }
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+              const int row = row0 + row_at(i), piece = piece_at(i) * 2;
               u32 h[8];
               decode_along<F>(w[i].x, h[0], h[1]);
               decode_along<F>(w[i].y, h[2], h[3]);
               decode_along<F>(w[i].z, h[4], h[5]);
               decode_along<F>(w[i].w, h[6], h[7]);
               if (kv) {
-                const u32 f = sh.v_factor[slot][row];
                 if (F == kE4m3 && !every) {
 #pragma unroll
                   for (int k = 0; k < 8; ++k) h[k] = finite_codes<F>(h[k]);
                 }
 #pragma unroll
-                for (int k = 0; k < 8; ++k) h[k] = mul_f16x2(h[k], f);
+                for (int k = 0; k < 8; ++k) h[k] = mul_f16x2(h[k], f[i]);
               }
-              unsigned char *const to = sh.kv[stage] + (piece >> 3) * (kTileKeys * 128) + row * 128;
+              unsigned char *const to = tile + (piece >> 3) * (kTileKeys * 128) + row * 128;
               *(uint4 *)(to + (((piece & 7) ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
               *(uint4 *)(to + (((piece + 1) & 7 ^ (row & 7)) << 4)) = make_uint4(h[4], h[5], h[6], h[7]);
             }
           }
-          if (!fine) break;
           fence_async();
           __syncwarp();
           if (lane == 0) {
@@ -435,7 +429,6 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
             u32 v_ph, k_ph;
             const u32 t = at & 1, v_stage = ahead(1, v_ph), k_stage = ahead(4, k_ph);
             const bool more = at + 2 < n_tiles;
-            // with four stages the keys of the next but one tile come to the stage of this tile's, whose scores are done
             fine = wait(&sh.kv_full[v_stage], v_ph) && (!more || wait(&sh.kv_full[k_stage], k_ph));
             for (u32 half = 0; half < 2 && fine; ++half) {
               fine = wait(&sh.p_full[t][half], (p_phase >> t) & 1);
@@ -496,70 +489,57 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
       drain(&sh.drained, 0);
     } else if (warp == 9) {
       // ---------------------------------------------------------------- the copies of codes and scales
-      const int boxes = kHalfKeys / (int)box_rows;                    // at most 8 for 64 keys: a lane each
+      const int boxes = kTileKeys / (int)box_rows;                    // at most 16: a lane each
       int stage = 0;
       u32 phase = 1, tile_no = 0;                                     // the first round finds the stages free
       bool fine = true;
-      PartInfo p;
+      PartInfo p{};
       // Page and place of this lane's box in each half of a tile, looked up a tile ahead: the entry of a table is far away.
-      int page[2], in[2];
+      int page, in;
       auto look_up = [&](int tile) {
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const int key = tile * kTileKeys + half * kHalfKeys + lane * (int)box_rows;
-          page[half] = (int)a.n_pages;                                // past the last page: zeros
-          in[half] = 0;
-          if (lane < boxes && key < p.hi && key + (int)box_rows > p.lo) {
-            const u32 pi = (u32)key / a.page;
-            const int pg = __ldg(a.tables + (i64)p.r * a.tab_r + pi);
-            if ((u32)pg < a.n_pages) { page[half] = pg; in[half] = (int)((u32)key - pi * a.page); }
-          }
+        const int key = tile * kTileKeys + lane * (int)box_rows;
+        page = (int)a.n_pages;                                        // past the last page: zeros
+        in = 0;
+        if (lane < boxes && key < p.hi && key + (int)box_rows > p.lo) {
+          const u32 pi = (u32)key / a.page;
+          const int pg = __ldg(a.tables + (i64)p.r * a.tab_r + pi);
+          if ((u32)pg < a.n_pages) { page = pg; in = (int)((u32)key - pi * a.page); }
         }
       };
       for (u32 no = 0; fine && take_part(no, p); ++no) {
         look_up(p.tile);
         for (int at = 0; at < p.tiles && fine; ++at, ++tile_no) {
-          const int page_now[2] = {page[0], page[1]}, in_now[2] = {in[0], in[1]};
+          const int page_now = page, in_now = in;
           if (at + 1 < p.tiles) look_up(p.tile + at + 1);
           const u32 slot = tile_no % kScaleSlots;
           fine = wait(&sh.scales_empty[slot], ((tile_no / kScaleSlots) & 1) ^ 1);
           if (!fine) break;
-          bool there[2];
-          u32 all = 0;                                                // a bit for each box
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            there[half] = lane < boxes && page_now[half] < (int)a.n_pages;
-            all |= __ballot_sync(0xffffffffu, there[half]) << (half * boxes);
-          }
+          const bool there = lane < boxes && page_now < (int)a.n_pages;
+          const u32 all = __ballot_sync(0xffffffffu, there);          // a bit for each box
           if (lane == 0) {
             sh.scales_boxes[slot] = all;
             bar_expect(&sh.scales_there[slot], (u32)__popc(all) * 2 * box_rows * 4);
           }
           __syncwarp();
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            if (!there[half]) continue;
-            const int to = half * kHalfKeys + lane * (int)box_rows;
-            const i64 page = page_now[half], row = in_now[half];
-            copy_scales(&sh.k_scale[slot][to], a.ks + (i64)p.h * a.ks_h + page * a.ks_p + row, box_rows * 4, &sh.scales_there[slot]);
-            copy_scales(&sh.v_factor[slot][to], a.vs + (i64)p.h * a.vs_h + page * a.vs_p + row, box_rows * 4, &sh.scales_there[slot]);
+          if (there) {
+            const int to = lane * (int)box_rows;
+            copy_scales(&sh.k_scale[slot][to], a.ks + (i64)p.h * a.ks_h + (i64)page_now * a.ks_p + in_now, box_rows * 4, &sh.scales_there[slot]);
+            copy_scales(&sh.v_factor[slot][to], a.vs + (i64)p.h * a.vs_h + (i64)page_now * a.vs_p + in_now, box_rows * 4, &sh.scales_there[slot]);
           }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {                               // keys, then values
-            const int half = i & 1;
-            fine = fine && wait(&sh.codes_empty[stage], phase);
+          for (int kv = 0; kv < 2; ++kv) {
+            fine = fine && wait(&sh.kv_empty[stage], phase);
             if (!fine) break;
-            if (lane == 0) bar_expect(&sh.codes_full[stage], (u32)S::half_bytes);
+            if (lane == 0) bar_expect(&sh.codes_full[stage], (u32)(kTileKeys * 128));
             __syncwarp();
-            if (lane < boxes)
-              copy_box(sh.codes[stage] + lane * (int)box_rows * D, i < 2 ? &keys : &values, 0, in_now[half], p.h, page_now[half], &sh.codes_full[stage]);
-            if (++stage == S::halves) { stage = 0; phase ^= 1; }
+            if (lane < boxes) copy_box(sh.kv[stage] + lane * (int)box_rows * 128, kv ? &values : &keys, 0, in_now, p.h, page_now, &sh.codes_full[stage]);
+            if (++stage == S::stages) { stage = 0; phase ^= 1; }
           }
         }
         part_done(no);
       }
       // No copy is left in flight, even where the warps that wait for it have given up: each stage's last one.
-      for (int i = 0; i < S::halves; ++i) drain(&sh.codes_full[i], i < stage ? phase ^ 1 : phase);
+      for (int i = 0; i < S::stages; ++i) drain(&sh.codes_full[i], i < stage ? phase ^ 1 : phase);
       for (u32 i = 0; i < kScaleSlots; ++i) drain(&sh.scales_there[i], i < tile_no % kScaleSlots ? (tile_no / kScaleSlots) & 1 : ((tile_no / kScaleSlots) & 1) ^ 1);
     } else if (warp == 10) {
       // ---------------------------------------------------------------- the scales
@@ -652,10 +632,11 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
   if (tid == 0 && sh.failed) *error_word(a) = 1;
 }
 
+// Rows come 128 bytes apart, the last of them zeros where a head is shorter.
 bool codes_map(CUtensorMap *map, const CodedAttn &a, const void *base, i64 st, i64 sh, i64 sp, int dim, u32 box_rows) {
   const cuuint64_t dims[4] = {(cuuint64_t)dim, a.page, a.hkv, a.n_pages};
   const cuuint64_t strides[3] = {(cuuint64_t)st, (cuuint64_t)sh, (cuuint64_t)sp};
-  const cuuint32_t box[4] = {(cuuint32_t)dim, box_rows, 1, 1}, step[4] = {1, 1, 1, 1};
+  const cuuint32_t box[4] = {128, box_rows, 1, 1}, step[4] = {1, 1, 1, 1};
   return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void *>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
                    CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -710,7 +691,7 @@ bool launch_coded_chunk_of(const CodedAttn &a, int dtype, int dim, u32 sms, cuda
   if (!encoder() || a.n_pages == 0 || !scales_in_line(a.ks, a.ks_t, a.ks_h, a.ks_p) || !scales_in_line(a.vs, a.vs_t, a.vs_h, a.vs_p)) return false;
   CodedMaps m;
   m.box_rows = a.page & (0u - a.page);                 // the largest power of two in the page size, so that a box stays in its page
-  if (m.box_rows > (u32)kHalfKeys) m.box_rows = kHalfKeys;
+  if (m.box_rows > (u32)kTileKeys) m.box_rows = kTileKeys;
   if (!codes_map(&m.k, a, a.kp, a.k_t, a.k_h, a.k_p, dim, m.box_rows) || !codes_map(&m.v, a, a.vp, a.v_t, a.v_h, a.v_p, dim, m.box_rows)) return false;
   *e = dtype == 0 ? pick_coded_chunk_dim<__nv_bfloat16, F>(a, m, dim, sms, s) : pick_coded_chunk_dim<__half, F>(a, m, dim, sms, s);
   return true;
