@@ -9,7 +9,7 @@
 //   10        makes a tile's factors of the scales of its values.
 //   11        walks the block's share of the work and tells the others its parts.
 //   12-15     take codes apart, in place, into the 16-bit tiles that the products read.  (With a ring of their own for codes three pieces of 64 keys
-//             were all that shared memory held beside them, too few on their way: 972 us where this takes 698 for 2048 tokens over 18432 keys.)
+//             were all that shared memory held beside them, too few on their way: 972 us where this takes 658 for 2048 tokens over 18432 keys.)
 // Keys become their codes, exactly; a score is multiplied by its key's scale in 32 bits.  Values are multiplied by their scales as they
 // become float16, one rounding to 11 bits; so that neither side of that leaves float16's range, a tile has a power of two of its own, taken out of
 // its values and put into its weights: 2^(x + shift - m) with m the running maximum of x + shift, whose sum is taken back by 2^-shift once a tile.
@@ -22,13 +22,15 @@
 #include "chunk.cuh"
 #include "coded.cuh"
 
+#include <type_traits>
+
 namespace gorio {
 namespace paged {
 
 namespace {
 
 constexpr int kCodedThreads = 512;
-constexpr int kCodedSoftmaxRegs = 200, kCodedOtherRegs = 64, kDecodeRegs = 48;   // a thread, of 128 * 4 = 200 * 2 + 64 + 48 at launch
+constexpr int kCodedSoftmaxRegs = 184, kCodedOtherRegs = 72, kDecodeRegs = 72;   // a thread, of 128 * 4 = 184 * 2 + 72 + 72 at launch
 constexpr int kScaleSlots = 4;                                   // tiles whose scales are there
 
 template <int D>
@@ -221,16 +223,16 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
             m = to;
             l *= f;
             if (at > first) {                                // the scores' arrival says that the product before is done
-#pragma unroll 2
-              for (int i = 0; i < D / 32; ++i) {
-                float o[32];
-                tmem_ld32(o, outputs + 32 * i);
+              // 16 columns at a time: with 32, beside the 128 scores, values that every tile needs were spilled
+#pragma unroll 1
+              for (int i = 0; i < D / 16; ++i) {
+                float o[16];
+                tmem_ld16(o, outputs + 16 * i);
                 tmem_wait_ld();
-                keep(o);
-                u32 w[32];
+                keep16(o);
 #pragma unroll
-                for (int k = 0; k < 32; ++k) w[k] = __float_as_uint(o[k] * f);
-                tmem_st32(outputs + 32 * i, w);
+                for (int k = 0; k < 16; ++k) o[k] *= f;
+                tmem_st16(outputs + 16 * i, o);
               }
             }
           }
@@ -313,6 +315,38 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
     constexpr int kGroup = D == 64 ? 32 : 16, kEach = D == 96 ? 3 : 4;      // rows that are read before they are written; a lane's pieces of them
     auto row_at = [&](int i) { return D == 128 ? (i >> 1) * 8 + (lane >> 2) : D == 96 && i == 2 ? lane >> 1 : i * 8 + (lane >> 2); };
     auto piece_at = [&](int i) { return D == 128 ? (i & 1) * 4 + (lane & 3) : D == 96 && i == 2 ? 4 + (lane & 1) : lane & 3; };
+    // This warp's 32 rows of a tile; `factors` are its values' or NULL.
+    auto decode_rows = [&](unsigned char *tile, const u32 *factors, auto clean) {
+#pragma unroll 1
+      for (int row0 = (warp - 12) * 32; row0 < (warp - 11) * 32; row0 += kGroup) {
+        uint4 w[kEach];
+        u32 f[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+          w[i] = *(const uint4 *)(tile + (row0 + row_at(i)) * 128 + piece_at(i) * 16);
+          if (factors) f[i] = factors[row0 + row_at(i)];
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+          const int row = row0 + row_at(i), piece = piece_at(i) * 2;
+          u32 h[8];
+          decode_along<F>(w[i].x, h[0], h[1]);
+          decode_along<F>(w[i].y, h[2], h[3]);
+          decode_along<F>(w[i].z, h[4], h[5]);
+          decode_along<F>(w[i].w, h[6], h[7]);
+          if (factors) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) h[k] = mul_f16x2(decltype(clean)::value ? finite_codes<F>(h[k]) : h[k], f[i]);
+          }
+          unsigned char *const at = tile + (piece >> 3) * (kTileKeys * 128) + row * 128;
+          *(uint4 *)(at + (((piece & 7) ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+          *(uint4 *)(at + (((piece + 1) & 7 ^ (row & 7)) << 4)) = make_uint4(h[4], h[5], h[6], h[7]);
+        }
+      }
+      fence_async();
+      __syncwarp();
+    };
     int stage = 0;
     u32 phase = 0, tile_no = 0;
     bool fine = true;
@@ -327,40 +361,9 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
           if (kv) fine = fine && wait(&sh.scales_full[slot], (tile_no / kScaleSlots) & 1);
           fine = fine && wait(&sh.codes_full[stage], phase);
           if (!fine) break;
-          unsigned char *const tile = sh.kv[stage];
-#pragma unroll 1
-          for (int row0 = (warp - 12) * 32; row0 < (warp - 11) * 32; row0 += kGroup) {
-            uint4 w[kEach];
-            u32 f[kEach];
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-              w[i] = *(const uint4 *)(tile + (row0 + row_at(i)) * 128 + piece_at(i) * 16);
-              if (kv) f[i] = sh.v_factor[slot][row0 + row_at(i)];
-            }
-            __syncwarp();
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-              const int row = row0 + row_at(i), piece = piece_at(i) * 2;
-              u32 h[8];
-              decode_along<F>(w[i].x, h[0], h[1]);
-              decode_along<F>(w[i].y, h[2], h[3]);
-              decode_along<F>(w[i].z, h[4], h[5]);
-              decode_along<F>(w[i].w, h[6], h[7]);
-              if (kv) {
-                if (F == kE4m3 && !every) {
-#pragma unroll
-                  for (int k = 0; k < 8; ++k) h[k] = finite_codes<F>(h[k]);
-                }
-#pragma unroll
-                for (int k = 0; k < 8; ++k) h[k] = mul_f16x2(h[k], f[i]);
-              }
-              unsigned char *const to = tile + (piece >> 3) * (kTileKeys * 128) + row * 128;
-              *(uint4 *)(to + (((piece & 7) ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
-              *(uint4 *)(to + (((piece + 1) & 7 ^ (row & 7)) << 4)) = make_uint4(h[4], h[5], h[6], h[7]);
-            }
-          }
-          fence_async();
-          __syncwarp();
+          if (!kv) decode_rows(sh.kv[stage], nullptr, std::false_type{});
+          else if (F != kE4m3 || every) decode_rows(sh.kv[stage], sh.v_factor[slot], std::false_type{});
+          else decode_rows(sh.kv[stage], sh.v_factor[slot], std::true_type{});
           if (lane == 0) {
             bar_arrive(&sh.kv_full[stage]);
             if (kv) bar_arrive(&sh.scales_empty[slot]);
