@@ -4,7 +4,7 @@
 namespace gorio {
 namespace paged {
 
-cudaError_t launch_coded_rows_int8(const CodedAttn &a, int dtype, int dim, u32 sms, cudaStream_t s) { return launch_coded_rows_of<kInt8>(a, dtype, dim, sms, s); }
+cudaError_t launch_coded_rows_int8(const CodedAttn &a, int dtype, int dim, bool few, u32 sms, cudaStream_t s) { return launch_coded_rows_of<kInt8>(a, dtype, dim, few, sms, s); }
 
 }  // namespace paged
 }  // namespace gorio

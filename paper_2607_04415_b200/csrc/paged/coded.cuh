@@ -73,8 +73,8 @@ __device__ __forceinline__ float query_factor(float largest) {
 }
 
 // launchers, one for each format
-cudaError_t launch_coded_rows_e4m3(const CodedAttn &a, int dtype, int dim, u32 sms, cudaStream_t s);
-cudaError_t launch_coded_rows_int8(const CodedAttn &a, int dtype, int dim, u32 sms, cudaStream_t s);
+cudaError_t launch_coded_rows_e4m3(const CodedAttn &a, int dtype, int dim, bool few, u32 sms, cudaStream_t s);
+cudaError_t launch_coded_rows_int8(const CodedAttn &a, int dtype, int dim, bool few, u32 sms, cudaStream_t s);
 bool launch_coded_chunk_e4m3(const CodedAttn &a, int dtype, int dim, u32 sms, cudaStream_t s, cudaError_t *e);
 bool launch_coded_chunk_int8(const CodedAttn &a, int dtype, int dim, u32 sms, cudaStream_t s, cudaError_t *e);
 

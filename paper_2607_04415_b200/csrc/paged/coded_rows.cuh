@@ -1,12 +1,15 @@
 // Attention of few rows over a quantised paged cache: the single-token form.
 //
-// The plan, the units of 16 rows and the four warps with a ring each are those of the 16-bit cache's kernel (rows.cuh).  What is
-// different comes from the 8 bits.  The same bytes in flight are twice as many keys, so a warp's tile is 32 keys.  Codes
-// become float16 in registers, exactly, in the lanes and the order in which the matrix instructions want them:
+// The plan and the four warps with a ring each are those of the 16-bit cache's kernel (rows.cuh).  What is different comes from the
+// 8 bits.  The same bytes in flight are twice as many keys, and what is computed for a key has half the time: with the 16-bit kernel's products,
+// 16 rows by 8 keys, 64 requests over up to 16384 keys took 254 us, waiting for one operation after the other.  So keys are
+// the products' first operand here, 16 by 8 rows, which up to 8 rows (heads that share a key head) halves products, scores and registers, and
+// so leaves room for more warps; more rows take two of them.  A warp's tile is 32 keys.
+// Codes become float16 in registers, exactly, in the lanes and the order in which the matrix instructions want them:
 //   keys     a 16-byte piece of a row is what one product over 16 elements takes.  A lane gets four neighbouring codes of a
 //            key, and its queries are loaded in the same order, so that nothing is moved.
-//   values   read transposed by pairs of codes, a lane gets two neighbouring columns of two neighbouring keys; taken apart they are
-//            the operand of one product for the even columns and of one for the odd ones.
+//   values   read transposed by pairs of codes, a lane gets two neighbouring columns of two neighbouring keys; taken apart the even columns are
+//            the first eight rows of a product's operand, the odd ones the other eight.
 // Products of queries (float16, a power of two a row) and codes are summed in 32 bits; the key's scale comes after.  The value's scale
 // goes to the weight before that is rounded to float16: 2^(x - base) * scale.  So that the largest such weight is 2^15 whatever the scales are,
 // a row's running maximum is that of x + log2(scale).
@@ -21,14 +24,15 @@ namespace {
 
 constexpr int kCodedKeys = 32;                   // of a warp's tile
 constexpr int kCodedTile = kWarps * kCodedKeys;
-constexpr int kCodedStages = 3;
-template <int D>
-constexpr int kCodedBlocks = D == 64 ? 4 : D == 96 ? 3 : 2;
+constexpr int kCodedStages = 2;
+// Blocks of an SM for heads of D and 8 * NT rows: what shared memory (17 KB a warp at head size 128) and registers hold.
+template <int D, int NT>
+constexpr int kCodedBlocks = D == 64 ? 4 : NT == 1 ? 3 : 2;
 constexpr float kScaleRange = 80.0f;             // a scale's power of two that the maximum counts, at most
 
 template <int D>
 struct CodedShared {
-  // per warp and stage: the codes of 32 keys, then of 32 values; the same bytes hold the warp's 16 x D output at a unit's end
+  // per warp and stage: the codes of 32 keys, then of 32 values; the same bytes hold the warp's output, up to 16 x D, at a unit's end
   u8 ring[kWarps][kCodedStages][2][kCodedKeys * D];
   float scales[kWarps][kCodedStages][2][kCodedKeys];
   float m[kWarps][kRows], l[kWarps][kRows];
@@ -52,15 +56,20 @@ __device__ __forceinline__ float scale_log2(float scale) {
   return fminf(fmaxf(e, -kScaleRange), kScaleRange);          // also of a scale that is not a number
 }
 
-// q.k of one 16 x 8 tile and 16 elements, of one 16 x 8 output tile and 16 keys
-__device__ __forceinline__ void mma_half(float (&c)[4], const u32 (&a)[4], u32 b0, u32 b1) { mma16816<__half>(c, a, b0, b1); }
+// The transpose of an 8 x 8 matrix of 16-bit numbers, two neighbouring columns of a row to a lane.
+__device__ __forceinline__ u32 transpose8(u32 v) {
+  u32 r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
 
-template <typename T, Format F, int D, bool SCORED>
-__global__ void __launch_bounds__(kThreads, kCodedBlocks<D>) coded_rows_kernel(const CodedAttn a) {
+template <typename T, Format F, int D, bool SCORED, int NT>
+__global__ void __launch_bounds__(kThreads, (kCodedBlocks<D, NT>)) coded_rows_kernel(const CodedAttn a) {
   extern __shared__ __align__(128) unsigned char raw[];
   CodedShared<D> &sh = *(CodedShared<D> *)raw;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const Plan plan = block_plan<kRows, kCodedTile, kOver, kThreads>(a, sh.plan, kSpread);
+  constexpr int kUnitRows = 8 * NT;
+  const Plan plan = block_plan<kUnitRows, kCodedTile, kOver, kThreads>(a, sh.plan, kSpread);
   if (plan.begin >= plan.end) return;
 
   constexpr int P = D / 16;                      // 16-byte pieces of a row
@@ -73,7 +82,7 @@ __global__ void __launch_bounds__(kThreads, kCodedBlocks<D>) coded_rows_kernel(c
   const bool in_line = 32 % P == 0 && a.page % 16 == 0;
   Cursor ld = plan.first;
   u32 ld_left = plan.end - plan.begin;
-  settle<kRows, kCodedTile, kOver>(a, ld, ld_left, plan.fill);
+  settle<kUnitRows, kCodedTile, kOver>(a, ld, ld_left, plan.fill);
   int key_page = -1, key_in = 0;                 // of key `lane` of the warp's tile at ld; -1: zeros
   auto look_up = [&]() {
     if (ld_left == 0) return;
@@ -126,7 +135,7 @@ __global__ void __launch_bounds__(kThreads, kCodedBlocks<D>) coded_rows_kernel(c
       cp_async4(&sh.scales[warp][stage][1][lane], a.vs + (i64)ld.h * a.vs_h + page * a.vs_p + tok * a.vs_t, bytes);
       --ld_left;
       ++ld.at;
-      settle<kRows, kCodedTile, kOver>(a, ld, ld_left, plan.fill);
+      settle<kUnitRows, kCodedTile, kOver>(a, ld, ld_left, plan.fill);
       look_up();
     }
     cp_async_commit();
@@ -140,25 +149,19 @@ __global__ void __launch_bounds__(kThreads, kCodedBlocks<D>) coded_rows_kernel(c
   int stage = 0;
   const int g = lane >> 2, t4 = lane & 3;
   u32 left = plan.end - plan.begin;
-  for (settle<kRows, kCodedTile, kOver>(a, c, left, plan.fill); left; settle<kRows, kCodedTile, kOver>(a, c, left, plan.fill)) {
+  for (settle<kUnitRows, kCodedTile, kOver>(a, c, left, plan.fill); left; settle<kUnitRows, kCodedTile, kOver>(a, c, left, plan.fill)) {
     const int from = c.at;
     const int to = (int)min((u32)c.span.tiles, (u32)from + left);
-    const i64 row0 = (i64)c.m * kRows;
-    const int rows = (int)min((i64)kRows, (i64)c.req.n * a.group - row0);
-    // this lane's two rows: g and g + 8
-    u32 qf[P][4];
-    int lo_key[2], hi_key[2];                     // visible keys of the row
-    float slope[2], to_dot[2];
-    int pos[2];
+    const i64 row0 = (i64)c.m * kUnitRows;
+    const int rows = (int)min((i64)kUnitRows, (i64)c.req.n * a.group - row0);
+    // queries: this lane's row of each eight is g
+    u32 qf[P][NT][2];
+    float inverse[NT];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int row = g + 8 * i;
+    for (int i = 0; i < NT; ++i) {
+      const int row = 8 * i + g;
       const int tok = row < rows ? (int)((row0 + row) / a.group) : 0;
       const int head = row < rows ? (int)((row0 + row) - (i64)tok * a.group) + (int)(c.h * a.group) : 0;
-      pos[i] = position_of(a, c.req, tok);
-      hi_key[i] = a.causal ? min(c.req.len, pos[i] + 1) : c.req.len;
-      lo_key[i] = a.window ? (int)max((i64)0, (i64)pos[i] - a.window + 1) : 0;
-      slope[i] = SCORED && a.slopes ? a.slopes[head] * kLog2e : 0.0f;
       const u16 *src = (const u16 *)a.q + (i64)(c.req.q0 + tok) * a.q_t + (i64)head * a.q_h + t4 * 4;
       uint2 x[P];
       float top = 0.0f;
@@ -171,20 +174,40 @@ __global__ void __launch_bounds__(kThreads, kCodedBlocks<D>) coded_rows_kernel(c
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
       const float f = query_factor(top);
-      to_dot[i] = 1.0f / f;                       // powers of two
+      inverse[i] = 1.0f / f;                      // powers of two
 #pragma unroll
       for (int k = 0; k < P; ++k) {
         const float2 lo = unpack2<T>(x[k].x), hi = unpack2<T>(x[k].y);
-        qf[k][i] = pack2<__half>(lo.x * f, lo.y * f);
-        qf[k][2 + i] = pack2<__half>(hi.x * f, hi.y * f);
+        qf[k][i][0] = pack2<__half>(lo.x * f, lo.y * f);
+        qf[k][i][1] = pack2<__half>(hi.x * f, hi.y * f);
       }
     }
-    float o[P][2][4];                             // even and odd columns of 16
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+    // scores and outputs: this lane's rows of each eight are 2 * t4 and the next
+    int lo_key[2 * NT], hi_key[2 * NT];           // visible keys of the row
+    float slope[2 * NT], to_dot[2 * NT];
+    int pos[2 * NT];
+    bool sees_all = true;
+#pragma unroll
+    for (int i = 0; i < 2 * NT; ++i) {
+      const int row = (i >> 1) * 8 + t4 * 2 + (i & 1);
+      const int tok = row < rows ? (int)((row0 + row) / a.group) : 0;
+      const int head = row < rows ? (int)((row0 + row) - (i64)tok * a.group) + (int)(c.h * a.group) : 0;
+      pos[i] = position_of(a, c.req, tok);
+      hi_key[i] = a.causal ? min(c.req.len, pos[i] + 1) : c.req.len;
+      lo_key[i] = a.window ? (int)max((i64)0, (i64)pos[i] - a.window + 1) : 0;
+      slope[i] = SCORED && a.slopes ? a.slopes[head] * kLog2e : 0.0f;
+      to_dot[i] = __shfl_sync(0xffffffffu, inverse[i >> 1], (t4 * 2 + (i & 1)) * 4);
+    }
+    float o[P][NT][4];                            // column 2g of 16: rows 2 * t4 and the next; column 2g + 1: the same
+    float m[2 * NT], l[2 * NT];
+#pragma unroll
+    for (int i = 0; i < 2 * NT; ++i) { m[i] = -INFINITY; l[i] = 0.0f; }
 #pragma unroll
     for (int n = 0; n < P; ++n)
 #pragma unroll
-      for (int x = 0; x < 4; ++x) o[n][0][x] = o[n][1][x] = 0.0f;
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) o[n][i][x] = 0.0f;
 
     for (int at = from; at < to; ++at) {
       issue(stage == 0 ? kCodedStages - 1 : stage - 1);      // the slot that the tile before has left
@@ -192,72 +215,91 @@ __global__ void __launch_bounds__(kThreads, kCodedBlocks<D>) coded_rows_kernel(c
       __syncwarp();
       const u8 *ks = sh.ring[warp][stage][0], *vs = sh.ring[warp][stage][1];
       const int key0 = (c.span.first + at) * kCodedTile + warp * kCodedKeys;
-      float s[4][4];
+      float s[2][NT][4];                          // of 16 keys: g, rows 2 * t4 and the next; g + 8, the same
 #pragma unroll
-      for (int n = 0; n < 4; ++n)
+      for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) s[n][x] = 0.0f;
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) s[n][i][x] = 0.0f;
 #pragma unroll
       for (int k = 0; k < P; ++k) {
         u32 w[4];
         ldmatrix4(w, ks + code_piece<D>(lane, k) * 16);
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
-          u32 b0, b1;
-          decode_along<F>(w[n], b0, b1);
-          mma_half(s[n], qf[k], b0, b1);
+        for (int n = 0; n < 2; ++n) {
+          u32 b[4];
+          decode_along<F>(w[2 * n], b[0], b[2]);
+          decode_along<F>(w[2 * n + 1], b[1], b[3]);
+#pragma unroll
+          for (int i = 0; i < NT; ++i) mma16816<__half>(s[n][i], b, qf[k][i][0], qf[k][i][1]);
         }
       }
-      // scores in units of log2, masked; v_scale: of the values, 0 where no lane's row may take them
-      const bool all_seen = __all_sync(0xffffffffu, key0 >= lo_key[0] && key0 >= lo_key[1] && key0 + kCodedKeys <= hi_key[0] &&
-                                                        key0 + kCodedKeys <= hi_key[1]);
-      float2 v_scale[4], v_log2[4];
+      // scores in units of log2, masked
+      sees_all = true;
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        const float2 k_scale = *(const float2 *)&sh.scales[warp][stage][0][n * 8 + t4 * 2];
-        v_scale[n] = *(const float2 *)&sh.scales[warp][stage][1][n * 8 + t4 * 2];
-        v_log2[n] = make_float2(scale_log2(v_scale[n].x), scale_log2(v_scale[n].y));
+      for (int i = 0; i < 2 * NT; ++i) sees_all = sees_all && key0 >= lo_key[i] && key0 + kCodedKeys <= hi_key[i];
+      const bool all_seen = __all_sync(0xffffffffu, sees_all);
+      float v_scale[4], v_log2[4];                // of keys g, g + 8 ...
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const int i = x >> 1, key = key0 + n * 8 + t4 * 2 + (x & 1);
-          const float dot = s[n][x] * (x & 1 ? k_scale.y : k_scale.x) * to_dot[i];
+      for (int j = 0; j < 4; ++j) {
+        const float k_scale = sh.scales[warp][stage][0][8 * j + g];
+        v_scale[j] = sh.scales[warp][stage][1][8 * j + g];
+        v_log2[j] = scale_log2(v_scale[j]);
+        const int key = key0 + 8 * j + g;
+#pragma unroll
+        for (int i = 0; i < 2 * NT; ++i) {
+          float &x = s[j >> 1][i >> 1][2 * (j & 1) + (i & 1)];
+          const float dot = x * k_scale * to_dot[i];
           if (SCORED) {
             const float v = a.softcap > 0.0f ? capped_log2(dot, to_cap, a.softcap * kLog2e, to_log2) : dot * to_log2;
-            s[n][x] = v + slope[i] * (float)(key - pos[i]);
+            x = v + slope[i] * (float)(key - pos[i]);
           } else {
-            s[n][x] = dot * to_log2;
+            x = dot * to_log2;
           }
-          if (!all_seen && (key < lo_key[i] || key >= hi_key[i])) s[n][x] = -INFINITY;
+          if (!all_seen && (key < lo_key[i] || key >= hi_key[i])) x = -INFINITY;
         }
       }
+      bool moved = false;
+      float f[2 * NT], base[2 * NT];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < 2 * NT; ++i) {
         float top = -INFINITY;
 #pragma unroll
-        for (int n = 0; n < 4; ++n) top = fmaxf(top, fmaxf(s[n][2 * i] + v_log2[n].x, s[n][2 * i + 1] + v_log2[n].y));
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        for (int j = 0; j < 4; ++j) top = fmaxf(top, s[j >> 1][i >> 1][2 * (j & 1) + (i & 1)] + v_log2[j]);
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
         const float was = m[i];
         m[i] = fmaxf(was, top);
-        const float most = m[i] == -INFINITY ? 0.0f : m[i], base = most - kLift;   // nothing seen yet: every weight is 2^-inf = 0
-        if (__any_sync(0xffffffffu, m[i] != was)) {
-          const float f = exp2_approx(was - most);
-          l[i] *= f;
+        const float most = m[i] == -INFINITY ? 0.0f : m[i];
+        base[i] = most - kLift;                   // nothing seen yet: every weight is 2^-inf = 0
+        f[i] = exp2_approx(was - most);
+        moved = moved || m[i] != was;
+      }
+      if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
-          for (int n = 0; n < P; ++n)
+        for (int i = 0; i < 2 * NT; ++i) {
+          l[i] *= f[i];
 #pragma unroll
-            for (int y = 0; y < 2; ++y) { o[n][y][2 * i] *= f; o[n][y][2 * i + 1] *= f; }
+          for (int n = 0; n < P; ++n) { o[n][i >> 1][i & 1] *= f[i]; o[n][i >> 1][2 + (i & 1)] *= f[i]; }
         }
+      }
+      u32 weights[4][NT];                         // of 8 keys, then of their transposes
 #pragma unroll
-        for (int n = 0; n < 4; ++n)
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          float u[2];
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            const float w = exp2_approx(s[n][2 * i + x] - base), scale = x ? v_scale[n].y : v_scale[n].x;
-            l[i] += w;
+            const float score = s[j >> 1][n][2 * (j & 1) + x], w = exp2_approx(score - base[2 * n + x]);
+            l[2 * n + x] += w;
             // a key that the row does not see has weight 0 whatever its value's scale is
-            s[n][2 * i + x] = !all_seen && s[n][2 * i + x] == -INFINITY ? 0.0f : w * scale;
+            u[x] = !all_seen && score == -INFINITY ? 0.0f : w * v_scale[j];
           }
-      }
+          weights[j][n] = transpose8(pack2<__half>(u[0], u[1]));
+        }
 #pragma unroll
       for (int n = 0; n < P; ++n) {
         u32 w[4], even[4], odd[4];
@@ -270,10 +312,9 @@ __global__ void __launch_bounds__(kThreads, kCodedBlocks<D>) coded_rows_kernel(c
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const u32 pf[4] = {pack2<__half>(s[2 * j][0], s[2 * j][1]), pack2<__half>(s[2 * j][2], s[2 * j][3]), pack2<__half>(s[2 * j + 1][0], s[2 * j + 1][1]),
-                             pack2<__half>(s[2 * j + 1][2], s[2 * j + 1][3])};
-          mma_half(o[n][0], pf, even[2 * j], even[2 * j + 1]);
-          mma_half(o[n][1], pf, odd[2 * j], odd[2 * j + 1]);
+          const u32 b[4] = {even[2 * j], odd[2 * j], even[2 * j + 1], odd[2 * j + 1]};
+#pragma unroll
+          for (int i = 0; i < NT; ++i) mma16816<__half>(o[n][i], b, weights[2 * j][i], weights[2 * j + 1][i]);
         }
       }
       __syncwarp();
@@ -285,15 +326,16 @@ __global__ void __launch_bounds__(kThreads, kCodedBlocks<D>) coded_rows_kernel(c
     // --- join the four warps
     float *mine = (float *)sh.ring[warp][stage][0];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-      const int row = g + 8 * i;
-      if (t4 == 0) { sh.m[warp][row] = m[i] - kLift; sh.l[warp][row] = l[i]; }
+    for (int i = 0; i < 2 * NT; ++i) {
+      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 4);
+      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 8);
+      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 16);
+      const int row = (i >> 1) * 8 + t4 * 2 + (i & 1);
+      if (g == 0) { sh.m[warp][row] = m[i] - kLift; sh.l[warp][row] = l[i]; }
       if (row < rows) {
 #pragma unroll
         for (int n = 0; n < P; ++n)
-          *(float4 *)(mine + row * D + (n ^ (row & 1)) * 16 + t4 * 4) = make_float4(o[n][0][2 * i], o[n][1][2 * i], o[n][0][2 * i + 1], o[n][1][2 * i + 1]);
+          *(float2 *)(mine + row * D + (n ^ (t4 & 1)) * 16 + g * 2) = make_float2(o[n][i >> 1][i & 1], o[n][i >> 1][2 + (i & 1)]);
       }
     }
     __syncthreads();
@@ -312,15 +354,15 @@ __global__ void __launch_bounds__(kThreads, kCodedBlocks<D>) coded_rows_kernel(c
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
         const float f = exp2_approx(sh.m[w][row] - base);
-        const float4 v = *(const float4 *)((const float *)sh.ring[w][stage][0] + row * D + ((col >> 4) ^ (row & 1)) * 16 + (col & 15));
+        const float4 v = *(const float4 *)((const float *)sh.ring[w][stage][0] + row * D + ((col >> 4) ^ (row >> 1 & 1)) * 16 + (col & 15));
         sum += f * sh.l[w][row];
         acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
       }
       if (whole) {
         finish_row<T, D>((const Attn &)a, NoRows{}, c.req.q0, row0 + row, c.h, col, acc, top, sum);
       } else {
-        *(float4 *)(a.part_o + ((i64)slot * kRows + row) * D + col) = acc;
-        if (col == 0) *(float2 *)(a.part_ml + ((i64)slot * kRows + row) * 2) = make_float2(top, sum);
+        *(float4 *)(a.part_o + ((i64)slot * kUnitRows + row) * D + col) = acc;
+        if (col == 0) *(float2 *)(a.part_ml + ((i64)slot * kUnitRows + row) * 2) = make_float2(top, sum);
       }
     }
     if (!whole) {
@@ -334,7 +376,7 @@ __global__ void __launch_bounds__(kThreads, kCodedBlocks<D>) coded_rows_kernel(c
         __threadfence();
       }
       __syncthreads();
-      if (sh.last) join_parts<T, D, kRows, kThreads, 1, 8>((const Attn &)a, NoRows{}, c, row0, rows, i0, i1);
+      if (sh.last) join_parts<T, D, kUnitRows, kThreads, 1, 8>((const Attn &)a, NoRows{}, c, row0, rows, i0, i1);
     }
     __syncthreads();
     stage = stage + 1 == kCodedStages ? 0 : stage + 1;
@@ -342,35 +384,37 @@ __global__ void __launch_bounds__(kThreads, kCodedBlocks<D>) coded_rows_kernel(c
   cp_async_wait<0>();
 }
 
-template <typename T, Format F, int D, bool SCORED>
+template <typename T, Format F, int D, bool SCORED, int NT>
 cudaError_t launch_coded(const CodedAttn &a, u32 sms, cudaStream_t s) {
   static bool ready[64] = {};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev < 64 && !ready[dev]) {
-    e = cudaFuncSetAttribute(coded_rows_kernel<T, F, D, SCORED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(CodedShared<D>));
+    e = cudaFuncSetAttribute(coded_rows_kernel<T, F, D, SCORED, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(CodedShared<D>));
     if (e != cudaSuccess) return e;
     ready[dev] = true;
   }
-  return launch_kernel<Attn>(coded_rows_kernel<T, F, D, SCORED>, sms * kCodedBlocks<D>, kThreads, sizeof(CodedShared<D>), s, a);
+  return launch_kernel<Attn>(coded_rows_kernel<T, F, D, SCORED, NT>, sms * kCodedBlocks<D, NT>, kThreads, sizeof(CodedShared<D>), s, a);
 }
 
 template <typename T, Format F, int D>
-cudaError_t pick_coded_scored(const CodedAttn &a, u32 sms, cudaStream_t s) {
-  return a.softcap > 0.0f || a.slopes ? launch_coded<T, F, D, true>(a, sms, s) : launch_coded<T, F, D, false>(a, sms, s);
+cudaError_t pick_coded_scored(const CodedAttn &a, bool few, u32 sms, cudaStream_t s) {
+  if (a.softcap > 0.0f || a.slopes) return few ? launch_coded<T, F, D, true, 1>(a, sms, s) : launch_coded<T, F, D, true, 2>(a, sms, s);
+  return few ? launch_coded<T, F, D, false, 1>(a, sms, s) : launch_coded<T, F, D, false, 2>(a, sms, s);
 }
 
 template <typename T, Format F>
-cudaError_t pick_coded_dim(const CodedAttn &a, int dim, u32 sms, cudaStream_t s) {
-  if (dim == 64) return pick_coded_scored<T, F, 64>(a, sms, s);
-  if (dim == 96) return pick_coded_scored<T, F, 96>(a, sms, s);
-  return pick_coded_scored<T, F, 128>(a, sms, s);
+cudaError_t pick_coded_dim(const CodedAttn &a, int dim, bool few, u32 sms, cudaStream_t s) {
+  if (dim == 64) return pick_coded_scored<T, F, 64>(a, few, sms, s);
+  if (dim == 96) return pick_coded_scored<T, F, 96>(a, few, sms, s);
+  return pick_coded_scored<T, F, 128>(a, few, sms, s);
 }
 
+// few: no request has more than 8 rows.
 template <Format F>
-cudaError_t launch_coded_rows_of(const CodedAttn &a, int dtype, int dim, u32 sms, cudaStream_t s) {
-  return dtype == 0 ? pick_coded_dim<__nv_bfloat16, F>(a, dim, sms, s) : pick_coded_dim<__half, F>(a, dim, sms, s);
+cudaError_t launch_coded_rows_of(const CodedAttn &a, int dtype, int dim, bool few, u32 sms, cudaStream_t s) {
+  return dtype == 0 ? pick_coded_dim<__nv_bfloat16, F>(a, dim, few, sms, s) : pick_coded_dim<__half, F>(a, dim, few, sms, s);
 }
 
 }  // namespace

@@ -318,7 +318,8 @@ extern "C" int gorio_paged_attention_quantized(const gorio_quantized_attention_d
                                                    : launch_coded_chunk_int8(a, (int)p.dtype, (int)p.dim, (u32)sms, s, &e);
     if (ran) return launched(e, "quantized attention");
   }
-  e = d->format == GORIO_CODES_E4M3 ? launch_coded_rows_e4m3(a, (int)p.dtype, (int)p.dim, (u32)sms, s)
-                                    : launch_coded_rows_int8(a, (int)p.dtype, (int)p.dim, (u32)sms, s);
+  const bool few = (uint64_t)p.max_new * (p.n_heads / p.n_kv_heads) <= 8;
+  e = d->format == GORIO_CODES_E4M3 ? launch_coded_rows_e4m3(a, (int)p.dtype, (int)p.dim, few, (u32)sms, s)
+                                    : launch_coded_rows_int8(a, (int)p.dtype, (int)p.dim, few, (u32)sms, s);
   return launched(e, "quantized attention");
 }
