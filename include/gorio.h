@@ -512,7 +512,7 @@ int gorio_paged_attention_quantized(const gorio_quantized_attention_desc *d, voi
  *                 tables hold.
  *   group_starts  i32 [n_groups+1], cut to [0, n_requests]; it must not decrease (where it does, results are not defined).
  *   scratch       gorio_prefix_scratch_bytes() bytes, 256-byte aligned, of any content; free again when the call's kernels have run.
- * Two kernels, of which the second may begin before the first has ended.  Preconditions: those of gorio_paged_attention, 1 to 2^20 groups,
+ * Two or three kernels, each of which may begin before the one before it has ended.  Preconditions: those of gorio_paged_attention, 1 to 2^20 groups,
  * (prefix_width + table_width) * page_size + n_tokens < 2^31.
  */
 typedef struct {

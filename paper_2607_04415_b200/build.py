@@ -9,7 +9,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libgorio.so")
 SOURCES = ["gorio_api.cu", "search_kernels.cu", "noalloc_entry.cu", "paged_api.cu", "paged_tables.cu", "paged_rows.cu", "paged_chunk.cu",
-           "prefix_rows.cu", "prefix_chunk.cu", "prefix_chunk_own.cu",
+           "prefix_rows.cu", "prefix_chunk.cu", "prefix_chunk_own.cu", "prefix_join.cu",
            "coded_store.cu", "coded_rows_e4m3.cu", "coded_rows_int8.cu", "coded_chunk_e4m3.cu", "coded_chunk_int8.cu"]
 HEADERS = ["gorio_internal.h", os.path.join("..", "..", "include", "gorio.h")] + [
     os.path.join("device", f) for f in ("mem.cuh", "queue.cuh", "page_cache.cuh", "scoring.cuh", "arrival.cuh", "batch.cuh",

@@ -58,45 +58,55 @@ __device__ __forceinline__ u32 encode4(float2 a, float2 b, float inverse) {
   return __byte_perm(__byte_perm(b0, b1, 0x0040), __byte_perm(b2, b3, 0x0040), 0x5410);
 }
 
-// A row of d numbers: M = max |x|, scale = M / L, codes = x * (L / M) rounded (L = 448 or 127).  LANES lanes a row, 16 bytes each,
-// all loads of EACH tokens in flight at once; M is a maximum over bits and over the lanes.  Read once, written once: 3 bytes and a bit a
-// number.  Below M = 2^-100 (bfloat16 only) L / M would leave the range of 32 bits: such a row is stored as zeros.
+// A row of d numbers: M = max |x|, scale = M / L, codes = x * (L / M) rounded (L = 448 or 127).  LANES lanes a row, two pieces of 16 bytes each, one
+// LANES pieces behind the other; all loads of EACH tokens are in flight at once; M is a maximum over bits and over the lanes.  Read once, written
+// once: 3 bytes and a bit a number.  What is left beside that are instructions, and of those the ones that a row has whatever its length (slots,
+// the maximum over lanes, two divisions): a piece a lane, with twice the lanes, took 34 us for 16383 tokens of 8 heads of 128 (float16 to int8) where this takes 28.
+// Below M = 2^-100 (bfloat16 only) L / M would leave the range of 32 bits: such a row is stored as zeros.
+constexpr int kPieces = 2;
+
 template <typename T, Format F, int LANES, int EACH>
 __global__ void __launch_bounds__(kThreads) store_kernel(const RowsArgs a) {
   const u32 group = blockIdx.x * (kThreads / LANES) + threadIdx.x / LANES, lane = threadIdx.x % LANES;
   const u32 step = group / a.columns;
   const i64 first = (i64)step * EACH;
   if (first >= a.d.n_tokens) return;             // all lanes of a row together
-  const u32 row_lanes = (LANES == 32 ? 0xffffffffu : (1u << (LANES & 31)) - 1) << ((threadIdx.x & 31) / LANES * LANES);
+  const u32 row_lanes = ((1u << LANES) - 1) << ((threadIdx.x & 31) / LANES * LANES);
   const Side s = side_of(a.d, group - step * a.columns);
-  const bool mine = lane * 8 < a.d.dim;
   const u32 places = a.d.n_pages * a.d.page_size;
-  uint4 x[EACH];
+  uint4 x[EACH][kPieces];
   i64 slot[EACH];
 #pragma unroll
   for (int i = 0; i < EACH; ++i) {
-    slot[i] = -1;
-    x[i] = make_uint4(0, 0, 0, 0);
-    if (first + i < a.d.n_tokens) {
-      slot[i] = a.d.slots[first + i];
-      if (mine) x[i] = __ldcs((const uint4 *)(s.wide + (first + i) * s.wide_t + lane * 8));
+    slot[i] = first + i < a.d.n_tokens ? a.d.slots[first + i] : -1;
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+      const u32 at = (lane + j * LANES) * 8;
+      x[i][j] = make_uint4(0, 0, 0, 0);
+      if (first + i < a.d.n_tokens && at < a.d.dim) x[i][j] = __ldcs((const uint4 *)(s.wide + (first + i) * s.wide_t + at));
     }
   }
 #pragma unroll
   for (int i = 0; i < EACH; ++i) {
-    u32 m = largest8(x[i]);
+    if ((u64)slot[i] >= (u64)places) continue;   // negative ones too; the same for all lanes of a row
+    u32 m = __vmaxu2(largest8(x[i][0]), largest8(x[i][1]));
 #pragma unroll
     for (int k = LANES / 2; k; k >>= 1) m = __vmaxu2(m, __shfl_xor_sync(row_lanes, m, k));
     m = max(m & 0xffffu, m >> 16);
-    if ((u64)slot[i] >= (u64)places) continue;   // negative ones too; the same for all lanes of a row
     const bool finite = (m & ExponentBits<T>::mask) != ExponentBits<T>::mask;
     const float top = unpack2<T>(m).x;
     const bool some = finite && top >= 0x1p-100f;
     const float scale = finite ? (some ? top / kLargest<F> : 0.0f) : __int_as_float(0x7fffffff), inverse = some ? kLargest<F> / top : 0.0f;
-    uint2 codes = make_uint2(encode4<F>(unpack2<T>(x[i].x), unpack2<T>(x[i].y), inverse), encode4<F>(unpack2<T>(x[i].z), unpack2<T>(x[i].w), inverse));
-    if (!some) codes = make_uint2(0, 0);
     const u32 page = (u32)slot[i] / a.d.page_size, in = (u32)slot[i] - page * a.d.page_size;
-    if (mine) *(uint2 *)(s.codes + (i64)page * s.codes_p + (i64)in * s.codes_t + lane * 8) = codes;
+    u8 *const to = s.codes + (i64)page * s.codes_p + (i64)in * s.codes_t;
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+      const u32 at = (lane + j * LANES) * 8;
+      const uint4 w = x[i][j];
+      uint2 codes = make_uint2(encode4<F>(unpack2<T>(w.x), unpack2<T>(w.y), inverse), encode4<F>(unpack2<T>(w.z), unpack2<T>(w.w), inverse));
+      if (!some) codes = make_uint2(0, 0);
+      if (at < a.d.dim) *(uint2 *)(to + at) = codes;
+    }
     if (lane == 0) s.scale[(i64)page * s.scale_p + (i64)in * s.scale_t] = scale;
   }
 }
@@ -107,36 +117,46 @@ __global__ void __launch_bounds__(kThreads) load_kernel(const RowsArgs a) {
   const u32 group = blockIdx.x * (kThreads / LANES) + threadIdx.x / LANES, lane = threadIdx.x % LANES;
   const u32 step = group / a.columns;
   const i64 first = (i64)step * EACH;
-  if (first >= a.d.n_tokens || lane * 8 >= a.d.dim) return;
+  if (first >= a.d.n_tokens) return;
   const Side s = side_of(a.d, group - step * a.columns);
   const u32 places = a.d.n_pages * a.d.page_size;
   i64 slot[EACH];
 #pragma unroll
   for (int i = 0; i < EACH; ++i) slot[i] = first + i < a.d.n_tokens ? a.d.slots[first + i] : -1;
-  uint2 codes[EACH];
+  uint2 codes[EACH][kPieces];
   float scale[EACH];
 #pragma unroll
   for (int i = 0; i < EACH; ++i) {
-    codes[i] = make_uint2(0, 0);
     scale[i] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) codes[i][j] = make_uint2(0, 0);
     if ((u64)slot[i] < (u64)places) {
       const u32 page = (u32)slot[i] / a.d.page_size, in = (u32)slot[i] - page * a.d.page_size;
-      codes[i] = *(const uint2 *)(s.codes + (i64)page * s.codes_p + (i64)in * s.codes_t + lane * 8);
+      const u8 *const from = s.codes + (i64)page * s.codes_p + (i64)in * s.codes_t;
+#pragma unroll
+      for (int j = 0; j < kPieces; ++j) {
+        const u32 at = (lane + j * LANES) * 8;
+        if (at < a.d.dim) codes[i][j] = *(const uint2 *)(from + at);
+      }
       scale[i] = s.scale[(i64)page * s.scale_p + (i64)in * s.scale_t];
     }
   }
 #pragma unroll
   for (int i = 0; i < EACH; ++i) {
     if (first + i >= a.d.n_tokens) break;
-    u32 h[4];
-    decode_along<F>(codes[i].x, h[0], h[1]);
-    decode_along<F>(codes[i].y, h[2], h[3]);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float2 v = unpack2<__half>(h[k]);
-      h[k] = pack2<T>(v.x * scale[i], v.y * scale[i]);
+    for (int j = 0; j < kPieces; ++j) {
+      const u32 at = (lane + j * LANES) * 8;
+      u32 h[4];
+      decode_along<F>(codes[i][j].x, h[0], h[1]);
+      decode_along<F>(codes[i][j].y, h[2], h[3]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 v = unpack2<__half>(h[k]);
+        h[k] = pack2<T>(v.x * scale[i], v.y * scale[i]);
+      }
+      if (at < a.d.dim) __stcs((uint4 *)(s.wide + (first + i) * s.wide_t + at), make_uint4(h[0], h[1], h[2], h[3]));
     }
-    __stcs((uint4 *)(s.wide + (first + i) * s.wide_t + lane * 8), make_uint4(h[0], h[1], h[2], h[3]));
   }
 }
 
@@ -161,9 +181,9 @@ cudaError_t launch_lanes(const RowsArgs &a, bool store, cudaStream_t s) {
 
 template <typename T, Format F>
 cudaError_t pick_lanes(const RowsArgs &a, bool store, cudaStream_t s) {
-  if (a.d.dim <= 64) return launch_lanes<T, F, 8>(a, store, s);
-  if (a.d.dim <= 128) return launch_lanes<T, F, 16>(a, store, s);
-  return launch_lanes<T, F, 32>(a, store, s);
+  if (a.d.dim <= 64) return launch_lanes<T, F, 4>(a, store, s);
+  if (a.d.dim <= 128) return launch_lanes<T, F, 8>(a, store, s);
+  return launch_lanes<T, F, 16>(a, store, s);
 }
 
 template <typename T>

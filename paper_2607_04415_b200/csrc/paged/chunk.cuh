@@ -184,6 +184,21 @@ __device__ __forceinline__ bool write_part(const A &a, const Rows &covered, Shar
           if (valid) end.template write32<T>(a, r.tok, r.head, col + k, o + k);
       }
     }
+  } else if (leaves_parts(a)) {
+    // A part of a cut unit stays as it is, [part][row][column], as its readers go along a row.
+    if (mine && fine) {
+      const i64 slot = 2 * (i64)blockIdx.x + (blockIdx.x == p.i0 ? 1 : 0);
+      *(float2 *)(a.part_ml + (slot * kRows + unit_row) * 2) = make_float2(m, l);
+      if (valid && blockIdx.x == p.i0) tell_parts(a, r.tok * a.hq + r.head, p.i0, p.i1, unit_row, kRows);
+#pragma unroll 1
+      for (int col = 0; col < D; col += kCols) {
+        float o[kCols];
+        output(o, col);
+#pragma unroll
+        for (int k = 0; k < kCols / 4; ++k)
+          __stcg((float4 *)(a.part_o + (slot * kRows + unit_row) * D + col) + k, make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]));
+      }
+    }
   } else if (fine) {
     // A cut unit.  The last block to get here joins the parts, its own out of tensor memory; the others leave theirs in
     // the workspace: [part][column / 4][row][4], so that neighbouring threads' rows lie side by side.
@@ -349,7 +364,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
     tmem_alloc(&sh.tmem, 512);
   }
   let_second_begin(a);
-  const Plan plan = block_plan<kRows, kTileKeys, kOver, kThreads>(a, sh.plan, kSpread);
+  const Plan plan = block_plan<kRows, kTileKeys, kOver, kThreads>(a, sh.plan, leaves_parts(a) ? 0.0f : kSpread);
   const auto covered = covered_rows(a);
   mma_fence_before();
   __syncthreads();

@@ -39,17 +39,21 @@ struct Attn {
   u32 wait_ticks;              // of 1024 ns: a wait inside the chunk kernel gives up when it has lasted as long
 };
 
-// Attention over keys that the requests of a group share takes two kernels.  The first, over the shared keys, sees the groups as its
+// Attention over keys that the requests of a group share takes three kernels.  The first, over the shared keys, sees the groups as its
 // requests (Attn's tables, lengths and n_req are theirs, `starts` are the requests' rows) and leaves each row's weighted sum of
-// values, its maximum and its sum of weights in 32 bits.  The second, over each request's own keys, joins them to its own
-// before it writes a row.  It may begin while the first still runs (and then has its own counters and parts), and waits for its end
-// before it reads what the first has left.
+// values, its maximum and its sum of weights in 32 bits.  Where there are few units, it leaves the parts of those that are cut, and a small second
+// kernel joins them, a warp a row: in the first that would be the work of one block for each unit (64 requests over 16391 shared keys, 8
+// units: 67 us, where it takes 39 without).  The last, over each request's own keys, joins what is left to its own rows before it writes them.
+// Each may begin while the one before still runs, and waits for its end before it reads what that has left; the last has
+// its own counters and parts.
 struct PrefixAttn : Attn {
   const int *group_starts;     // [n_req + 1]: the requests of each group
   const int *own_lengths;      // [n_members]
   u32 n_members, own_places;   // requests; the most keys of its own that one can have
   float *mid_o;                // [n_tok][hq][dim]
   float2 *mid_ml;              // [n_tok][hq]: maximum in units of log2, sum
+  u32 leaves_parts;
+  int4 *mid_at;                // [n_tok][hq]: first and last block of its unit's parts (none: whole), row in the part, rows of a part
 };
 struct OwnAttn : Attn {
   const int *group_starts;
@@ -57,17 +61,26 @@ struct OwnAttn : Attn {
   const float *mid_o;
   const float2 *mid_ml;
 };
+__device__ __forceinline__ bool leaves_parts(const Attn &) { return false; }
+__device__ __forceinline__ bool leaves_parts(const PrefixAttn &a) { return a.leaves_parts != 0; }
+// A row's parts are those of blocks i0..i1, of `rows` rows, and in each in row `place`.
+__device__ __forceinline__ void tell_parts(const Attn &, i64, u32, u32, int, int) {}
+__device__ __forceinline__ void tell_parts(const PrefixAttn &a, i64 row, u32 i0, u32 i1, int place, int rows) {
+  a.mid_at[row] = make_int4((int)i0, (int)i1, place, rows);
+}
 constexpr u32 kOwnCounters = (u32)(kCounterBytes / 8);     // the second kernel's counters: the other half
 
 __device__ __forceinline__ u32 *error_word(const Attn &a) { return a.arrived + kErrorWord; }
 __device__ __forceinline__ u32 *error_word(const OwnAttn &a) { return a.arrived + (kErrorWord - kOwnCounters); }
 
 // The kernel that was launched before this one with leave to overlap has ended, and what it wrote is visible.
+__device__ __forceinline__ void wait_for_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_first(const Attn &) {}
-__device__ __forceinline__ void wait_for_first(const OwnAttn &) { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_first(const OwnAttn &) { wait_for_kernel(); }
 // The next kernel of the stream may begin where this one leaves room.
+__device__ __forceinline__ void let_next_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void let_second_begin(const Attn &) {}
-__device__ __forceinline__ void let_second_begin(const PrefixAttn &) { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void let_second_begin(const PrefixAttn &) { let_next_begin(); }
 
 // One request as the kernels see it: keys it can have at most, its new tokens and where their rows
 // start.  Bad lengths or starts are cut to what the tables and the query tensor hold, so that no
@@ -412,11 +425,17 @@ cudaError_t launch_rows(const PrefixAttn &a, int dtype, int dim, u32 sms, cudaSt
 bool launch_chunk(const OwnAttn &a, int dtype, int dim, u32 sms, cudaStream_t s, cudaError_t *e);
 cudaError_t launch_rows(const OwnAttn &a, int dtype, int dim, u32 sms, cudaStream_t s);
 
-// A kernel that reads what a first one leaves is launched with leave to begin before that one has ended.
+// Joins the parts that the first kernel has left of cut units.
+cudaError_t launch_prefix_join(const PrefixAttn &a, int dim, u32 sms, cudaStream_t s);
+
+// A kernel that reads what the one before leaves is launched with leave to begin before that one has ended.
+struct Joining {};
 template <typename A>
 struct Overlaps { static constexpr bool value = false; };
 template <>
 struct Overlaps<OwnAttn> { static constexpr bool value = true; };
+template <>
+struct Overlaps<Joining> { static constexpr bool value = true; };
 template <typename A, typename... Args>
 cudaError_t launch_kernel(void (*kernel)(Args...), u32 blocks, u32 threads, size_t shared, cudaStream_t s, Args... args) {
   cudaLaunchAttribute overlap{};

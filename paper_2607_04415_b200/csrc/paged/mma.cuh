@@ -141,7 +141,10 @@ struct PrefixRowEnd {
   float *to;
   __device__ __forceinline__ PrefixRowEnd(const PrefixAttn &a, const NoRows &, i64 tok, int head, int dim, float m, float l, bool first) {
     to = a.mid_o + (tok * a.hq + head) * dim;
-    if (first) a.mid_ml[tok * a.hq + head] = make_float2(m, l);
+    if (first) {
+      a.mid_ml[tok * a.hq + head] = make_float2(m, l);
+      a.mid_at[tok * a.hq + head] = make_int4(0, -1, 0, 0);
+    }
   }
   template <typename T>
   __device__ __forceinline__ void write4(const PrefixAttn &, i64, int, int col, float4 o) const { *(float4 *)(to + col) = o; }

@@ -310,9 +310,13 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<D>) attention_rows_kern
       } else {
         *(float4 *)(a.part_o + ((i64)slot * kRows + row) * D + col) = acc;
         if (col == 0) *(float2 *)(a.part_ml + ((i64)slot * kRows + row) * 2) = make_float2(top, sum);
+        if (leaves_parts(a) && col == 0 && blockIdx.x == i0) {
+          const int tok = (int)((row0 + row) / a.group), head = (int)((row0 + row) - (i64)tok * a.group) + (int)(c.h * a.group);
+          tell_parts(a, (i64)(c.req.q0 + tok) * a.hq + head, i0, plan.shares.owner(unit0 + (u32)c.span.tiles - 1), row, kRows);
+        }
       }
     }
-    if (!whole) {
+    if (!whole && !leaves_parts(a)) {
       const u32 i1 = plan.shares.owner(unit0 + (u32)c.span.tiles - 1);
       __threadfence();
       __syncthreads();

@@ -56,7 +56,15 @@ std::atomic<uint64_t> wait_limit{kWaitLimitNs};
 //   8 key heads of 128, 1 request, 192 rows each:   150 keys 12 us, chunk kernel 24;     2000 keys 27 against 32
 //                                    96 rows each:  8000 keys 38 against 39;            131072 keys 482 against 150
 //   2 key heads of 64, 64 requests, 24 rows each:    150 keys 12 against 18;              8000 keys 94 against 88
-bool takes_rows(const gorio_paged_attention_desc &d) {
+// For 8-bit codes both kernels pay for taking them apart: a unit of 16 rows 0.5 ps for half the bytes, one of the chunk kernel 1.12 ps, and with
+// at most 128 rows, one row tile, 1.44 (16 requests, 8 key heads of 128, 65536 keys: 16 rows 542 us, 24 rows some 1090 against 1550, 48 rows 1626
+// against 1551, 192 rows 6500 against 1183).
+struct Costs {
+  double row_unit, chunk_unit, chunk_tile;       // ps an element of a key
+};
+constexpr Costs kWideCosts{0.6, 1.0, 1.0}, kCodedCosts{0.5, 1.12, 1.44};
+
+bool takes_rows(const gorio_paged_attention_desc &d, const Costs &c = kWideCosts) {
   const double group = d.n_heads / d.n_kv_heads, requests = d.n_requests < d.n_tokens ? d.n_requests : d.n_tokens;
   if ((double)d.max_new * group <= 16) return true;
   auto units = [&](double rows) {
@@ -65,7 +73,8 @@ bool takes_rows(const gorio_paged_attention_desc &d) {
   };
   const double places = (double)d.table_width * d.page_size, seen = (double)d.window + d.max_new;
   const double keys = d.window && seen < places ? seen : places;
-  return 0.6 * units(16) * (keys + 384) * d.dim <= 14e6 + units(256) * keys * d.dim;
+  const double chunk = d.max_new * group <= 128 ? c.chunk_tile : c.chunk_unit;
+  return c.row_unit * units(16) * (keys + 384) * d.dim <= 14e6 + chunk * units(256) * keys * d.dim;
 }
 
 }  // namespace
@@ -209,9 +218,9 @@ extern "C" int gorio_paged_attention(const gorio_paged_attention_desc *d, void *
 
 namespace {
 
-// What a call on shared keys needs besides the workspace: the second kernel's parts, then the first kernel's results.
+// What a call on shared keys needs besides the workspace: the last kernel's parts, then the first one's results.
 uint64_t mid_ml_bytes(uint64_t rows) { return (rows * sizeof(float2) + 255) / 256 * 256; }
-uint64_t scratch_bytes(int sms, uint64_t rows, uint64_t dim) { return part_bytes((u32)sms) + mid_ml_bytes(rows) + rows * dim * sizeof(float); }
+uint64_t scratch_bytes(int sms, uint64_t rows, uint64_t dim) { return part_bytes((u32)sms) + 3 * mid_ml_bytes(rows) + rows * dim * sizeof(float); }
 
 }  // namespace
 
@@ -237,7 +246,8 @@ extern "C" int gorio_prefix_attention(const gorio_prefix_attention_desc *d, void
 
   const uint64_t rows = (uint64_t)own.n_tokens * own.n_heads;
   float2 *const mid_ml = (float2 *)((char *)d->scratch + part_bytes((u32)sms));
-  float *const mid_o = (float *)((char *)mid_ml + mid_ml_bytes(rows));
+  int4 *const mid_at = (int4 *)((char *)mid_ml + mid_ml_bytes(rows));             // twice as large
+  float *const mid_o = (float *)((char *)mid_at + 2 * mid_ml_bytes(rows));
   PrefixAttn p{};
   fill_attention(p, &own, sms);
   p.tables = d->prefix_tables; p.lengths = d->prefix_lengths; p.tab_r = d->prefix_table_stride;
@@ -245,10 +255,16 @@ extern "C" int gorio_prefix_attention(const gorio_prefix_attention_desc *d, void
   p.causal = 0;                                              // shared keys stand before all new tokens
   p.group_starts = d->group_starts; p.own_lengths = own.lengths;
   p.n_members = own.n_requests; p.own_places = own.table_width * own.page_size;
-  p.mid_o = mid_o; p.mid_ml = mid_ml;
+  p.mid_o = mid_o; p.mid_ml = mid_ml; p.mid_at = mid_at;
   gorio_paged_attention_desc shared = own;                   // bounds of the first kernel's rows and keys
   shared.n_requests = d->n_groups; shared.table_width = d->prefix_width; shared.max_new = own.n_tokens;
+  // Units of the first kernel, by their bounds: with few, joining their parts is a kernel of its own.  9 groups of 1155 tokens in all, 2 key heads of 7:
+  // some 80 units, 84 us with the joins in the first kernel and 94 with their own.
+  const bool rows_kernel = takes_rows(shared);
+  const double per_unit = rows_kernel ? 16 : 256, units = own.n_kv_heads * ((double)own.n_tokens * (own.n_heads / own.n_kv_heads) / per_unit + d->n_groups);
+  p.leaves_parts = units < sms / 2;
   cudaError_t e = launch_attention(p, shared, sms, (cudaStream_t)cuda_stream);
+  if (e == cudaSuccess && p.leaves_parts) e = launch_prefix_join(p, (int)own.dim, (u32)sms, (cudaStream_t)cuda_stream);
   if (e != cudaSuccess) return launched(e, "prefix attention");
 
   OwnAttn o{};
@@ -313,7 +329,7 @@ extern "C" int gorio_paged_attention_quantized(const gorio_quantized_attention_d
   }
   const cudaStream_t s = (cudaStream_t)cuda_stream;
   cudaError_t e = cudaSuccess;
-  if (!takes_rows(p)) {
+  if (!takes_rows(p, kCodedCosts)) {
     const bool ran = d->format == GORIO_CODES_E4M3 ? launch_coded_chunk_e4m3(a, (int)p.dtype, (int)p.dim, (u32)sms, s, &e)
                                                    : launch_coded_chunk_int8(a, (int)p.dtype, (int)p.dim, (u32)sms, s, &e);
     if (ran) return launched(e, "quantized attention");
