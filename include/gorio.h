@@ -487,8 +487,9 @@ int gorio_cache_load_quantized(const gorio_quantized_rows_desc *d, void *cuda_st
 /*
  * Attention over a quantised cache: gorio_paged_attention where key_pages and value_pages hold codes, with code * scale for each
  * number.  attention.dtype is that of q and out; strides of its pages count codes and must be multiples of 16.  Scores
- * are products of exact codes and of q in 32-bit sums.  A weight is multiplied by its value's scale before it is rounded, once, to
- * 16 bits, or the value by its scale, rounded once to 11 bits (many rows); a scale counts fully between 2^-80 and 2^80.
+ * are products of exact codes and of q (as float16 times a power of two a row, exact but for what lies below 2^-38 of the row's largest) in
+ * 32-bit sums.  A weight is multiplied by its value's scale before it is rounded, once, to float16's 11 bits, of the whole range of that
+ * type; a scale counts fully between 2^-80 and 2^80.
  * A scale that is not a number reaches the queries that see its key, and no others.  Preconditions otherwise as there.
  */
 typedef struct {

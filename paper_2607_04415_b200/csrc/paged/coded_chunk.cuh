@@ -6,18 +6,18 @@
 //             power of two.
 //   8         issues both products (one thread).
 //   9         copies codes of keys and values, and their scales, into the stages that they are taken apart in.
-//   10        makes a tile's factors of the scales of its values.
+//   10        brings the scales of a tile's values to its power of two.
 //   11        walks the block's share of the work and tells the others its parts.
 //   12-15     take codes apart, in place, into the 16-bit tiles that the products read.  (With a ring of their own for codes three pieces of 64 keys
-//             were all that shared memory held beside them, too few on their way: 972 us where this takes 658 for 2048 tokens over 18432 keys.)
-// Keys become their codes, exactly; a score is multiplied by its key's scale in 32 bits.  Values are multiplied by their scales as they
-// become float16, one rounding to 11 bits; so that neither side of that leaves float16's range, a tile has a power of two of its own, taken out of
-// its values and put into its weights: 2^(x + shift - m) with m the running maximum of x + shift, whose sum is taken back by 2^-shift once a tile.
-// The factor is a float16 too: a second rounding to 11 bits, which all numbers of a row share (a factor of 22 bits in two numbers took 25 % longer).
+//             were all that shared memory held beside them, too few on their way: 972 us where this takes 663 for 2048 tokens over 18432 keys.)
+// Keys and values become their codes, exactly.  A score is multiplied by its key's scale in 32 bits, and a weight by its value's before it is rounded, once, to
+// float16.  So that weights use that type's range whatever the scales are, a tile has a power of two of its own, that of its largest value's scale: weights
+// are 2^(x + shift - m) * (scale * 2^-shift) with m the running maximum of x + shift; their sum, without the scale, is taken back by 2^-shift once a
+// tile.  (With values multiplied by their scales as they become float16, two roundings more, float16 results were 3.7e-4 off where this is 2.9e-4 off and
+// a rounding is 2.1e-4.)
 //
-// A value's scale that is not finite would reach rows that do not see its key as 0 * inf in the product.  It is left out there, and stands in the
-// key's place instead: scores of rows that see the key are then not a number.  With it all operands are finite, so that tiles that some rows
-// see and others do not need no care beyond the mask.
+// A value's scale that is not finite counts as 0 there, and stands in the key's place instead: scores of rows that see the key are then not a number,
+// others do not notice.  With it all operands are finite, so that tiles that some rows see and others do not need no care beyond the mask.
 #pragma once
 #include "chunk.cuh"
 #include "coded.cuh"
@@ -30,7 +30,7 @@ namespace paged {
 namespace {
 
 constexpr int kCodedThreads = 512;
-constexpr int kCodedSoftmaxRegs = 184, kCodedOtherRegs = 72, kDecodeRegs = 72;   // a thread, of 128 * 4 = 184 * 2 + 72 + 72 at launch
+constexpr int kCodedSoftmaxRegs = 200, kCodedOtherRegs = 64, kDecodeRegs = 48;   // a thread, of 128 * 4 = 200 * 2 + 64 + 48 at launch
 constexpr int kScaleSlots = 4;                                   // tiles whose scales are there
 
 template <int D>
@@ -44,7 +44,7 @@ struct CodedChunkShared {
   unsigned char q[2][CodedShape<D>::tile_bytes];
   unsigned char kv[CodedShape<D>::stages][CodedShape<D>::tile_bytes];
   __align__(128) float k_scale[kScaleSlots][kTileKeys];
-  u32 v_factor[kScaleSlots][kTileKeys];          // float16, twice; until it is there, the scale
+  float v_scale[kScaleSlots][kTileKeys];         // times 2^-shift, when warp 10 is done with it
   u32 scales_boxes[kScaleSlots];                 // which boxes of them were copied
   int shift[kScaleSlots];
   float q_to_dot[kTileRows];                     // of the rows of a unit of one row tile
@@ -65,10 +65,21 @@ __device__ __forceinline__ f32x2 mul_f32x2(f32x2 a, f32x2 b) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
   return v;
 }
-__device__ __forceinline__ u32 mul_f16x2(u32 a, u32 b) {
-  u32 v;
-  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(v) : "r"(a), "r"(b));
-  return v;
+// weights64 for values with scales of their own: the sum is that of the weights alone.
+__device__ __forceinline__ void scaled_weights64(const float *s, const float *scale, f32x2 mul, f32x2 minus_base, f32x2 (&sum)[2], u32 *w) {
+#pragma unroll
+  for (int k = 0; k < 32; k += 2) {
+    const float4 v = *(const float4 *)(scale + 2 * k);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float x0, x1;
+      unpack_f32(fma_f32x2(pack_f32(s[2 * (k + i)], s[2 * (k + i) + 1]), mul, minus_base), x0, x1);
+      const f32x2 x = pack_f32(exp2_approx(x0), exp2_approx(x1));
+      sum[i] = add_f32x2(sum[i], x);
+      unpack_f32(mul_f32x2(x, i ? pack_f32(v.z, v.w) : pack_f32(v.x, v.y)), x0, x1);
+      w[k + i] = pack2<__half>(x0, x1);
+    }
+  }
 }
 __device__ __forceinline__ void bar_arrive_n(u64 *bar, u32 n) {
   asm volatile("mbarrier.arrive.shared.b64 _, [%0], %1;" ::"r"(smem_addr(bar)), "r"(n) : "memory");
@@ -92,7 +103,7 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (warp == 8) {
     if (lane < S::stages) { bar_init(&sh.codes_full[lane], 1); bar_init(&sh.kv_full[lane], 4); bar_init(&sh.kv_empty[lane], 1); }
-    if (lane < kScaleSlots) { bar_init(&sh.scales_there[lane], 1); bar_init(&sh.scales_full[lane], 1); bar_init(&sh.scales_empty[lane], 12); }
+    if (lane < kScaleSlots) { bar_init(&sh.scales_there[lane], 1); bar_init(&sh.scales_full[lane], 1); bar_init(&sh.scales_empty[lane], 8); }
     if (lane < kParts) { bar_init(&sh.part_full[lane], 1); bar_init(&sh.part_empty[lane], 15); }
     if (lane < 2) {
       bar_init(&sh.q_full[lane], 4); bar_init(&sh.q_empty[lane], 1); bar_init(&sh.s_full[lane], 1); bar_init(&sh.o_full[lane], 1);
@@ -207,8 +218,6 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
             unpack_f32(mul_f32x2(pack_f32(s[i + 2], s[i + 3]), pack_f32(k.z, k.w)), s[i + 2], s[i + 3]);
           }
           const int shift = sh.shift[slot];
-          __syncwarp();
-          if (lane == 0) bar_arrive_n(&sh.scales_empty[slot], split ? 2 : 1);
           const int key0 = (p.tile + at) * kTileKeys;
           if (SCORES != kPlain) {                            // to units of log2, with cap and bias
             const float linear = a.scale * kLog2e * to_dot;
@@ -223,7 +232,7 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
             m = to;
             l *= f;
             if (at > first) {                                // the scores' arrival says that the product before is done
-              // 16 columns at a time: with 32, beside the 128 scores, values that every tile needs were spilled
+              // 16 columns at a time: with 32, beside the 128 scores, what every tile needs was spilled
 #pragma unroll 1
               for (int i = 0; i < D / 16; ++i) {
                 float o[16];
@@ -242,13 +251,14 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
 #pragma unroll
           for (int i = 0; i < 2; ++i) {                      // the product starts on the first half of the weights
             u32 w[32];
-            weights64<__half>(s + 64 * i, mul2, base2, sum, w);
+            scaled_weights64(s + 64 * i, sh.v_scale[slot] + 64 * i, mul2, base2, sum, w);
             tmem_st32(scores + 32 * i, w);
             tmem_wait_st();
             mma_fence_before();
             __syncwarp();
             if (lane == 0) bar_arrive(&sh.p_full[t][i]);
           }
+          if (lane == 0) bar_arrive_n(&sh.scales_empty[slot], split ? 2 : 1);      // all lanes have read them before they told of their weights
           float l0, l1;
           unpack_f32(add_f32x2(sum[0], sum[1]), l0, l1);
           l = fmaf(l0 + l1, power_of_two(-shift), l);
@@ -315,17 +325,13 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
     constexpr int kGroup = D == 64 ? 32 : 16, kEach = D == 96 ? 3 : 4;      // rows that are read before they are written; a lane's pieces of them
     auto row_at = [&](int i) { return D == 128 ? (i >> 1) * 8 + (lane >> 2) : D == 96 && i == 2 ? lane >> 1 : i * 8 + (lane >> 2); };
     auto piece_at = [&](int i) { return D == 128 ? (i & 1) * 4 + (lane & 3) : D == 96 && i == 2 ? 4 + (lane & 1) : lane & 3; };
-    // This warp's 32 rows of a tile; `factors` are its values' or NULL.
-    auto decode_rows = [&](unsigned char *tile, const u32 *factors, auto clean) {
+    // This warp's 32 rows of a tile.
+    auto decode_rows = [&](unsigned char *tile, auto clean) {
 #pragma unroll 1
       for (int row0 = (warp - 12) * 32; row0 < (warp - 11) * 32; row0 += kGroup) {
         uint4 w[kEach];
-        u32 f[kEach];
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-          w[i] = *(const uint4 *)(tile + (row0 + row_at(i)) * 128 + piece_at(i) * 16);
-          if (factors) f[i] = factors[row0 + row_at(i)];
-        }
+        for (int i = 0; i < kEach; ++i) w[i] = *(const uint4 *)(tile + (row0 + row_at(i)) * 128 + piece_at(i) * 16);
         __syncwarp();
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
@@ -335,9 +341,9 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
           decode_along<F>(w[i].y, h[2], h[3]);
           decode_along<F>(w[i].z, h[4], h[5]);
           decode_along<F>(w[i].w, h[6], h[7]);
-          if (factors) {
+          if (decltype(clean)::value) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) h[k] = mul_f16x2(decltype(clean)::value ? finite_codes<F>(h[k]) : h[k], f[i]);
+            for (int k = 0; k < 8; ++k) h[k] = finite_codes<F>(h[k]);
           }
           unsigned char *const at = tile + (piece >> 3) * (kTileKeys * 128) + row * 128;
           *(uint4 *)(at + (((piece & 7) ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
@@ -348,26 +354,20 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
       __syncwarp();
     };
     int stage = 0;
-    u32 phase = 0, tile_no = 0;
+    u32 phase = 0;
     bool fine = true;
     PartInfo p;
     for (u32 no = 0; fine && take_part(no, p); ++no) {
-      for (int at = 0; at < p.tiles && fine; ++at, ++tile_no) {
-        const u32 slot = tile_no % kScaleSlots;
+      for (int at = 0; at < p.tiles && fine; ++at) {
         const int key0 = (p.tile + at) * kTileKeys;
         const bool every = key0 >= p.every0 && key0 + kTileKeys <= p.every1;      // all rows see all keys of the tile
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
-          if (kv) fine = fine && wait(&sh.scales_full[slot], (tile_no / kScaleSlots) & 1);
           fine = fine && wait(&sh.codes_full[stage], phase);
           if (!fine) break;
-          if (!kv) decode_rows(sh.kv[stage], nullptr, std::false_type{});
-          else if (F != kE4m3 || every) decode_rows(sh.kv[stage], sh.v_factor[slot], std::false_type{});
-          else decode_rows(sh.kv[stage], sh.v_factor[slot], std::true_type{});
-          if (lane == 0) {
-            bar_arrive(&sh.kv_full[stage]);
-            if (kv) bar_arrive(&sh.scales_empty[slot]);
-          }
+          if (F != kE4m3 || !kv || every) decode_rows(sh.kv[stage], std::false_type{});
+          else decode_rows(sh.kv[stage], std::true_type{});
+          if (lane == 0) bar_arrive(&sh.kv_full[stage]);
           if (++stage == S::stages) { stage = 0; phase ^= 1; }
         }
       }
@@ -527,7 +527,7 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
           if (there) {
             const int to = lane * (int)box_rows;
             copy_scales(&sh.k_scale[slot][to], a.ks + (i64)p.h * a.ks_h + (i64)page_now * a.ks_p + in_now, box_rows * 4, &sh.scales_there[slot]);
-            copy_scales(&sh.v_factor[slot][to], a.vs + (i64)p.h * a.vs_h + (i64)page_now * a.vs_p + in_now, box_rows * 4, &sh.scales_there[slot]);
+            copy_scales(&sh.v_scale[slot][to], a.vs + (i64)p.h * a.vs_h + (i64)page_now * a.vs_p + in_now, box_rows * 4, &sh.scales_there[slot]);
           }
 #pragma unroll
           for (int kv = 0; kv < 2; ++kv) {
@@ -546,10 +546,9 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
       for (u32 i = 0; i < kScaleSlots; ++i) drain(&sh.scales_there[i], i < tile_no % kScaleSlots ? (tile_no / kScaleSlots) & 1 : ((tile_no / kScaleSlots) & 1) ^ 1);
     } else if (warp == 10) {
       // ---------------------------------------------------------------- the scales
-      // A lane has keys lane, lane + 32 ... of a tile.  Of the finite scales of a tile's values the largest one's power of two becomes the
-      // tile's: factors are then below 2^7 (e4m3, whose codes are at most 448) or 2^8 (whole numbers, at most 128).  Keys outside the unit's have
-      // factor 0, whatever is there.
-      constexpr int kTop = F == kE4m3 ? 6 : 7, kRange = 100;
+      // A lane has keys lane, lane + 32 ... of a tile.  The power of two above the largest finite scale of its values becomes the tile's.  Keys outside the
+      // unit's have scale 0, whatever is there.
+      constexpr int kRange = 100;
       u32 tile_no = 0;
       bool fine = true;
       PartInfo p;
@@ -564,7 +563,7 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
 #pragma unroll
           for (int j = 0; j < kTileKeys / 32; ++j) {
             const int key = (p.tile + at) * kTileKeys + j * 32 + lane;
-            v[j] = __uint_as_float(sh.v_factor[slot][j * 32 + lane]);
+            v[j] = sh.v_scale[slot][j * 32 + lane];
             if (!(all >> ((u32)(j * 32 + lane) / box_rows) & 1)) {    // outside the cache: zeros
               v[j] = 0.0f;
               sh.k_scale[slot][j * 32 + lane] = 0.0f;
@@ -577,13 +576,10 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
             most = max(most, __float_as_uint(fabsf(v[j])));
           }
           most = __reduce_max_sync(0xffffffffu, most);
-          const int e = min(kRange, max(-kRange, (int)(most >> 23) - 127)) - kTop;
+          const int e = min(kRange, max(-kRange, (int)(most >> 23) - 126));
           const float down = power_of_two(-e);
 #pragma unroll
-          for (int j = 0; j < kTileKeys / 32; ++j) {
-            const float f = fminf(fmaxf(v[j] * down, -power_of_two(kTop + 1)), power_of_two(kTop + 1));   // scales past 2^100 too are finite here
-            sh.v_factor[slot][j * 32 + lane] = pack2<__half>(f, f);
-          }
+          for (int j = 0; j < kTileKeys / 32; ++j) sh.v_scale[slot][j * 32 + lane] = fminf(fmaxf(v[j] * down, -1.0f), 1.0f);     // past 2^100 it is cut
           if (lane == 0) sh.shift[slot] = e;
           fence_async();                                              // the next copy to this slot comes after these accesses
           __syncwarp();

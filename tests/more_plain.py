@@ -7,15 +7,14 @@ import torch
 UNIT = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}      # largest relative error of one rounding
 
 
-def attend(q, k, v, sees, far, softcap=0.0, slopes=None, scale=None, weights=None, value_unit=0.0, tiny=None):
+def attend(q, k, v, sees, far, softcap=0.0, slopes=None, scale=None, weights=None, tiny=None):
     """(out, lse, out_tolerance, lse_tolerance) of one request: q [n, heads, d] of its type, k and v [key heads, keys, d] in 64 bits, sees
     [n, keys], far [n, keys] = key's position - query's.
 
     Tolerances, for a unit `weights` of the weights' type (default: q's), and sums of D products in 32 bits: a score is off by at
     most e = D * 2^-23 * scale * sum|q||k| (each of D additions rounds or cuts one unit) plus a few 2^-22 of its own
     size for scale, cap, bias and the change to log2, so a weight by 2e relative to their sum, and by `weights` for its
-    rounding (plus, in float16, `tiny` of the largest weight below the normal numbers); values by `value_unit` of
-    themselves; the result rounds once more."""
+    rounding (plus, in float16, `tiny` of the largest weight below the normal numbers); the result rounds once more."""
     n, heads, d = q.shape
     kv, keys, _ = k.shape
     group = heads // kv
@@ -56,7 +55,7 @@ def attend(q, k, v, sees, far, softcap=0.0, slopes=None, scale=None, weights=Non
         eb = torch.where(sees, e, 0.0).amax(1, keepdim=True)
         a = w @ clean.abs()
         out[:, h] = o
-        out_tol[:, h] = u * o.abs() + (w_unit + value_unit + 2 * eb + 2.0 ** -18) * a + tiny * keys * clean.abs().amax()
+        out_tol[:, h] = u * o.abs() + (w_unit + 2 * eb + 2.0 ** -18) * a + tiny * keys * clean.abs().amax()
         lse[:, h] = (base + total.log())[:, 0]
         lse_tol[:, h] = eb[:, 0] + 2.0 ** -18 + 2.0 ** -21 * torch.where(torch.isfinite(lse[:, h]), lse[:, h].abs(), 0.0)
     return out, lse, out_tol, lse_tol

@@ -240,10 +240,9 @@ class Coded:
                 sees &= j[None] <= at[:, None]
             if self.opts["window"]:
                 sees &= j[None] > at[:, None] - self.opts["window"]
-            # rounded to float16's 11 bits, 2^-11 of themselves at most: weights (few rows: times scales); many rows: a scale's factor and the
-            # value times it, one after the other
+            # weights times scales are rounded to float16's 11 bits, 2^-11 of themselves at most; codes are exact
             parts.append(attend(self.q[self.starts[r]:self.starts[r + 1]], k, v, sees, j[None] - at[:, None], self.opts["softcap"], self.opts["slopes"],
-                                weights=2.0 ** -11, value_unit=2.0 ** -10, **more))
+                                weights=2.0 ** -11, **more))
         return [torch.cat(x) for x in zip(*parts)]
 
     def check(self, gorio, **more):

@@ -48,6 +48,6 @@ def test_sample_and_keep(codes):
         k, v = _rows(c["key_codes"], ids, length, c["key_scales"]), _rows(c["value_codes"], ids, length, c["value_scales"])
         at, j = torch.arange(length - n, length, device="cuda"), torch.arange(length, device="cuda")
         rows = slice(int(c["starts"][i]), int(c["starts"][i + 1]))
-        # the roundings to 11 bits of weights, of a scale's factor and of the value times it
-        parts.append(attend(c["q"][rows], k, v, j[None] <= at[:, None], j[None] - at[:, None], weights=2.0 ** -11, value_unit=2.0 ** -10))
+        # the rounding to 11 bits of weights times scales
+        parts.append(attend(c["q"][rows], k, v, j[None] <= at[:, None], j[None] - at[:, None], weights=2.0 ** -11))
     assert_near(c, [torch.cat(x) for x in zip(*parts)])
