@@ -61,12 +61,12 @@ __device__ __forceinline__ u32 encode4(float2 a, float2 b, float inverse) {
 // A row of d numbers: M = max |x|, scale = M / L, codes = x * (L / M) rounded (L = 448 or 127).  LANES lanes a row, two pieces of 16 bytes each, one
 // LANES pieces behind the other; all loads of EACH tokens are in flight at once; M is a maximum over bits and over the lanes.  Read once, written
 // once: 3 bytes and a bit a number.  What is left beside that are instructions, and of those the ones that a row has whatever its length (slots,
-// the maximum over lanes, two divisions): a piece a lane, with twice the lanes, took 34 us for 16383 tokens of 8 heads of 128 (float16 to int8) where this takes 28.
+// the maximum over lanes, two divisions): a piece a lane, with twice the lanes, took 34 us for 16383 tokens of 8 heads of 128 (float16 to int8) where this takes 25.
 // Below M = 2^-100 (bfloat16 only) L / M would leave the range of 32 bits: such a row is stored as zeros.
 constexpr int kPieces = 2;
 
 template <typename T, Format F, int LANES, int EACH>
-__global__ void __launch_bounds__(kThreads) store_kernel(const RowsArgs a) {
+__global__ void __launch_bounds__(kThreads, 4) store_kernel(const RowsArgs a) {
   const u32 group = blockIdx.x * (kThreads / LANES) + threadIdx.x / LANES, lane = threadIdx.x % LANES;
   const u32 step = group / a.columns;
   const i64 first = (i64)step * EACH;

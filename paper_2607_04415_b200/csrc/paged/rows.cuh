@@ -31,6 +31,12 @@ constexpr int kWarpKeys = 16;
 constexpr int kTile = kWarps * kWarpKeys;
 constexpr int kStages = 3;
 constexpr int kOver = 1;            // a unit's start and end cost about what a tile does
+// Behind shared keys, requests' own are few: with more places without work between units fewer of them are cut, which there costs more than uneven
+// shares do (64 requests of up to 1024 own keys behind 16391 shared ones: 102 us with 1, 96 with 3 and with 6, 100 with 12).
+template <typename A>
+constexpr int kOverOf = kOver;
+template <>
+constexpr int kOverOf<OwnAttn> = 4;
 constexpr float kSpread = 0.25f;    // joining 16 parts takes about what a tile does
 // As many as shared memory (24 KB a warp at head size 128) and registers hold: at head size 64, 64 ragged single-token requests take
 // 96 us with four blocks, 101 with three, 122 with two; more stages instead did nothing.
@@ -62,7 +68,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<D>) attention_rows_kern
   RowsShared<D> &sh = *(RowsShared<D> *)raw;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   let_second_begin(a);
-  const Plan plan = block_plan<kRows, kTile, kOver, kThreads>(a, sh.plan, kSpread);
+  const Plan plan = block_plan<kRows, kTile, kOverOf<A>, kThreads>(a, sh.plan, kSpread);
   if (plan.begin >= plan.end) {
     wait_for_first(a);                           // so that this kernel never ends before the first
     return;
@@ -80,7 +86,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<D>) attention_rows_kern
   const bool in_line = 32 % P == 0 && a.page % kWarpKeys == 0;
   Cursor ld = plan.first;
   u32 ld_left = plan.end - plan.begin;
-  settle<kRows, kTile, kOver>(a, ld, ld_left, plan.fill);
+  settle<kRows, kTile, kOverOf<A>>(a, ld, ld_left, plan.fill);
   int key_page = -1, key_in = 0;                 // of key (lane & 15) of the tile at ld; -1: zeros
   auto look_up = [&]() {
     if (ld_left == 0) return;
@@ -123,7 +129,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<D>) attention_rows_kern
       }
       --ld_left;
       ++ld.at;
-      settle<kRows, kTile, kOver>(a, ld, ld_left, plan.fill);
+      settle<kRows, kTile, kOverOf<A>>(a, ld, ld_left, plan.fill);
       look_up();
     }
     cp_async_commit();
@@ -137,7 +143,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<D>) attention_rows_kern
   int stage = 0;
   const int g = lane >> 2, t4 = lane & 3;
   u32 left = plan.end - plan.begin;
-  for (settle<kRows, kTile, kOver>(a, c, left, plan.fill); left; settle<kRows, kTile, kOver>(a, c, left, plan.fill)) {
+  for (settle<kRows, kTile, kOverOf<A>>(a, c, left, plan.fill); left; settle<kRows, kTile, kOverOf<A>>(a, c, left, plan.fill)) {
     const int from = c.at;
     const int to = (int)min((u32)c.span.tiles, (u32)from + left);
     const i64 row0 = (i64)c.m * kRows;
