@@ -489,7 +489,8 @@ int gorio_cache_load_quantized(const gorio_quantized_rows_desc *d, void *cuda_st
  * number.  attention.dtype is that of q and out; strides of its pages count codes and must be multiples of 16.  Scores
  * are products of exact codes and of q (as float16 times a power of two a row, exact but for what lies below 2^-38 of the row's largest) in
  * 32-bit sums.  A weight is multiplied by its value's scale before it is rounded, once, to float16's 11 bits, of the whole range of that
- * type; a scale counts fully between 2^-80 and 2^80.
+ * type; a scale counts fully between 2^-80 and 2^80.  Weights count from maxima of x + log2(scale of the value), so that scores and lse are off by some
+ * 2^-23 of that logarithm besides.
  * A scale that is not a number reaches the queries that see its key, and no others.  Preconditions otherwise as there.
  */
 typedef struct {

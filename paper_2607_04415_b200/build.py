@@ -70,7 +70,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
             def compile_one(src, obj):
                 subprocess.check_call([nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-c", os.path.join(CSRC, src), "-o", obj])
             from concurrent.futures import ThreadPoolExecutor
-            with ThreadPoolExecutor(max(1, min(len(SOURCES), os.cpu_count() or 1))) as pool:
+            with ThreadPoolExecutor(max(1, min(8, os.cpu_count() or 1))) as pool:      # a compiler takes a gigabyte or two
                 list(pool.map(compile_one, SOURCES, objs))
             tmp = LIB_PATH + ".tmp"
             subprocess.check_call([nvcc, "-shared", "-o", tmp] + objs + ["-lcudart"])
