@@ -31,7 +31,10 @@ namespace {
 
 constexpr int kCodedThreads = 512;
 constexpr int kCodedSoftmaxRegs = 200, kCodedOtherRegs = 64, kDecodeRegs = 48;   // a thread, of 128 * 4 = 200 * 2 + 64 + 48 at launch
-constexpr int kScaleSlots = 4;                                   // tiles whose scales are there
+// Tiles whose scales are there.  The second softmax warpgroup has nothing to wait for in a part of one row tile and one key tile, and so may come to a tile that is
+// as many behind the first one's as parts are told ahead.  Parity says whether a slot has been filled for it only while that slot cannot be the first one's.
+constexpr int kScaleSlots = 8;
+static_assert(kScaleSlots > kParts, "a wait for scales would pass on those of an earlier tile");
 
 template <int D>
 struct CodedShape {
