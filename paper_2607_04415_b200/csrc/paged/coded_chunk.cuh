@@ -579,7 +579,8 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
             most = max(most, __float_as_uint(fabsf(v[j])));
           }
           most = __reduce_max_sync(0xffffffffu, most);
-          const int e = min(kRange, max(-kRange, (int)(most >> 23) - 126));
+          // values that are all 0 add nothing: as far down as this goes, their tile's sum could leave the range when it is taken back
+          const int e = most ? min(kRange, max(-kRange, (int)(most >> 23) - 126)) : 0;
           const float down = power_of_two(-e);
 #pragma unroll
           for (int j = 0; j < kTileKeys / 32; ++j) sh.v_scale[slot][j * 32 + lane] = fminf(fmaxf(v[j] * down, -1.0f), 1.0f);     // past 2^100 it is cut
