@@ -60,6 +60,14 @@ __device__ __forceinline__ u32 finite_codes(u32 h) {
   return h;
 }
 
+// log2 of a value's scale, cut to what running maxima count.  A weight is 2^(x - m + 15) at most, m >= x + log2(scale): with a scale of 0 it is 2^95, which sums
+// of 2^32 keys hold; with the largest scale it is some 2^-90, and still above what is flushed to 0 for keys that weigh 2^-30 of it.
+__device__ __forceinline__ float scale_log2(float scale) {
+  float e;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fabsf(scale)));
+  return fminf(fmaxf(e, -80.0f), 100.0f);                     // also of a scale that is not a number
+}
+
 // 4 bytes, or zeros
 __device__ __forceinline__ void cp_async4(void *to, const void *from, u32 bytes) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_addr(to)), "l"(from), "r"(bytes) : "memory");

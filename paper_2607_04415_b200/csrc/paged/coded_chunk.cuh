@@ -6,15 +6,17 @@
 //             power of two.
 //   8         issues both products (one thread).
 //   9         copies codes of keys and values, and their scales, into the stages that they are taken apart in.
-//   10        brings the scales of a tile's values to its power of two.
+//   10        finds the logarithms of the scales of a tile's values, and their range.
 //   11        walks the block's share of the work and tells the others its parts.
 //   12-15     take codes apart, in place, into the 16-bit tiles that the products read.  (With a ring of their own for codes three pieces of 64 keys
-//             were all that shared memory held beside them, too few on their way: 972 us where this takes 663 for 2048 tokens over 18432 keys.)
+//             were all that shared memory held beside them, too few on their way: 972 us where this takes 674 for 2048 tokens over 18432 keys.)
 // Keys and values become their codes, exactly.  A score is multiplied by its key's scale in 32 bits, and a weight by its value's before it is rounded, once, to
-// float16.  So that weights use that type's range whatever the scales are, a tile has a power of two of its own, that of its largest value's scale: weights
-// are 2^(x + shift - m) * (scale * 2^-shift) with m the running maximum of x + shift; their sum, without the scale, is taken back by 2^-shift once a
-// tile.  (With values multiplied by their scales as they become float16, two roundings more, float16 results were 3.7e-4 off where this is 2.9e-4 off and
-// a rounding is 2.1e-4.)
+// float16: 2^(x - m) * scale.  So that weights use that type's range whatever the scales are, m follows the maximum of x + log2(scale), as in the kernel of few rows.
+// Where a row sees all of a tile and the tile's scales lie within 2^4 of each other, the largest x and the largest scale stand for it, at most 4 more; elsewhere it is found
+// key by key, where it may move m.  So a row's weights are the same whatever scales the keys have that it does not see.  (Key by key in every tile is 128 numbers more
+// from shared memory for each row: 771 us where this takes 674 for 2048 tokens over 18432 keys; scales within the exponent, 2^(x + log2(scale) - m), which the
+// sum then takes back by a product, 861.  The largest scale in every tile loses the weights of rows whose own scales lie far below it.  With values
+// multiplied by their scales as they become float16, two roundings more, float16 results were 3.7e-4 off where this is 2.9e-4 off and a rounding is 2.1e-4.)
 //
 // A value's scale that is not finite counts as 0 there, and stands in the key's place instead: scores of rows that see the key are then not a number,
 // others do not notice.  With it all operands are finite, so that tiles that some rows see and others do not need no care beyond the mask.
@@ -47,9 +49,10 @@ struct CodedChunkShared {
   unsigned char q[2][CodedShape<D>::tile_bytes];
   unsigned char kv[CodedShape<D>::stages][CodedShape<D>::tile_bytes];
   __align__(128) float k_scale[kScaleSlots][kTileKeys];
-  float v_scale[kScaleSlots][kTileKeys];         // times 2^-shift, when warp 10 is done with it
+  float v_scale[kScaleSlots][kTileKeys];
+  float v_log2[kScaleSlots][kTileKeys];
+  float2 v_range[kScaleSlots];                   // the largest and the smallest of them
   u32 scales_boxes[kScaleSlots];                 // which boxes of them were copied
-  int shift[kScaleSlots];
   float q_to_dot[kTileRows];                     // of the rows of a unit of one row tile
   PartInfo part[kParts];
   u64 codes_full[CodedShape<D>::stages], kv_full[CodedShape<D>::stages], kv_empty[CodedShape<D>::stages];
@@ -94,7 +97,19 @@ __device__ __forceinline__ void copy_scales(void *to, const float *from, u32 byt
                "r"(smem_addr(bar))
                : "memory");
 }
-__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((u32)(127 + e) << 23); }
+// The largest of 128 scores * mul + logarithms of their values' scales.  Few registers, one load after the other: where this stands nearly all are taken, and what
+// the compiler would load ahead it spills for in every tile (757 us where this way takes 694 for 2048 tokens over 18432 keys, before the part was read anew).
+__device__ __forceinline__ float largest_scaled128(const float *s, float mul, const float *log2s) {
+  float top = -INFINITY;
+  const u32 at = smem_addr(log2s);
+#pragma unroll
+  for (int i = 0; i < 128; i += 2) {
+    float a, b;
+    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(a), "=f"(b) : "r"(at + i * 4));
+    top = fmaxf(fmaxf(top, fmaf(s[i], mul, a)), fmaf(s[i + 1], mul, b));
+  }
+  return top;
+}
 
 template <typename T, Format F, int D, Scores SCORES>
 __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __grid_constant__ CodedAttn a, const __grid_constant__ CUtensorMap keys,
@@ -220,14 +235,21 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
             unpack_f32(mul_f32x2(pack_f32(s[i], s[i + 1]), pack_f32(k.x, k.y)), s[i], s[i + 1]);
             unpack_f32(mul_f32x2(pack_f32(s[i + 2], s[i + 3]), pack_f32(k.z, k.w)), s[i + 2], s[i + 3]);
           }
-          const int shift = sh.shift[slot];
           const int key0 = (p.tile + at) * kTileKeys;
           if (SCORES != kPlain) {                            // to units of log2, with cap and bias
             const float linear = a.scale * kLog2e * to_dot;
             scores128<SCORES>(a, s, a.softcap > 0.0f ? cap_in(a) * to_dot : linear, linear, slope, slope * (float)(key0 - r.pos));
           }
           if (__any_sync(0xffffffffu, key0 < r.lo || key0 + kTileKeys > r.hi)) mask128(s, r.lo - key0, r.hi - key0);
-          const float top = largest128(s) * mul + (float)shift;
+          const f32x2 mul2 = pack_f32(mul, mul);
+          const float2 range = sh.v_range[slot];
+          float top = largest128(s) * mul + range.x;
+          const bool by_key = key0 < r.lo || key0 + kTileKeys > r.hi || range.x - range.y > 4.0f;
+          // half an octave less than what moves m, for the roundings of what stands for the maximum
+          if (__any_sync(0xffffffffu, by_key && (top > m + 7.5f || (m == -INFINITY && top > -INFINITY)))) {
+            const float found = largest_scaled128(s, mul, sh.v_log2[slot]);
+            if (by_key) top = found;
+          }
           const bool moves = top > m + 8.0f || (m == -INFINITY && top > -INFINITY);
           if (__any_sync(0xffffffffu, moves)) {
             const float to = moves ? top : m;
@@ -248,9 +270,9 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
               }
             }
           }
-          const float minus_base = m == -INFINITY ? 0.0f : kLift - m + (float)shift;
-          const f32x2 mul2 = pack_f32(mul, mul), base2 = pack_f32(minus_base, minus_base);
-          f32x2 sum[2] = {pack_f32(0.0f, 0.0f), pack_f32(0.0f, 0.0f)};
+          const float minus_base = m == -INFINITY ? 0.0f : kLift - m;
+          const f32x2 base2 = pack_f32(minus_base, minus_base);
+          f32x2 sum[2] = {pack_f32(l, 0.0f), pack_f32(0.0f, 0.0f)};
 #pragma unroll
           for (int i = 0; i < 2; ++i) {                      // the product starts on the first half of the weights
             u32 w[32];
@@ -264,9 +286,10 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
           if (lane == 0) bar_arrive_n(&sh.scales_empty[slot], split ? 2 : 1);      // all lanes have read them before they told of their weights
           float l0, l1;
           unpack_f32(add_f32x2(sum[0], sum[1]), l0, l1);
-          l = fmaf(l0 + l1, power_of_two(-shift), l);
+          l = l0 + l1;
         }
       }
+      p = sh.part[no % kParts];                              // anew: kept through the tiles, it would take the registers that those are short of
       tile_no += (u32)p.tiles;
       m -= kLift;                                            // what the weights and their sum count from
       const bool two = split && p.tiles > 1;                 // both warpgroups have a part of the same rows
@@ -314,7 +337,8 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
 #pragma unroll
         for (int k = 0; k < kCols; k += 32) keep(o + k);
       };
-      fine = write_part<T, D, kCols>((const Attn &)a, NoRows{}, sh, p, r, valid, mine, fine, unit_row, m, l, meet, output, output32);
+      fine = write_part<T, D, kCols>((const Attn &)a, NoRows{}, sh, p, row_of(a, p, (u32)p.row0 + (valid ? unit_row : 0)), valid, mine, fine, unit_row, m, l, meet,
+                                     output, output32);
       mma_fence_before();
       if (two || !p.whole) fine = fine && meet();            // sh.last and the other's output are free again
       part_done(no);
@@ -549,9 +573,7 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
       for (u32 i = 0; i < kScaleSlots; ++i) drain(&sh.scales_there[i], i < tile_no % kScaleSlots ? (tile_no / kScaleSlots) & 1 : ((tile_no / kScaleSlots) & 1) ^ 1);
     } else if (warp == 10) {
       // ---------------------------------------------------------------- the scales
-      // A lane has keys lane, lane + 32 ... of a tile.  The power of two above the largest finite scale of its values becomes the tile's.  Keys outside the
-      // unit's have scale 0, whatever is there.
-      constexpr int kRange = 100;
+      // A lane has keys lane, lane + 32 ... of a tile.  Keys outside the unit's have scale 0, whatever is there.
       u32 tile_no = 0;
       bool fine = true;
       PartInfo p;
@@ -561,30 +583,32 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
           fine = wait(&sh.scales_there[slot], (tile_no / kScaleSlots) & 1);
           if (!fine) break;
           const u32 all = sh.scales_boxes[slot];
-          float v[kTileKeys / 32];
-          u32 most = 0;
+          float most = -INFINITY, least = INFINITY;
 #pragma unroll
           for (int j = 0; j < kTileKeys / 32; ++j) {
-            const int key = (p.tile + at) * kTileKeys + j * 32 + lane;
-            v[j] = sh.v_scale[slot][j * 32 + lane];
-            if (!(all >> ((u32)(j * 32 + lane) / box_rows) & 1)) {    // outside the cache: zeros
-              v[j] = 0.0f;
-              sh.k_scale[slot][j * 32 + lane] = 0.0f;
+            const int at_key = j * 32 + lane, key = (p.tile + at) * kTileKeys + at_key;
+            float v = sh.v_scale[slot][at_key];
+            if (!(all >> ((u32)at_key / box_rows) & 1)) {             // outside the cache: zeros
+              v = 0.0f;
+              sh.k_scale[slot][at_key] = 0.0f;
             }
-            if (key < p.lo || key >= p.hi) v[j] = 0.0f;
-            if (!isfinite(v[j])) {
-              sh.k_scale[slot][j * 32 + lane] = __int_as_float(0x7fffffff);
-              v[j] = 0.0f;
+            if (key < p.lo || key >= p.hi) v = 0.0f;
+            if (!isfinite(v)) {
+              sh.k_scale[slot][at_key] = __int_as_float(0x7fffffff);
+              v = 0.0f;
             }
-            most = max(most, __float_as_uint(fabsf(v[j])));
+            const float e = scale_log2(v);
+            sh.v_scale[slot][at_key] = v;
+            sh.v_log2[slot][at_key] = e;
+            most = fmaxf(most, e);
+            least = fminf(least, e);
           }
-          most = __reduce_max_sync(0xffffffffu, most);
-          // values that are all 0 add nothing: as far down as this goes, their tile's sum could leave the range when it is taken back
-          const int e = most ? min(kRange, max(-kRange, (int)(most >> 23) - 126)) : 0;
-          const float down = power_of_two(-e);
 #pragma unroll
-          for (int j = 0; j < kTileKeys / 32; ++j) sh.v_scale[slot][j * 32 + lane] = fminf(fmaxf(v[j] * down, -1.0f), 1.0f);     // past 2^100 it is cut
-          if (lane == 0) sh.shift[slot] = e;
+          for (int d = 16; d; d >>= 1) {
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+            least = fminf(least, __shfl_xor_sync(0xffffffffu, least, d));
+          }
+          if (lane == 0) sh.v_range[slot] = make_float2(most, least);
           fence_async();                                              // the next copy to this slot comes after these accesses
           __syncwarp();
           if (lane == 0) bar_arrive(&sh.scales_full[slot]);

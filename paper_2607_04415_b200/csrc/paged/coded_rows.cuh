@@ -28,7 +28,6 @@ constexpr int kCodedStages = 2;
 // Blocks of an SM for heads of D and 8 * NT rows: what shared memory (17 KB a warp at head size 128) and registers hold.
 template <int D, int NT>
 constexpr int kCodedBlocks = D == 64 ? 4 : NT == 1 ? 3 : 2;
-constexpr float kScaleRange = 80.0f;             // a scale's power of two that the maximum counts, at most
 
 template <int D>
 struct CodedShared {
@@ -47,13 +46,6 @@ __device__ __forceinline__ int code_piece(int row, int piece) {
   if (P == 8) return row * P + (piece ^ (row & 7));
   if (P == 4) return row * P + (piece ^ ((row >> 1) & 3));
   return row * P + (piece ^ ((row >> 2) & 1));   // 96 bytes: four rows lie apart by themselves, the next four one piece on
-}
-
-// log2 of a value's scale, cut to what the running maximum counts
-__device__ __forceinline__ float scale_log2(float scale) {
-  float e;
-  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fabsf(scale)));
-  return fminf(fmaxf(e, -kScaleRange), kScaleRange);          // also of a scale that is not a number
 }
 
 // The transpose of an 8 x 8 matrix of 16-bit numbers, two neighbouring columns of a row to a lane.

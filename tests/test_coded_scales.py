@@ -26,8 +26,8 @@ def keys_of(c, r, j):
 
 
 def check(c, got, rows=slice(None)):
-    """One request's rows against 64 bits.  A weight times its value's scale is rounded to float16 where the row's largest one is 2^7 or more: by
-    2^-11 of itself or, below the normal numbers, by 2^-25, which is 2^-32 of the largest.  The other errors are those of more_plain.attend: e of a score,
+    """One request's rows against 64 bits.  A weight times its value's scale is rounded to float16 where the row's largest one is 2^3 or more (2^7, or 2^4
+    less where the tile's scales lie within 2^4): by 2^-11 of itself or, below the normal numbers, by 2^-25, which is 2^-28 of the largest.  The other errors are those of more_plain.attend: e of a score,
     2e + 2^-18 of a weight, the result's own rounding; and, as weights count from a maximum that holds the logarithm of a scale (`far`, at most 80), four
     roundings of numbers of that size, 2^-24 each: score minus maximum, maximum minus 15, times ln 2, logarithm of the sum."""
     n, length = c.new[0], c.lens[0]
@@ -47,7 +47,7 @@ def check(c, got, rows=slice(None)):
         w = torch.exp(x - lse)
         out, sums = w @ vh, w @ vh.abs()
         largest = (w * vh.abs().amax(1)).amax(1, keepdim=True)
-        tol = UNIT[c.q.dtype] * out.abs() + (2.0 ** -11 + 2 * e + 2.0 ** -18 + far) * sums + length * 2.0 ** -32 * largest
+        tol = UNIT[c.q.dtype] * out.abs() + (2.0 ** -11 + 2 * e + 2.0 ** -18 + far) * sums + length * 2.0 ** -28 * largest
         off = (got["out"][rows, h].double() - out).abs()
         assert (off <= tol).all(), f"head {h}: out is off by {(off / tol).max().item():.3g} of the tolerance"
         off, tol = (got["lse"][rows, h].double() - lse[:, 0]).abs(), e[:, 0] + 2.0 ** -18 + far + 2.0 ** -21 * lse[:, 0].abs()
@@ -77,3 +77,51 @@ def test_thousands_of_values_that_are_zero(gorio, form, new):
                                           want_lse=True)
     for r in range(0, many, 13):
         check(c, {k: got[k][r * new:(r + 1) * new] for k in ("out", "lse")})
+
+
+@pytest.mark.parametrize("form", [E4M3, INT8])
+@pytest.mark.parametrize("new", [1, 5, 150])
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("down", [10, 24, 32, 40, None])
+def test_the_heaviest_key_has_the_smallest_value(gorio, form, new, wide, down):
+    """One key's score lies some 39 octaves above the others', and its value's scale `down` powers of two below theirs, or is 0."""
+    c = Coded([new], [300], heads=4, kv_heads=2, dim=64, form=form, uneven=0.5, seed=3)
+    c.q.fill_(1.0)
+    page, place = keys_of(c, 0, torch.tensor(70, device="cuda"))
+    c.ks.mul_(0.25)
+    codes, scales = encode(torch.full((2, 64), 3.5, device="cuda"), form)      # 3.5 * 64 / 8 = 28
+    c.kp.view(torch.uint8)[page, :, place], c.ks[page, :, place] = codes.view(torch.uint8), scales
+    c.vs[page, :, place] *= 0.0 if down is None else 2.0 ** -down
+    if wide:                                                                   # the chunk kernel, for more than 16 rows a key head
+        c.tables = widen(c.tables, c.page)
+    check(c, c.run(gorio))
+
+
+@pytest.mark.parametrize("form", [E4M3, INT8])
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("up", [2.0 ** 5, 2.0 ** 23, 2.0 ** 40, 0.0])
+def test_a_later_value_of_any_size_changes_nothing(gorio, form, wide, up):
+    c = Coded([150], [300], heads=4, kv_heads=2, dim=64, form=form, uneven=0.5)
+    if wide:
+        c.tables = widen(c.tables, c.page)
+    want = c.run(gorio)
+    page, place = keys_of(c, 0, torch.tensor(299, device="cuda"))
+    c.vs[page, :, place] *= up
+    got = c.run(gorio)
+    assert torch.equal(got["out"][:149], want["out"][:149]) and torch.equal(got["lse"][:149], want["lse"][:149])
+    check(c, got)
+
+
+@pytest.mark.parametrize("dim", [64, 96, 128])
+@pytest.mark.parametrize("opts", [dict(softcap=30.0), dict(softcap=100.0, slopes=True), dict(slopes=True, window=90), dict(window=140)])
+def test_a_later_value_changes_no_score_of_any_kind(gorio, dim, opts):
+    """The last two keys' scales, seen by the last two rows alone, of a size that the other keys' have, and far from it."""
+    c = Coded([250], [400], heads=4, kv_heads=2, dim=dim, uneven=0.5, seed=dim, **opts)
+    c.tables = widen(c.tables, c.page)
+    want = c.run(gorio)
+    page, place = keys_of(c, 0, torch.tensor([398, 399], device="cuda"))
+    old = c.vs[page, :, place].clone()
+    for up in (1.7, 2.0 ** 6, 2.0 ** -6, 2.0 ** 60, 0.0, math.inf):
+        c.vs[page, :, place] = old * up
+        got = c.run(gorio)
+        assert torch.equal(got["out"][:248], want["out"][:248]) and torch.equal(got["lse"][:248], want["lse"][:248])
