@@ -166,7 +166,7 @@ __device__ __forceinline__ void weights64(const float *s, f32x2 mul, f32x2 minus
 // The end of a part, by the eight warps of the softmax: its rows written, or left for or joined with the unit's other parts.  `output` gives
 // COLS columns of this thread's row, `output32` 32, as weighted sums that count from 2^m, like l.  `mine`: the thread's warpgroup writes the row.
 // Returns false once a wait has run out.
-template <typename T, int D, int COLS, typename A, typename Rows, typename Shared, typename Meet, typename Output, typename Output32>
+template <typename T, int D, int COLS, bool WIDE, typename A, typename Rows, typename Shared, typename Meet, typename Output, typename Output32>
 __device__ __forceinline__ bool write_part(const A &a, const Rows &covered, Shared &sh, const PartInfo &p, const Row &r, bool valid, bool mine, bool fine,
                                            int unit_row, float m, float l, const Meet &meet, const Output &output, const Output32 &output32) {
   typedef typename EndOf<A>::type End;
@@ -239,7 +239,7 @@ __device__ __forceinline__ bool write_part(const A &a, const Rows &covered, Shar
 #pragma unroll 4
         for (u32 i = p.i0; i <= p.i1; ++i) {
           const float2 x = __ldcg((const float2 *)(a.part_ml + (place(i) * kRows + unit_row) * 2));
-          sum += i == own ? exp2_approx(m - base) * l : exp2_approx(x.x - base) * x.y;
+          sum += i == own ? moved_sum<WIDE>(l, m - base) : moved_sum<WIDE>(x.y, x.x - base);
         }
         const End end(a, covered, r.tok, r.head, D, top, sum, valid);
 #pragma unroll 1
@@ -525,7 +525,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
 #pragma unroll
         for (int k = 0; k < kCols; k += 32) keep(o + k);
       };
-      fine = write_part<T, D, kCols>(a, covered, sh, p, r, valid, mine, fine, unit_row, m, l, meet, output, output32);
+      fine = write_part<T, D, kCols, false>(a, covered, sh, p, r, valid, mine, fine, unit_row, m, l, meet, output, output32);
       mma_fence_before();
       if (two || !p.whole) fine = fine && meet();            // sh.last and the other's output are free again
       part_done(no);

@@ -253,9 +253,9 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
           const bool moves = top > m + 8.0f || (m == -INFINITY && top > -INFINITY);
           if (__any_sync(0xffffffffu, moves)) {
             const float to = moves ? top : m;
-            const float f = m == -INFINITY ? 0.0f : exp2_approx(m - to);
+            const float half = m == -INFINITY ? 0.0f : exp2_approx(0.5f * (m - to)), f = half * half;
             m = to;
-            l *= f;
+            l = l * half * half;                             // see moved_sum
             if (at > first) {                                // the scores' arrival says that the product before is done
               // 16 columns at a time: with 32, beside the 128 scores, what every tile needs was spilled
 #pragma unroll 1
@@ -308,7 +308,7 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
           const float top = fmaxf(m, other.x), base = top == -INFINITY ? 0.0f : top;
           f0 = exp2_approx(m - base);
           f1 = exp2_approx(other.x - base);
-          l = l * f0 + other.y * f1;
+          l = moved_sum<true>(l, m - base) + moved_sum<true>(other.y, other.x - base);
           m = top;
         }
       }
@@ -337,7 +337,7 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
 #pragma unroll
         for (int k = 0; k < kCols; k += 32) keep(o + k);
       };
-      fine = write_part<T, D, kCols>((const Attn &)a, NoRows{}, sh, p, row_of(a, p, (u32)p.row0 + (valid ? unit_row : 0)), valid, mine, fine, unit_row, m, l, meet,
+      fine = write_part<T, D, kCols, true>((const Attn &)a, NoRows{}, sh, p, row_of(a, p, (u32)p.row0 + (valid ? unit_row : 0)), valid, mine, fine, unit_row, m, l, meet,
                                      output, output32);
       mma_fence_before();
       if (two || !p.whole) fine = fine && meet();            // sh.last and the other's output are free again

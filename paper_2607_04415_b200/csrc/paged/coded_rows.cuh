@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(kThreads, (kCodedBlocks<D, NT>)) coded_rows_ke
         }
       }
       bool moved = false;
-      float f[2 * NT], base[2 * NT];
+      float down[2 * NT], base[2 * NT];
 #pragma unroll
       for (int i = 0; i < 2 * NT; ++i) {
         float top = -INFINITY;
@@ -266,15 +266,16 @@ __global__ void __launch_bounds__(kThreads, (kCodedBlocks<D, NT>)) coded_rows_ke
         m[i] = fmaxf(was, top);
         const float most = m[i] == -INFINITY ? 0.0f : m[i];
         base[i] = most - kLift;                   // nothing seen yet: every weight is 2^-inf = 0
-        f[i] = exp2_approx(was - most);
+        down[i] = was - most;
         moved = moved || m[i] != was;
       }
       if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
         for (int i = 0; i < 2 * NT; ++i) {
-          l[i] *= f[i];
+          const float half = exp2_approx(0.5f * down[i]), f = half * half;
+          l[i] = l[i] * half * half;             // see moved_sum
 #pragma unroll
-          for (int n = 0; n < P; ++n) { o[n][i >> 1][i & 1] *= f[i]; o[n][i >> 1][2 + (i & 1)] *= f[i]; }
+          for (int n = 0; n < P; ++n) { o[n][i >> 1][i & 1] *= f; o[n][i >> 1][2 + (i & 1)] *= f; }
         }
       }
       u32 weights[4][NT];                         // of 8 keys, then of their transposes
@@ -347,7 +348,7 @@ __global__ void __launch_bounds__(kThreads, (kCodedBlocks<D, NT>)) coded_rows_ke
       for (int w = 0; w < kWarps; ++w) {
         const float f = exp2_approx(sh.m[w][row] - base);
         const float4 v = *(const float4 *)((const float *)sh.ring[w][stage][0] + row * D + ((col >> 4) ^ (row >> 1 & 1)) * 16 + (col & 15));
-        sum += f * sh.l[w][row];
+        sum += moved_sum<true>(sh.l[w][row], sh.m[w][row] - base);
         acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
       }
       if (whole) {
@@ -368,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, (kCodedBlocks<D, NT>)) coded_rows_ke
         __threadfence();
       }
       __syncthreads();
-      if (sh.last) join_parts<T, D, kUnitRows, kThreads, 1, 8>((const Attn &)a, NoRows{}, c, row0, rows, i0, i1);
+      if (sh.last) join_parts<T, D, kUnitRows, kThreads, 1, 8, true>((const Attn &)a, NoRows{}, c, row0, rows, i0, i1);
     }
     __syncthreads();
     stage = stage + 1 == kCodedStages ? 0 : stage + 1;

@@ -90,6 +90,15 @@ __device__ __forceinline__ float exp2_approx(float x) {
   return y;
 }
 
+// A sum that counted from 2^(m + d), d <= 0, now that it counts from 2^m.  WIDE: over codes a maximum holds the logarithm of a scale and may move by 180 octaves, while
+// the sum's weights are as far above 1: 2^d alone would be 0 and the sum lost.
+template <bool WIDE>
+__device__ __forceinline__ float moved_sum(float sum, float d) {
+  if (!WIDE) return exp2_approx(d) * sum;
+  const float h = exp2_approx(0.5f * d);
+  return sum * h * h;
+}
+
 __device__ __forceinline__ float rcp_approx(float x) {
   float y;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -214,7 +223,7 @@ __device__ __forceinline__ void finish_row(const A &a, const Rows &rows, int q0,
 // Joins the parts of a unit that blocks i0..i1 left, in the order of the key axis.  Block-collective.  What it costs
 // is waiting for loads, 0.7 us a time, so a thread keeps those of AHEAD parts in flight: the 33 parts of one token over
 // 4097 keys take 22 us in all with 2, 16 with 4, 14 with 8, no less with 16.
-template <typename T, int D, int ROWS, int NT, int ITEMS, int AHEAD, typename A, typename Rows>
+template <typename T, int D, int ROWS, int NT, int ITEMS, int AHEAD, bool WIDE, typename A, typename Rows>
 __device__ __forceinline__ void join_parts(const A &a, const Rows &covered, const Cursor &c, i64 row0, int rows, u32 i0, u32 i1) {
   const int items = rows * (D / 4);
   for (int x0 = (int)threadIdx.x; x0 < items; x0 += NT * ITEMS) {
@@ -244,13 +253,13 @@ __device__ __forceinline__ void join_parts(const A &a, const Rows &covered, cons
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) now = fmaxf(now, ml[k][j].x);
         const float base = now == -INFINITY ? 0.0f : now, f = exp2_approx(top[k] - base);
+        sum[k] = moved_sum<WIDE>(sum[k], top[k] - base);
         top[k] = now;
-        sum[k] *= f;
         acc[k].x *= f; acc[k].y *= f; acc[k].z *= f; acc[k].w *= f;
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
           const float g = exp2_approx(ml[k][j].x - base);
-          sum[k] += g * ml[k][j].y;
+          sum[k] += WIDE ? moved_sum<WIDE>(ml[k][j].y, ml[k][j].x - base) : g * ml[k][j].y;
           acc[k].x += g * v[k][j].x; acc[k].y += g * v[k][j].y; acc[k].z += g * v[k][j].z; acc[k].w += g * v[k][j].w;
         }
       }

@@ -333,7 +333,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<D>) attention_rows_kern
         __threadfence();
       }
       __syncthreads();
-      if (sh.last) join_parts<T, D, kRows, kThreads, 1, 8>(a, covered, c, row0, rows, i0, i1);
+      if (sh.last) join_parts<T, D, kRows, kThreads, 1, 8, false>(a, covered, c, row0, rows, i0, i1);
     }
     __syncthreads();
     stage = stage + 1 == kStages ? 0 : stage + 1;

@@ -125,3 +125,16 @@ def test_a_later_value_changes_no_score_of_any_kind(gorio, dim, opts):
         c.vs[page, :, place] = old * up
         got = c.run(gorio)
         assert torch.equal(got["out"][:248], want["out"][:248]) and torch.equal(got["lse"][:248], want["lse"][:248])
+
+
+@pytest.mark.parametrize("form", [E4M3, INT8])
+@pytest.mark.parametrize("new", [1, 5, 100])
+@pytest.mark.parametrize("length", [400, 9000])
+@pytest.mark.parametrize("first,then", [(2.0 ** -75, 2.0 ** 65), (2.0 ** 65, 2.0 ** -75), (0.0, 2.0 ** 65)])
+def test_scales_from_one_end_of_the_range_to_the_other(gorio, form, new, length, first, then):
+    """The first keys' scales and the others' lie 140 powers of two apart: weights of both count in the sums."""
+    c = Coded([new], [length], heads=4, kv_heads=1, dim=64, form=form, uneven=0.5, sharp=0.5)
+    pages, places = keys_of(c, 0, torch.arange(length, device="cuda"))
+    c.vs[pages, :, places] *= torch.where(torch.arange(length, device="cuda") < length // 3, first, then)[:, None]
+    c.tables = widen(c.tables, c.page)
+    check(c, c.run(gorio))
