@@ -371,7 +371,16 @@ __global__ void __launch_bounds__(kThreads, 1) attention_chunk_kernel(const __gr
   mma_fence_after();
   const u32 tmem = sh.tmem;
   const WaitLimit limit{a.wait_ticks, &sh.failed};
-  auto wait = [&](u64 *bar, u32 parity) { return warp_wait(bar, parity, limit); };
+  // A kernel that may begin before the one before it has ended waits for that one's end without a limit, at a row's end; a warp's first wait that passes
+  // the limit meanwhile does so too, and counts from there.
+  bool alone = !Overlaps<A>::value;
+  auto wait = [&](u64 *bar, u32 parity) {
+    return warp_wait(bar, parity, limit, [&] {
+      if (alone) return false;
+      wait_for_first(a);
+      return alone = true;
+    });
+  };
   // the part that is told `no`-th; false at the end
   auto take_part = [&](u32 no, PartInfo &p) {
     if (!wait(&sh.part_full[no % kParts], (no / kParts) & 1)) return false;

@@ -29,22 +29,30 @@ __device__ __forceinline__ bool bar_try(u64 *bar, u32 parity) {
 // Waits of a whole warp for the phase of the given parity, with one answer for all its lanes: what follows a wait (tensor memory,
 // votes) needs them together, and decided lane by lane some could see the phase end and others the limit pass.  False once a
 // wait of this block has lasted longer than its limit: the warp then leaves its loops, and the block ends with its error word set.
+// `anew` is asked when the limit has passed: true where the time until now does not count.
 struct WaitLimit {
   u32 ticks;               // of 1024 ns
   volatile u32 *failed;    // of the block
 };
 __device__ __forceinline__ u32 now_ticks() { return (u32)(now_ns() >> 10); }
-__device__ __forceinline__ bool warp_wait(u64 *bar, u32 parity, const WaitLimit &limit) {
+template <typename Anew>
+__device__ __forceinline__ bool warp_wait(u64 *bar, u32 parity, const WaitLimit &limit, const Anew &anew) {
   bool ok = bar_try(bar, parity);
   if (!__all_sync(0xffffffffu, ok)) {
-    const u32 t0 = now_ticks();
+    u32 t0 = now_ticks();
     do {
-      if (now_ticks() - t0 >= limit.ticks) *limit.failed = 1;
+      if (now_ticks() - t0 >= limit.ticks) {
+        if (anew()) t0 = now_ticks();
+        else *limit.failed = 1;
+      }
       if (__any_sync(0xffffffffu, *limit.failed)) return false;
       ok = bar_try(bar, parity);
     } while (!__all_sync(0xffffffffu, ok));
   }
   return true;
+}
+__device__ __forceinline__ bool warp_wait(u64 *bar, u32 parity, const WaitLimit &limit) {
+  return warp_wait(bar, parity, limit, [] { return false; });
 }
 // A wait for what this block itself has set going and nothing can hold up: no reason to give up early.
 __device__ __forceinline__ void drain(u64 *bar, u32 parity) {
