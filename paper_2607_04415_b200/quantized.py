@@ -86,8 +86,8 @@ def cache_store_quantized(keys: torch.Tensor, values: torch.Tensor, key_pages: t
 def cache_load_quantized(key_pages: torch.Tensor, value_pages: torch.Tensor, key_scales: torch.Tensor, value_scales: torch.Tensor, slots: torch.Tensor,
                          dtype: torch.dtype = torch.bfloat16, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,
                          stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
-    """Keys and values of the slots, [tokens, heads, head size] of `dtype` (gorio_cache_load_quantized), new or in the two tensors of `out`;
-    zeros for a negative slot."""
+    """Keys and values of the slots, [tokens, heads, head size] of `dtype` (gorio_cache_load_quantized), new or in the two tensors of `out`, which have to
+    be of that type; zeros for a negative slot.  There is no backward pass."""
     if stream is not None:
         with _on(stream, "key_pages", key_pages):
             return cache_load_quantized(key_pages, value_pages, key_scales, value_scales, slots, dtype, out)
@@ -101,6 +101,8 @@ def cache_load_quantized(key_pages: torch.Tensor, value_pages: torch.Tensor, key
         out = key_pages.new_empty(shape, dtype=dtype), key_pages.new_empty(shape, dtype=dtype)
     keys, values = out
     _move(False, keys, values, key_pages, value_pages, key_scales, value_scales, slots, index, dtype)
+    if key_scales.requires_grad or value_scales.requires_grad or key_pages.requires_grad or value_pages.requires_grad:
+        return _without_gradient(keys, values, (key_pages, value_pages, key_scales, value_scales))
     return keys, values
 
 
@@ -125,6 +127,7 @@ def paged_attention_quantized(q: torch.Tensor, key_pages: torch.Tensor, value_pa
     st = _call(lib.gorio_paged_attention_quantized, desc, index)
     if st:
         _fail(lib, st)
-    if q.requires_grad or key_scales.requires_grad or value_scales.requires_grad or slopes is not None:
-        out, lse = _without_gradient(out, lse, (q, key_scales, value_scales, slopes))
+    if (q.requires_grad or key_scales.requires_grad or value_scales.requires_grad or key_pages.requires_grad or value_pages.requires_grad
+            or slopes is not None):
+        out, lse = _without_gradient(out, lse, (q, key_pages, value_pages, key_scales, value_scales, slopes))
     return dict(out=out, lse=lse)
