@@ -112,18 +112,19 @@ class _NoBackward(torch.autograd.Function):
     """Hands results on, and refuses to go back through them."""
 
     @staticmethod
-    def forward(ctx, out, lse, *inputs):
+    def forward(ctx, call, out, lse, *inputs):
+        ctx.call = call
         return out, lse
 
     @staticmethod
     def backward(ctx, *gradients):
-        raise _invalid("paged_attention has no backward pass: its gradients do not exist (torch.no_grad() or detach() says that none are meant)")
+        raise _invalid(f"{ctx.call} has no backward pass: its gradients do not exist (torch.no_grad() or detach() says that none are meant)")
 
 
-def _without_gradient(out, lse, inputs):
+def _without_gradient(out, lse, inputs, call="paged_attention"):
     """The results as they are, or, where an input asks for a gradient, as results whose backward pass raises."""
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in inputs):
-        return _NoBackward.apply(out, lse, *inputs)
+        return _NoBackward.apply(call, out, lse, *inputs)
     return out, lse
 
 

@@ -94,5 +94,5 @@ def prefix_attention(q: torch.Tensor, key_pages: torch.Tensor, value_pages: torc
     if st:
         _fail(lib, st)
     if q.requires_grad or key_pages.requires_grad or value_pages.requires_grad or slopes is not None:
-        out, lse = _without_gradient(out, lse, (q, key_pages, value_pages, slopes))
+        out, lse = _without_gradient(out, lse, (q, key_pages, value_pages, slopes), "prefix_attention")
     return dict(out=out, lse=lse)

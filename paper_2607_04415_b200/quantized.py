@@ -102,7 +102,7 @@ def cache_load_quantized(key_pages: torch.Tensor, value_pages: torch.Tensor, key
     keys, values = out
     _move(False, keys, values, key_pages, value_pages, key_scales, value_scales, slots, index, dtype)
     if key_scales.requires_grad or value_scales.requires_grad or key_pages.requires_grad or value_pages.requires_grad:
-        return _without_gradient(keys, values, (key_pages, value_pages, key_scales, value_scales))
+        return _without_gradient(keys, values, (key_pages, value_pages, key_scales, value_scales), "cache_load_quantized")
     return keys, values
 
 
@@ -129,5 +129,5 @@ def paged_attention_quantized(q: torch.Tensor, key_pages: torch.Tensor, value_pa
         _fail(lib, st)
     if (q.requires_grad or key_scales.requires_grad or value_scales.requires_grad or key_pages.requires_grad or value_pages.requires_grad
             or slopes is not None):
-        out, lse = _without_gradient(out, lse, (q, key_pages, value_pages, key_scales, value_scales, slopes))
+        out, lse = _without_gradient(out, lse, (q, key_pages, value_pages, key_scales, value_scales, slopes), "paged_attention_quantized")
     return dict(out=out, lse=lse)

@@ -13,6 +13,16 @@ def gorio():
     return g
 
 
+def test_refusals_name_their_call(gorio):
+    from paper_2607_04415_b200 import paged
+    out, asks = torch.ones(4), torch.zeros(3, requires_grad=True)
+    for more, call in (((), "paged_attention"), (("prefix_attention",), "prefix_attention"), (("cache_load_quantized",), "cache_load_quantized")):
+        for x in paged._without_gradient(out, out.clone(), (asks, None), *more):
+            with pytest.raises(gorio.GorioError) as e:
+                x.sum().backward()
+            assert str(e.value).split(": ", 1)[1].startswith(call + " has no backward pass")
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("name", ["ks", "vs", "kp", "vp"])
 def test_caches_that_ask_for_a_gradient(gorio, name):
@@ -30,12 +40,12 @@ def test_caches_that_ask_for_a_gradient(gorio, name):
     for got in (load(), load(out=(wide[:, :4], wide[:, 4:]))):
         for x, y in zip(got, want):
             assert torch.equal(x.detach(), y)
-            with pytest.raises(gorio.GorioError):
+            with pytest.raises(gorio.GorioError, match="cache_load_quantized"):
                 x.float().sum().backward()
     assert torch.equal(wide[:, :4], want[0]) and torch.equal(wide[:, 4:], want[1])
     got = c.run(gorio)
     for k in ("out", "lse"):
         assert torch.equal(got[k].detach(), attended[k])
-        with pytest.raises(gorio.GorioError):
+        with pytest.raises(gorio.GorioError, match="paged_attention_quantized"):
             got[k].float().sum().backward()
     assert getattr(c, name).grad is None
