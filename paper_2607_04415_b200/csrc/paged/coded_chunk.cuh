@@ -9,12 +9,12 @@
 //   10        finds the logarithms of the scales of a tile's values, and their range.
 //   11        walks the block's share of the work and tells the others its parts.
 //   12-15     take codes apart, in place, into the 16-bit tiles that the products read.  (With a ring of their own for codes three pieces of 64 keys
-//             were all that shared memory held beside them, too few on their way: 972 us where this takes 674 for 2048 tokens over 18432 keys.)
+//             were all that shared memory held beside them, too few on their way: 972 us where this takes 671 for 2048 tokens over 18432 keys.)
 // Keys and values become their codes, exactly.  A score is multiplied by its key's scale in 32 bits, and a weight by its value's before it is rounded, once, to
 // float16: 2^(x - m) * scale.  So that weights use that type's range whatever the scales are, m follows the maximum of x + log2(scale), as in the kernel of few rows.
 // Where a row sees all of a tile and the tile's scales lie within 2^4 of each other, the largest x and the largest scale stand for it, at most 4 more; elsewhere it is found
 // key by key, where it may move m.  So a row's weights are the same whatever scales the keys have that it does not see.  (Key by key in every tile is 128 numbers more
-// from shared memory for each row: 771 us where this takes 674 for 2048 tokens over 18432 keys; scales within the exponent, 2^(x + log2(scale) - m), which the
+// from shared memory for each row: 771 us where this takes 671 for 2048 tokens over 18432 keys; scales within the exponent, 2^(x + log2(scale) - m), which the
 // sum then takes back by a product, 861.  The largest scale in every tile loses the weights of rows whose own scales lie far below it.  With values
 // multiplied by their scales as they become float16, two roundings more, float16 results were 3.7e-4 off where this is 2.9e-4 off and a rounding is 2.1e-4.)
 //
@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
     constexpr int kCols = D % 64 == 0 ? 64 : 32;             // columns of the output that are worked on at a time
     constexpr float kLift = WeightLift<__half, 8>::value;
     const u32 lanes = (u32)(warp & 3) << 21;                 // this warp's 32 lanes of tensor memory
-    const u32 scores = tmem + kScores + t * 128 + lanes, outputs = tmem + kOutputs + t * D + lanes;
+    const u32 scores = tmem + kScores + t * 128 + lanes, outputs = scores + (kOutputs - kScores) + t * (D - 128);
     u32 s_phase = 0, o_phase = 0, meet_phase = 0, q_phase = 1;   // o_phase: a bit for each row tile's output
     u32 tile_no = 0;                                         // tiles of the parts before
     auto meet = [&]() {                                      // all eight warps, with the limit of every other wait
@@ -171,49 +171,48 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
     PartInfo p;
     bool fine = true;                                        // no wait of this warp has run out
     for (u32 no = 0; fine && take_part(no, p); ++no) {
-      const bool split = p.rows <= kTileRows;                // one row tile: key tiles by turns
-      const bool mine = t == 0 || !split;                    // whose rows this warpgroup writes
-      const int unit_row = (split ? 0 : t * kTileRows) + row, first = split ? t : 0;
-      const bool valid = unit_row < p.rows;
-      const Row r = row_of(a, p, (u32)p.row0 + (valid ? unit_row : 0));
-      float to_dot = 1.0f;
-      if (mine) {
-        // this thread's row of queries: float16, times a power of two
-        fine = wait(&sh.q_empty[t], q_phase);
-        q_phase ^= 1;
-        const u16 *src = (const u16 *)a.q + r.tok * a.q_t + (i64)r.head * a.q_h;
-        uint4 x[D / 8];
-        float top = 0.0f;
-#pragma unroll
-        for (int k = 0; k < D / 8; ++k) x[k] = valid ? *(const uint4 *)(src + 8 * k) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-        for (int k = 0; k < D / 8; ++k) {
-          const u32 w[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float2 v = unpack2<T>(w[i]);
-            top = fmaxf(top, fmaxf(fabsf(v.x), fabsf(v.y)));
-          }
-        }
-        const float f = query_factor(top);
-        to_dot = 1.0f / f;                                   // powers of two
-#pragma unroll
-        for (int k = 0; k < D / 8; ++k) {
-          u32 w[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float2 v = unpack2<T>(w[i]);
-            w[i] = pack2<__half>(v.x * f, v.y * f);
-          }
-          if (fine) *(uint4 *)(sh.q[t] + (k >> 3) * (kTileRows * 128) + row * 128 + (((k & 7) ^ (row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-        if (split && fine) sh.q_to_dot[row] = to_dot;
-        fence_async();
-        __syncwarp();
-        if (lane == 0 && fine) bar_arrive(&sh.q_full[t]);
-      }
       float m = -INFINITY, l = 0.0f;
       {
+        const bool split = p.rows <= kTileRows;                // one row tile: key tiles by turns
+        const int unit_row = (split ? 0 : t * kTileRows) + row, first = split ? t : 0;
+        const bool valid = unit_row < p.rows;
+        const Row r = row_of(a, p, (u32)p.row0 + (valid ? unit_row : 0));
+        float to_dot = 1.0f;
+        if (t == 0 || !split) {
+          // this thread's row of queries: float16, times a power of two
+          fine = wait(&sh.q_empty[t], q_phase);
+          q_phase ^= 1;
+          const u16 *src = (const u16 *)a.q + r.tok * a.q_t + (i64)r.head * a.q_h;
+          uint4 x[D / 8];
+          float top = 0.0f;
+#pragma unroll
+          for (int k = 0; k < D / 8; ++k) x[k] = valid ? *(const uint4 *)(src + 8 * k) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+          for (int k = 0; k < D / 8; ++k) {
+            const u32 w[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float2 v = unpack2<T>(w[i]);
+              top = fmaxf(top, fmaxf(fabsf(v.x), fabsf(v.y)));
+            }
+          }
+          const float f = query_factor(top);
+          to_dot = 1.0f / f;                                   // powers of two
+#pragma unroll
+          for (int k = 0; k < D / 8; ++k) {
+            u32 w[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float2 v = unpack2<T>(w[i]);
+              w[i] = pack2<__half>(v.x * f, v.y * f);
+            }
+            if (fine) *(uint4 *)(sh.q[t] + (k >> 3) * (kTileRows * 128) + row * 128 + (((k & 7) ^ (row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+          if (split && fine) sh.q_to_dot[row] = to_dot;
+          fence_async();
+          __syncwarp();
+          if (lane == 0 && fine) bar_arrive(&sh.q_full[t]);
+        }
         const float slope = SCORES != kPlain && a.slopes ? a.slopes[r.head] * kLog2e : 0.0f;
         for (int at = first; at < p.tiles && fine; at += split ? 2 : 1) {
           const u32 slot = (tile_no + (u32)at) % kScaleSlots;
@@ -289,7 +288,11 @@ __global__ void __launch_bounds__(kCodedThreads, 1) coded_chunk_kernel(const __g
           l = l0 + l1;
         }
       }
-      p = sh.part[no % kParts];                              // anew: kept through the tiles, it would take the registers that those are short of
+      // Anew: kept through the tiles, these would take the registers that those are short of.
+      p = sh.part[no % kParts];
+      const bool split = p.rows <= kTileRows, mine = t == 0 || !split;   // mine: whose rows this warpgroup writes
+      const int unit_row = (split ? 0 : t * kTileRows) + row;
+      const bool valid = unit_row < p.rows;
       tile_no += (u32)p.tiles;
       m -= kLift;                                            // what the weights and their sum count from
       const bool two = split && p.tiles > 1;                 // both warpgroups have a part of the same rows
