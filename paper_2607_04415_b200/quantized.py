@@ -113,7 +113,8 @@ def paged_attention_quantized(q: torch.Tensor, key_pages: torch.Tensor, value_pa
     """Attention of each request's new tokens over its keys and values in a quantised cache (gorio_paged_attention_quantized).
 
     q and the result are bfloat16 or float16, key_pages, value_pages, key_scales and value_scales as cache_store_quantized leaves them;
-    all else, the workspaces included, is as for paged_attention.  There is no backward pass."""
+    all else, the workspaces included, is as for paged_attention.  Prompts are several times faster where scales are contiguous along
+    a page.  There is no backward pass."""
     if stream is not None:
         with _on(stream, "q", q):
             return paged_attention_quantized(q, key_pages, value_pages, key_scales, value_scales, tables, lengths, starts, max_new, scale, causal, window,

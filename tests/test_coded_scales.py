@@ -138,3 +138,14 @@ def test_scales_from_one_end_of_the_range_to_the_other(gorio, form, new, length,
     c.vs[pages, :, places] *= torch.where(torch.arange(length, device="cuda") < length // 3, first, then)[:, None]
     c.tables = widen(c.tables, c.page)
     check(c, c.run(gorio))
+
+
+@pytest.mark.parametrize("form", [E4M3, INT8])
+@pytest.mark.parametrize("new", [1, 100])
+@pytest.mark.parametrize("first,then", [(1.0, 2.0 ** 96), (2.0 ** 96, 1.0), (2.0 ** 96, 2.0 ** 96), (2.0 ** -66, 2.0 ** 96)])
+def test_scales_near_the_largest_that_count(gorio, form, new, first, then):
+    c = Coded([new], [500], heads=4, kv_heads=1, dim=64, form=form, uneven=0.5, sharp=0.5)
+    pages, places = keys_of(c, 0, torch.arange(500, device="cuda"))
+    c.vs[pages, :, places] *= torch.where(torch.arange(500, device="cuda") < 200, first, then)[:, None]
+    c.tables = widen(c.tables, c.page)
+    check(c, c.run(gorio))
